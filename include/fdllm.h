@@ -426,6 +426,133 @@ fdllm_status fdllm_check_inputs(const void* logits, fdllm_dtype dtype, int B, in
  * compute-unit count). */
 fdllm_status fdllm_workspace_size(int B, int L, int V, fdllm_dtype dtype, size_t* bytes);
 
+/*
+ * ---------------------------------------------------------------------------
+ * The attention sublayer around a cache (Alg. 1: cache initialise, and the
+ * model call on the active block against it)
+ * ---------------------------------------------------------------------------
+ * A model call over a prompt norms and rotates its query and key heads, fills
+ * the cache and attends over the prompt itself (fdllm_qk_norm_rope,
+ * fdllm_prompt_attention).  A decoding step does the same for the tokens of
+ * the active block and attends over the cache (fdllm_qk_norm_rope,
+ * fdllm_cache_attention); with the suffix cached too (a dual cache), the
+ * block's keys and values replace those at its positions.
+ *
+ * Rows.  q [T, H, D], k and v [T, Hk, D]: a token's heads lie side by side, a
+ *   token starts q_stride (k_stride, v_stride) elements after the one before
+ *   (slices of a fused projection need no copy).  H is a multiple of Hk; query
+ *   head h reads key head h / (H / Hk).  Pointers and strides are multiples of
+ *   16 bytes.  Outputs are contiguous.
+ * Packed sequences.  cu_q [B + 1] int32: sequence b has the rows
+ *   [cu_q[b], cu_q[b + 1]) of the T.  A sequence whose two counts are not
+ *   0 <= cu_q[b] <= cu_q[b + 1] <= T, or that has more than max_q rows, is
+ *   left out: its rows of the outputs are not written.
+ * Masks.  A query at position p of its sequence sees the keys
+ *   j < min(len, (floor(p / blk) + 1) * blk): blk = 1 is the causal mask, blk
+ *   = 32 that of decoding in blocks of 32, blk = 0 stands for no mask.  The
+ *   queries of a sequence are its last tokens unless q_start says otherwise
+ *   (the first then has p = len - n, negative where there are more queries
+ *   than keys).  A query that sees no key gets out = 0 and lse = -inf.
+ * Values.  q, k, v of the rows of a sequence must be finite; whatever lies
+ *   between sequences or behind one's end (in a page, or past kv_len) is never
+ *   part of a result.
+ *
+ * The 4-bit cache: [n_pages, Hk, fdllm_cache_tile_bytes(D)] bytes, 16-byte
+ * aligned.  A page holds FDLLM_CACHE_PAGE = 64 tokens; slot s is token s % 64
+ * of page s / 64.  A tile is one page of one head: key codes, value codes, key
+ * scales, value scales.
+ *   codes  [D / 32][64][16]: byte n of a token's group holds elements 2 n (low
+ *          nibble) and 2 n + 1 of 32, as E2M1: sign, then one of 0, 0.5, 1,
+ *          1.5, 2, 3, 4, 6.
+ *   scales [64][S], S = D / 32 rounded up to a multiple of 4: byte g is
+ *          127 + e (E8M0) of group g; an element is 2^e times its code.
+ * A group is written with the smallest e >= -126 for which its largest
+ * magnitude is at most 7 * 2^e, each element rounded to the nearest code, ties
+ * to the even code, beyond 6 to 6.  A group that holds a NaN or an infinity
+ * gets the scale byte 255 and reads back as NaN.
+ */
+#define FDLLM_CACHE_PAGE 64
+
+/* Bytes of one page of one head; D a multiple of 32, 32 to 256. */
+fdllm_status fdllm_cache_tile_bytes(int D, size_t* bytes);
+
+/*
+ * The query and key heads before attention, and the cache's new entries, in
+ * one pass: y = x rsqrt(mean(x^2) + eps) w for every head of q and k, then the
+ * rotation of its first `rot` elements by the token's position; in float32,
+ * rounded once.
+ *   dtype: element type of q, k, v, q_out, k_out;
+ *   q_weight, k_weight [D] float: norm weights (NULL: no norm);
+ *   positions [T] int32: row of cos_sin for each token;
+ *   cos_sin [n_pos, rot] float: rot / 2 cosines, then rot / 2 sines;
+ *   rot: multiple of 16, at most D, 0 for none; a pair is (i, i + rot / 2), or
+ *   with interleaved != 0 (2 i, 2 i + 1): (a cos - b sin, b cos + a sin);
+ *   q_out [T, H, D], k_out [T, Hk, D]: may be q and k themselves where those
+ *   are contiguous; k_out may be NULL when cache is given;
+ *   cache (may be NULL): rotated keys (from float32) and the values as they
+ *   are go to slot slots[t] of token t (int32; one outside the n_pages pages,
+ *   such as -1, is not stored).  A call's slots must differ.
+ *   A token whose position is outside [0, n_pos) gets zeros in q_out and k_out
+ *   and is not stored (with rot = 0 positions are not looked at).
+ *   D: a multiple of 32, 32 to 256.
+ */
+fdllm_status fdllm_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                int64_t v_stride, fdllm_dtype dtype, int T, int H, int Hk, int D,
+                                const float* q_weight, const float* k_weight, float eps,
+                                const int32_t* positions, const float* cos_sin, int n_pos, int rot,
+                                int interleaved, void* q_out, void* k_out, uint8_t* cache, int n_pages,
+                                const int32_t* slots, fdllm_stream stream);
+
+/* Type in which the cache's entries are read back; both hold them exactly
+ * (E5M2 from 2^-16 to 57344). */
+typedef int fdllm_cache_out;
+enum { FDLLM_OUT_BF16 = 0, FDLLM_OUT_E5M2 = 1 };
+
+/*
+ * What the cache holds for T slots: k_out, v_out [T, Hk, D] (either may be
+ * NULL).  A slot outside the pages gives zeros.
+ */
+fdllm_status fdllm_cache_read(const uint8_t* cache, int n_pages, int Hk, int D, const int32_t* slots, int T,
+                              fdllm_cache_out out_type, void* k_out, void* v_out, fdllm_stream stream);
+
+/*
+ * Attention of at most max_q query tokens per sequence over the cache.
+ *   q [T, H, D] bf16; cu_q, max_q: above;
+ *   page_table [B, table_width] int32: page of tokens [64 i, 64 i + 64) of a
+ *   sequence; entries behind its end are not read, and the tokens of a page
+ *   outside [0, n_pages) count as unseen;
+ *   kv_len [B] int32: tokens in the cache (negative counts as 0, more than 64 *
+ *   table_width as that);
+ *   q_start [B] int32: position of a sequence's first query (NULL: kv_len less
+ *   its number of queries); only blk > 0 looks at it;
+ *   scale: > 0, usually 1 / sqrt(D);
+ *   out [T, H, D] bf16; lse [T, H] float: log of the sum of exp(scale q.k) (may
+ *   be NULL);
+ *   workspace: fdllm_cache_attention_workspace_size() bytes, 16-byte aligned,
+ *   scratch between calls.
+ *   D: 64, 96 or 128.  bf16 rounding of the weights exp(s - max) and of out;
+ *   scores, sums and maxima in float32.  For fixed sizes, lengths and tables a
+ *   call is bitwise reproducible.
+ */
+fdllm_status fdllm_cache_attention_workspace_size(int B, int H, int Hk, int D, int max_q, int table_width,
+                                                  size_t* bytes);
+fdllm_status fdllm_cache_attention(const void* q, int64_t q_stride, int T, const int32_t* cu_q, int B, int max_q,
+                                   int H, int Hk, int D, const uint8_t* cache, int n_pages,
+                                   const int32_t* page_table, int table_width, const int32_t* kv_len,
+                                   const int32_t* q_start, float scale, int blk, void* out, float* lse,
+                                   void* workspace, size_t workspace_bytes, fdllm_stream stream);
+
+/*
+ * Attention of whole packed sequences: queries q [T, H, D] over keys and
+ * values k, v [Tk, Hk, D], bf16, sequence b's rows given by cu_q and cu_k
+ * [B + 1] (the same array where a sequence attends to itself; more keys than
+ * queries where its first tokens are done).  Other arguments as above.
+ */
+fdllm_status fdllm_prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                    int64_t v_stride, int T, int Tk, const int32_t* cu_q, const int32_t* cu_k, int B,
+                                    int max_q, int H, int Hk, int D, float scale, int blk, void* out, float* lse,
+                                    fdllm_stream stream);
+
 /* Static, human-readable text for a status code. */
 const char* fdllm_status_string(fdllm_status status);
 

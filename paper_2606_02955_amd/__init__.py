@@ -28,6 +28,8 @@ OK = 0
 ERR_INVALID_ARG, ERR_UNSUPPORTED_DTYPE, ERR_SIZE, ERR_WORKSPACE, ERR_HIP = -1, -2, -3, -4, -5
 ERR_BOUNDS, ERR_BLOCK_TOO_LARGE, ERR_NONFINITE, ERR_SCRATCH = -6, -7, -8, -9
 MAX_ABS_LOGIT = 1.0e7
+CACHE_PAGE = 64
+OUT_BF16, OUT_E5M2 = 0, 1
 STATIC_SCRATCH_BYTES = 8 << 20
 
 EXPORTS = ("fdllm_confidence", "fdllm_select_profile", "fdllm_select_factor",
@@ -36,7 +38,9 @@ EXPORTS = ("fdllm_confidence", "fdllm_select_profile", "fdllm_select_factor",
            "fdllm_advance_blocks", "fdllm_generation_workspace_size", "fdllm_generation_create",
            "fdllm_generation_run", "fdllm_generation_destroy", "fdllm_lmhead_workspace_size",
            "fdllm_lmhead_confidence", "fdllm_lmhead_decode_step", "fdllm_check_inputs",
-           "fdllm_decode_step_static")
+           "fdllm_decode_step_static", "fdllm_cache_tile_bytes", "fdllm_qk_norm_rope",
+           "fdllm_cache_read", "fdllm_cache_attention_workspace_size", "fdllm_cache_attention",
+           "fdllm_prompt_attention")
 
 
 class GenerationDesc(ctypes.Structure):
@@ -100,7 +104,19 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.fdllm_generation_create.argtypes = [dp, ctypes.POINTER(vp)]
     lib.fdllm_generation_run.argtypes = [vp, vp, ctypes.POINTER(i32)]
     lib.fdllm_generation_destroy.argtypes = [vp]
-    for name in ("fdllm_confidence", "fdllm_reveal", "fdllm_decode_step", "fdllm_workspace_size",
+    i64 = ctypes.c_int64
+    lib.fdllm_cache_tile_bytes.argtypes = [i32, ctypes.POINTER(sz)]
+    lib.fdllm_qk_norm_rope.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, i32, vp, vp, f32, vp, vp,
+                                       i32, i32, i32, vp, vp, vp, i32, vp, vp]
+    lib.fdllm_cache_read.argtypes = [vp, i32, i32, i32, vp, i32, i32, vp, vp, vp]
+    lib.fdllm_cache_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.fdllm_cache_attention.argtypes = [vp, i64, i32, vp, i32, i32, i32, i32, i32, vp, i32, vp, i32, vp, vp,
+                                          f32, i32, vp, vp, vp, sz, vp]
+    lib.fdllm_prompt_attention.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, i32, i32, i32, i32, i32,
+                                           f32, i32, vp, vp, vp]
+    for name in ("fdllm_cache_tile_bytes", "fdllm_qk_norm_rope", "fdllm_cache_read",
+                 "fdllm_cache_attention_workspace_size", "fdllm_cache_attention", "fdllm_prompt_attention",
+                 "fdllm_confidence", "fdllm_reveal", "fdllm_decode_step", "fdllm_workspace_size",
                  "fdllm_decode_step_static", "fdllm_check_inputs",
                  "fdllm_synth_logits", "fdllm_advance_blocks", "fdllm_generation_workspace_size",
                  "fdllm_lmhead_workspace_size", "fdllm_lmhead_confidence", "fdllm_lmhead_decode_step",
@@ -430,6 +446,132 @@ def select(selector: str, conf, eps, mask, block_start, block_end, param, commit
     {"profile": fdllm_select_profile, "factor": fdllm_select_factor,
      "threshold": fdllm_select_threshold}[selector](conf, eps, mask, block_start, block_end,
                                                     param, commit, n_commit)
+
+
+def fdllm_cache_tile_bytes(head_dim: int) -> int:
+    """Bytes of one page (64 tokens) of one key head in the 4-bit cache (layout in fdllm.h)."""
+    n = ctypes.c_size_t(0)
+    _check(load().fdllm_cache_tile_bytes(int(head_dim), ctypes.byref(n)), "fdllm_cache_tile_bytes")
+    return int(n.value)
+
+
+def new_cache(n_pages: int, kv_heads: int, head_dim: int, device=None) -> torch.Tensor:
+    """A 4-bit cache of one layer, [n_pages, kv_heads, tile bytes], zeroed."""
+    return torch.zeros((n_pages, kv_heads, fdllm_cache_tile_bytes(head_dim)), dtype=torch.uint8,
+                       device=device if device is not None else "cuda")
+
+
+def _heads(t: torch.Tensor, name: str, dtype=None):
+    """Pointer and token stride of [T, heads, D] whose tokens may lie apart."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens, heads, head size], got {tuple(t.shape)}")
+    T, h, D = t.shape
+    if t.numel() and ((D > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != D)):
+        raise ValueError(f"{name}: the heads of a token must lie side by side")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    return ctypes.c_void_p(t.data_ptr()), t.stride(0) if T > 1 else h * D
+
+
+def _cache(cache: torch.Tensor, kv_heads: int, head_dim: int):
+    if cache.dim() != 3 or tuple(cache.shape[1:]) != (kv_heads, fdllm_cache_tile_bytes(head_dim)):
+        raise ValueError(f"cache must be [pages, {kv_heads}, {fdllm_cache_tile_bytes(head_dim)}], "
+                         f"got {tuple(cache.shape)}")
+    return _ptr(cache, torch.uint8, name="cache"), cache.shape[0]
+
+
+def fdllm_qk_norm_rope(q, k, v, positions, cos_sin, q_out, k_out=None, q_weight=None, k_weight=None,
+                       eps: float = 1e-6, interleaved: bool = False, cache=None, slots=None):
+    """Head norm and rotation of q and k, keys and values into the cache, in one
+    pass (see fdllm.h).  cos_sin None: no rotation; v is only read for a cache."""
+    T, H, D = q.shape
+    Hk = k.shape[1]
+    code = _dtype_code(q)
+    qp, qs = _heads(q, "q")
+    kp, ks = _heads(k, "k", q.dtype)
+    if tuple(k.shape) != (T, Hk, D):
+        raise ValueError(f"k must be [{T}, heads, {D}], got {tuple(k.shape)}")
+    vp, vs, cp, n_pages = None, 0, None, 0
+    if cache is not None:
+        if v is None or tuple(v.shape) != (T, Hk, D):
+            raise ValueError(f"v must be [{T}, {Hk}, {D}] to go into the cache")
+        vp, vs = _heads(v, "v", q.dtype)
+        cp, n_pages = _cache(cache, Hk, D)
+    n_pos, rot = (0, 0) if cos_sin is None else tuple(cos_sin.shape)
+    st = load().fdllm_qk_norm_rope(
+        qp, qs, kp, ks, vp, vs, code, T, H, Hk, D, _ptr(q_weight, torch.float32, (D,), "q_weight"),
+        _ptr(k_weight, torch.float32, (D,), "k_weight"), float(eps),
+        _ptr(positions, torch.int32, (T,), "positions"), _ptr(cos_sin, torch.float32, name="cos_sin"), n_pos, rot,
+        int(bool(interleaved)), _ptr(q_out, q.dtype, (T, H, D), "q_out"),
+        _ptr(k_out, q.dtype, (T, Hk, D), "k_out"), cp, n_pages, _ptr(slots, torch.int32, (T,), "slots"),
+        _stream(q.device))
+    _check(st, "fdllm_qk_norm_rope")
+
+
+def fdllm_cache_read(cache, slots, k_out=None, v_out=None):
+    """What the cache holds for the given slots, as bfloat16 or float8_e5m2 (see fdllm.h)."""
+    like = k_out if k_out is not None else v_out
+    if like is None:
+        raise ValueError("k_out or v_out must be given")
+    T, Hk, D = like.shape
+    if like.dtype not in (torch.bfloat16, torch.float8_e5m2):
+        raise ValueError(f"the cache is read as bfloat16 or float8_e5m2, got {like.dtype}")
+    cp, n_pages = _cache(cache, Hk, D)
+    st = load().fdllm_cache_read(
+        cp, n_pages, Hk, D, _ptr(slots, torch.int32, (T,), "slots"), T,
+        OUT_BF16 if like.dtype == torch.bfloat16 else OUT_E5M2, _ptr(k_out, like.dtype, (T, Hk, D), "k_out"),
+        _ptr(v_out, like.dtype, (T, Hk, D), "v_out"), _stream(cache.device))
+    _check(st, "fdllm_cache_read")
+
+
+def fdllm_cache_attention_workspace_size(B: int, H: int, Hk: int, D: int, max_q: int, table_width: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().fdllm_cache_attention_workspace_size(B, H, Hk, D, max_q, table_width, ctypes.byref(n)),
+           "fdllm_cache_attention_workspace_size")
+    return int(n.value)
+
+
+def fdllm_cache_attention(q, cache, page_table, kv_len, cu_q, out, max_q: int, lse=None,
+                          scale: Optional[float] = None, blk: int = 0, q_start=None, workspace=None):
+    """Attention of q's tokens over the 4-bit cache (see fdllm.h).  scale
+    defaults to 1 / sqrt(head size); returns the workspace for reuse."""
+    T, H, D = q.shape
+    Hk = cache.shape[1]
+    B, width = page_table.shape
+    qp, qs = _heads(q, "q", torch.bfloat16)
+    cp, n_pages = _cache(cache, Hk, D)
+    if workspace is None:
+        workspace = torch.empty(fdllm_cache_attention_workspace_size(B, H, Hk, D, int(max_q), width),
+                                dtype=torch.uint8, device=q.device)
+    st = load().fdllm_cache_attention(
+        qp, qs, T, _ptr(cu_q, torch.int32, (B + 1,), "cu_q"), B, int(max_q), H, Hk, D, cp, n_pages,
+        _ptr(page_table, torch.int32, name="page_table"), width, _ptr(kv_len, torch.int32, (B,), "kv_len"),
+        _ptr(q_start, torch.int32, (B,), "q_start"), D ** -0.5 if scale is None else float(scale), int(blk),
+        _ptr(out, torch.bfloat16, (T, H, D), "out"), _ptr(lse, torch.float32, (T, H), "lse"),
+        _ptr(workspace, name="workspace"), workspace.numel() * workspace.element_size(), _stream(q.device))
+    _check(st, "fdllm_cache_attention")
+    return workspace
+
+
+def fdllm_prompt_attention(q, k, v, cu_q, cu_k, out, max_q: int, lse=None, scale: Optional[float] = None,
+                           blk: int = 0):
+    """Attention of packed sequences (see fdllm.h); scale defaults to 1 / sqrt(head size)."""
+    T, H, D = q.shape
+    Tk, Hk = k.shape[:2]
+    if tuple(k.shape) != (Tk, Hk, D) or tuple(v.shape) != (Tk, Hk, D):
+        raise ValueError(f"k and v must be [{Tk}, {Hk}, {D}], got {tuple(k.shape)} and {tuple(v.shape)}")
+    B = cu_q.shape[0] - 1
+    qp, qs = _heads(q, "q", torch.bfloat16)
+    kp, ks = _heads(k, "k", torch.bfloat16)
+    vp, vs = _heads(v, "v", torch.bfloat16)
+    st = load().fdllm_prompt_attention(
+        qp, qs, kp, ks, vp, vs, T, Tk, _ptr(cu_q, torch.int32, (B + 1,), "cu_q"),
+        _ptr(cu_k, torch.int32, (B + 1,), "cu_k"), B, int(max_q), H, Hk, D,
+        D ** -0.5 if scale is None else float(scale), int(blk), _ptr(out, torch.bfloat16, (T, H, D), "out"),
+        _ptr(lse, torch.float32, (T, H), "lse"), _stream(q.device))
+    _check(st, "fdllm_prompt_attention")
 
 
 def load_bench(path: Optional[str] = None) -> ctypes.CDLL:
