@@ -504,7 +504,8 @@ fdllm_status fdllm_qk_norm_rope(const void* q, int64_t q_stride, const void* k, 
                                 const int32_t* slots, fdllm_stream stream);
 
 /* Type in which the cache's entries are read back; both hold them exactly
- * (E5M2 from 2^-16 to 57344). */
+ * (bf16 but for 2^128, to which elements from 2.9e38 on may round: infinity;
+ * E5M2 from 2^-16 to 57344). */
 typedef int fdllm_cache_out;
 enum { FDLLM_OUT_BF16 = 0, FDLLM_OUT_E5M2 = 1 };
 
@@ -546,12 +547,15 @@ fdllm_status fdllm_cache_attention(const void* q, int64_t q_stride, int T, const
  * Attention of whole packed sequences: queries q [T, H, D] over keys and
  * values k, v [Tk, Hk, D], bf16, sequence b's rows given by cu_q and cu_k
  * [B + 1] (the same array where a sequence attends to itself; more keys than
- * queries where its first tokens are done).  Other arguments as above.
+ * queries where its first tokens are done).  workspace:
+ * fdllm_prompt_attention_workspace_size() bytes, 16-byte aligned (NULL where
+ * that is 0).  Other arguments as above.
  */
+fdllm_status fdllm_prompt_attention_workspace_size(int B, int Tk, int H, int Hk, int D, int max_q, size_t* bytes);
 fdllm_status fdllm_prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                     int64_t v_stride, int T, int Tk, const int32_t* cu_q, const int32_t* cu_k, int B,
                                     int max_q, int H, int Hk, int D, float scale, int blk, void* out, float* lse,
-                                    fdllm_stream stream);
+                                    void* workspace, size_t workspace_bytes, fdllm_stream stream);
 
 /* Static, human-readable text for a status code. */
 const char* fdllm_status_string(fdllm_status status);

@@ -40,7 +40,7 @@ EXPORTS = ("fdllm_confidence", "fdllm_select_profile", "fdllm_select_factor",
            "fdllm_lmhead_confidence", "fdllm_lmhead_decode_step", "fdllm_check_inputs",
            "fdllm_decode_step_static", "fdllm_cache_tile_bytes", "fdllm_qk_norm_rope",
            "fdllm_cache_read", "fdllm_cache_attention_workspace_size", "fdllm_cache_attention",
-           "fdllm_prompt_attention")
+           "fdllm_prompt_attention_workspace_size", "fdllm_prompt_attention")
 
 
 class GenerationDesc(ctypes.Structure):
@@ -113,10 +113,11 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.fdllm_cache_attention.argtypes = [vp, i64, i32, vp, i32, i32, i32, i32, i32, vp, i32, vp, i32, vp, vp,
                                           f32, i32, vp, vp, vp, sz, vp]
     lib.fdllm_prompt_attention.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, i32, i32, i32, i32, i32,
-                                           f32, i32, vp, vp, vp]
+                                           f32, i32, vp, vp, vp, sz, vp]
+    lib.fdllm_prompt_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
     for name in ("fdllm_cache_tile_bytes", "fdllm_qk_norm_rope", "fdllm_cache_read",
-                 "fdllm_cache_attention_workspace_size", "fdllm_cache_attention", "fdllm_prompt_attention",
-                 "fdllm_confidence", "fdllm_reveal", "fdllm_decode_step", "fdllm_workspace_size",
+                 "fdllm_cache_attention_workspace_size", "fdllm_cache_attention",
+                 "fdllm_prompt_attention_workspace_size", "fdllm_prompt_attention", "fdllm_confidence", "fdllm_reveal", "fdllm_decode_step", "fdllm_workspace_size",
                  "fdllm_decode_step_static", "fdllm_check_inputs",
                  "fdllm_synth_logits", "fdllm_advance_blocks", "fdllm_generation_workspace_size",
                  "fdllm_lmhead_workspace_size", "fdllm_lmhead_confidence", "fdllm_lmhead_decode_step",
@@ -555,9 +556,17 @@ def fdllm_cache_attention(q, cache, page_table, kv_len, cu_q, out, max_q: int, l
     return workspace
 
 
+def fdllm_prompt_attention_workspace_size(B: int, Tk: int, H: int, Hk: int, D: int, max_q: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().fdllm_prompt_attention_workspace_size(B, Tk, H, Hk, D, max_q, ctypes.byref(n)),
+           "fdllm_prompt_attention_workspace_size")
+    return int(n.value)
+
+
 def fdllm_prompt_attention(q, k, v, cu_q, cu_k, out, max_q: int, lse=None, scale: Optional[float] = None,
-                           blk: int = 0):
-    """Attention of packed sequences (see fdllm.h); scale defaults to 1 / sqrt(head size)."""
+                           blk: int = 0, workspace=None):
+    """Attention of packed sequences (see fdllm.h); scale defaults to 1 / sqrt(head
+    size); returns the workspace (None where the call needs none)."""
     T, H, D = q.shape
     Tk, Hk = k.shape[:2]
     if tuple(k.shape) != (Tk, Hk, D) or tuple(v.shape) != (Tk, Hk, D):
@@ -566,12 +575,18 @@ def fdllm_prompt_attention(q, k, v, cu_q, cu_k, out, max_q: int, lse=None, scale
     qp, qs = _heads(q, "q", torch.bfloat16)
     kp, ks = _heads(k, "k", torch.bfloat16)
     vp, vs = _heads(v, "v", torch.bfloat16)
+    if workspace is None:
+        need = fdllm_prompt_attention_workspace_size(B, Tk, H, Hk, D, int(max_q))
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     st = load().fdllm_prompt_attention(
         qp, qs, kp, ks, vp, vs, T, Tk, _ptr(cu_q, torch.int32, (B + 1,), "cu_q"),
         _ptr(cu_k, torch.int32, (B + 1,), "cu_k"), B, int(max_q), H, Hk, D,
         D ** -0.5 if scale is None else float(scale), int(blk), _ptr(out, torch.bfloat16, (T, H, D), "out"),
-        _ptr(lse, torch.float32, (T, H), "lse"), _stream(q.device))
+        _ptr(lse, torch.float32, (T, H), "lse"),
+        _ptr(workspace, name="workspace"), ws_bytes, _stream(q.device))
     _check(st, "fdllm_prompt_attention")
+    return workspace
 
 
 def load_bench(path: Optional[str] = None) -> ctypes.CDLL:

@@ -9,17 +9,18 @@
 // key head are the rows of one product; a (sequence, key head, group of rows)
 // is an item, a page of its cache a unit of work.
 //
-// K: the scaled matrix instruction takes the cache's 4-bit codes and their
-// scales as they lie in memory; no key is ever unpacked.  Its other operand
-// must have at most 8 bits, so a query is the sum of two E4M3 numbers: a
-// bfloat16's 8 significant bits are 4 and 4 of theirs, exactly, down to 2^-16
-// of the row's largest element.
-// V: unpacked to bfloat16 (exact: a code has two significant bits, its scale
-// none) into LDS and read back transposed as the second product's operand.
+// Keys and values are unpacked to bfloat16 (exact: a code has two significant
+// bits, its scale none): the keys in registers, as the first product's operand,
+// the values into LDS, to be read back transposed as the second's.
+//
+// Each workgroup takes an equal share of all units, whatever the sequences'
+// lengths; an item that lies in several shares is joined afterwards, in the
+// order of its pages.
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "attn_common.h"
@@ -29,8 +30,6 @@ namespace fdllm {
 
 constexpr int kCaThreads = 256;
 constexpr int kCaWaves = kCaThreads / kWave;
-constexpr int kHalf = kPage / 2;            // keys whose values are in LDS at a time
-constexpr int kCaRowFloats = 2;             // m and l beside a row's partial sums
 
 struct CacheAttnArgs {
   const uint16_t* q;
@@ -47,7 +46,9 @@ struct CacheAttnArgs {
   float c;                    // scale * log2 e
   uint16_t* out;
   float* lse;
-  float* part;                // [workgroups][2][rows][D + 2]
+  int32_t* plan;              // units of all sequences, then those before each
+  float* part_ml;             // [workgroups][2][rows][2]: reference and sum of a partial result
+  float* part;                // [workgroups][2][rows][D]
 };
 
 // A sequence as the plan sees it: its query rows, pages and groups of rows.
@@ -66,11 +67,11 @@ __device__ __forceinline__ Seq sequence(const CacheAttnArgs& a, int b) {
   return s;
 }
 
-// Units of all sequences, and the sequence and offset at which unit `u` lies.
+// Units of the sequences before b0, by all threads of a workgroup.
 template <int Rows>
-__device__ __forceinline__ int total_units(const CacheAttnArgs& a, int* s_sum) {
+__device__ __forceinline__ int units_before(const CacheAttnArgs& a, int b0, int* s_sum) {
   int n = 0;
-  for (int b = threadIdx.x; b < a.B; b += kCaThreads) {
+  for (int b = threadIdx.x; b < b0; b += kCaThreads) {
     const Seq s = sequence<Rows>(a, b);
     n += s.groups * s.pages;
   }
@@ -85,14 +86,6 @@ __device__ __forceinline__ int total_units(const CacheAttnArgs& a, int* s_sum) {
   return n * a.Hk;
 }
 
-// Units before sequence b0 (all of a.B: total_units).
-template <int Rows>
-__device__ __forceinline__ int units_before(const CacheAttnArgs& a, int b0, int* s_sum) {
-  CacheAttnArgs c = a;
-  c.B = b0;
-  return total_units<Rows>(c, s_sum);
-}
-
 // First unit of workgroup g's share.
 __device__ __forceinline__ int share_begin(int g, int groups, int units) {
   return (int)((long long)g * units / groups);
@@ -105,35 +98,6 @@ __device__ __forceinline__ int share_of(int u, int groups, int units) {
   return g;
 }
 
-// --- queries as pairs of E4M3 ---------------------------------------------
-struct PairScale {
-  float mul;        // 2^-e: the row's largest magnitude comes to lie in (128, 256]
-  int hi, lo;       // scale bytes of the two parts
-};
-
-__device__ __forceinline__ PairScale pair_scale(float top) {
-  int e = (int)(__float_as_uint(top) >> 23) - 127 - 7;
-  e = e < -100 ? -100 : e;
-  PairScale p;
-  p.mul = scale_of((uint32_t)(127 - e));
-  p.hi = 127 + e;
-  p.lo = 127 + e - 4;
-  return p;
-}
-
-// Four elements: hi = E4M3(x), lo = E4M3(16 (x - hi)).
-__device__ __forceinline__ void split4(const float* x, int* hi, int* lo) {
-  int h = 0, l = 0;
-  h = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], h, false);
-  h = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], h, true);
-  const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(h, false);
-  const auto b = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
-  l = __builtin_amdgcn_cvt_pk_fp8_f32((x[0] - a[0]) * 16.0f, (x[1] - a[1]) * 16.0f, l, false);
-  l = __builtin_amdgcn_cvt_pk_fp8_f32((x[2] - b[0]) * 16.0f, (x[3] - b[1]) * 16.0f, l, true);
-  *hi = h;
-  *lo = l;
-}
-
 // ---------------------------------------------------------------------------
 // NG: groups of 32 elements of a head.  MT: rows of a wave's tile, 16 or 32.
 // WR: waves that hold different rows of an item; the 4 / WR sets of them take
@@ -144,37 +108,114 @@ struct CaShape {
   static constexpr int D = NG * kGroup;
   static constexpr int WK = kCaWaves / WR;
   static constexpr int Rows = MT * WR;
-  static constexpr int RowBytes = 2 * D + 32;              // of a key's values in LDS
-  static constexpr int HalfBytes = kHalf * RowBytes;
+  static constexpr int RowBytes = 2 * D + 32;              // of a key's values in LDS: transposed reads meet no bank twice
+  static constexpr int PageBytes = kPage * RowBytes;
   static constexpr int Buffers = WR > 1 ? 2 : 1;
-  static constexpr int ValueBytes = WK * Buffers * HalfBytes;
+  static constexpr int ValueBytes = WK * Buffers * PageBytes;
   static constexpr int JoinBytes = WK > 1 ? (WK / 2) * Rows * (D + 4) * 4 : 0;
   static constexpr int LdsBytes = ValueBytes > JoinBytes ? ValueBytes : JoinBytes;
   static constexpr int DT = MT == 32 ? NG : 2 * NG;        // tiles of D of the second product
   static constexpr int OR = MT == 32 ? 16 : 4;             // registers of one
-  static constexpr int QS = MT == 32 ? (NG + 1) / 2 : 1;   // steps of the first product
+  static constexpr int SPT = kPage / MT;                   // subtiles of MT keys in a page
+  static constexpr int Steps = MT == 32 ? 2 * NG : NG;     // steps of the first product
+  static constexpr int VPairs = kPage * NG;                // (key, group) pairs of a page's values
+  static constexpr int VPer = (VPairs + WR * kWave - 1) / (WR * kWave);   // of them a lane unpacks
 };
+
+// Where in a head's row the first product's operand of step s begins for a
+// lane: any order of the elements will do that is the same for both operands,
+// and this one lets a lane take its keys' codes in 16-byte pieces.
+template <int NG, int MT>
+__device__ __forceinline__ int element_of(int s, int part) {
+  if constexpr (MT == 32) {   // halves take the groups of a pair; an odd last group is halved
+    if (NG % 2 == 0 || s < 4 * (NG / 2)) return 32 * (2 * (s / 4) + part) + 8 * (s % 4);
+    return 32 * (NG - 1) + 16 * part + 8 * (s % 4);
+  } else if constexpr (NG == 4) {   // a group a quarter
+    return 32 * part + 8 * s;
+  } else if constexpr (NG == 2) {   // half a group
+    return 32 * (part / 2) + 16 * (part % 2) + 8 * s;
+  } else {
+    return 32 * s + 8 * part;
+  }
+}
+
+// Codes and scales of one page for one lane.
+template <int NG, int MT, int WR>
+struct PageRegs {
+  typedef CaShape<NG, MT, WR> S;
+  uint32_t k[S::SPT][S::Steps];   // eight codes a step
+  uint32_t ks[S::SPT];            // scales of the lane's key of a subtile
+  u32x4 v[S::VPer];
+  uint32_t vs[S::VPer];
+  bool there;
+
+  __device__ __forceinline__ void load(const CacheAttnArgs& a, int page, int h, int lane, int wr) {
+    there = page >= 0 && page < a.n_pages;
+    const uint8_t* tile = a.cache + ((size_t)(there ? page : 0) * a.Hk + h) * tile_bytes(S::D);
+    const int col = lane % MT, part = lane / MT;
+#pragma unroll
+    for (int x = 0; x < S::SPT; ++x) {
+      const uint8_t* codes = tile + (x * MT + col) * kCodeBytes;
+      ks[x] = *(const uint32_t*)(tile + k_scales_at(S::D) + (x * MT + col) * scale_stride(S::D));
+      if constexpr (MT == 32 || NG == 4) {
+#pragma unroll
+        for (int i = 0; i < S::Steps / 4; ++i) {
+          const u32x4 c = *(const u32x4*)(codes + (MT == 32 ? 2 * i + part : part) * kPage * kCodeBytes);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) k[x][4 * i + j] = c[j];
+        }
+        if constexpr (S::Steps % 4 != 0) {
+          const u32x2 c = *(const u32x2*)(codes + (NG - 1) * kPage * kCodeBytes + 8 * part);
+          k[x][S::Steps - 2] = c[0];
+          k[x][S::Steps - 1] = c[1];
+        }
+      } else if constexpr (NG == 2) {
+        const u32x2 c = *(const u32x2*)(codes + (part / 2) * kPage * kCodeBytes + 8 * (part % 2));
+        k[x][0] = c[0];
+        k[x][1] = c[1];
+      } else {
+#pragma unroll
+        for (int s = 0; s < S::Steps; ++s) k[x][s] = *(const uint32_t*)(codes + s * kPage * kCodeBytes + 4 * part);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < S::VPer; ++i) {
+      const int w = min((i * WR + wr) * kWave + lane, S::VPairs - 1), key = w % kPage, g = w / kPage;
+      v[i] = *(const u32x4*)(tile + codes_bytes(S::D) + (g * kPage + key) * kCodeBytes);
+      vs[i] = tile[v_scales_at(S::D) + key * scale_stride(S::D) + g];
+    }
+  }
+};
+
+__device__ __forceinline__ u32x4 unpack8(uint32_t c, float s) {
+  u32x4 y;
+  y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
+  y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
+  y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
+  y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
+  return y;
+}
 
 template <int NG, int MT, int WR>
 __global__ void __launch_bounds__(kCaThreads, 2)
 k_cache_attn(const CacheAttnArgs a) {
   typedef CaShape<NG, MT, WR> S;
-  constexpr int D = S::D;
-  constexpr int SPT = kPage / MT;     // subtiles of MT keys in a page
+  constexpr int D = S::D, SPT = S::SPT, WK = S::WK;
   typedef typename std::conditional<MT == 32, f32x16, f32x4>::type Acc;
-  __shared__ __align__(16) uint8_t s_mem[S::LdsBytes];
+  extern __shared__ __align__(16) uint8_t s_mem[];
   __shared__ int s_sum[kCaWaves];
   __shared__ float s_ml[kCaWaves][MT][2];
 
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int wr = wave % WR, wk = wave / WR;   // its rows, its pages
   const int col = lane % MT, part = lane / MT;
 
   // this workgroup's share of the units
-  const int units = total_units<S::Rows>(a, s_sum);
+  const int units = units_before<S::Rows>(a, a.B, s_sum);
   if (units == 0) return;
   const int u_begin = share_begin(blockIdx.x, gridDim.x, units);
   const int u_end = share_begin(blockIdx.x + 1, gridDim.x, units);
+  if (blockIdx.x == 0 && tid == 0) a.plan[0] = units;
   if (u_begin >= u_end) return;
 
   // the sequence of its first unit: 256 at a time, then by steps
@@ -193,6 +234,7 @@ k_cache_attn(const CacheAttnArgs a) {
 
   int u = u_begin;
   int slot = 0;                       // of the next partial result
+  int buf = 0;                        // of values in LDS; goes on from item to item, so that one barrier a page will do
   while (u < u_end) {
     while (u >= before + seq.groups * seq.pages * a.Hk) {
       before += seq.groups * seq.pages * a.Hk;
@@ -203,6 +245,7 @@ k_cache_attn(const CacheAttnArgs a) {
     const int page1 = min(seq.pages, page0 + (u_end - u));
     const int h = item % a.Hk, group = item / a.Hk;
     u += page1 - page0;
+    if (item == 0 && page0 == 0 && tid == 0) a.plan[1 + b] = before;   // for the join
 
     // ---- the item's rows ----
     const int r = (group * WR + wr) * MT + col;             // row of this lane
@@ -210,225 +253,171 @@ k_cache_attn(const CacheAttnArgs a) {
     const int tok = row_ok ? r / a.R : 0, head = h * a.R + (row_ok ? r % a.R : 0);
     const int start = a.q_start ? a.q_start[b] : seq.len - seq.n;
     const int end = row_ok ? visible_end(start + tok, a.blk, seq.len) : 0;
-    i32x8 qh[S::QS], ql[S::QS];
-    PairScale ps;
+    int all_see = row_ok ? end : INT32_MAX;                 // keys that every row of the wave sees
+#pragma unroll
+    for (int x = 1; x < MT; x <<= 1) all_see = min(all_see, __shfl_xor(all_see, x));
+    all_see = __builtin_amdgcn_readfirstlane(all_see);
+    bf16x8 q[S::Steps];
     {
       const uint16_t* qrow = a.q + (size_t)(seq.first + tok) * a.q_stride + (size_t)head * D;
-      float top = 0.0f;
-      bf16x8 x[S::QS][4];
 #pragma unroll
-      for (int s = 0; s < S::QS; ++s)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          // the 8-bit operand's element order: 16 from each half of the step
-          const int span = MT == 32 ? 64 : 128;
-          const int d = s * span + (k / 2) * (span / 2) + part * 16 + (k % 2) * 8;
-          bf16x8 v = {};
-          if (row_ok && d < D) v = *(const bf16x8*)(qrow + d);
-          x[s][k] = v;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) top = fmaxf(top, __builtin_fabsf((float)v[i]));
-        }
-      top = max_row<MT>(top);
-      ps = pair_scale(top);
-#pragma unroll
-      for (int s = 0; s < S::QS; ++s)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          float y[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) y[i] = (float)x[s][k / 2][(k % 2) * 4 + i] * ps.mul;
-          int hi, lo;
-          split4(y, &hi, &lo);
-          qh[s][k] = hi;
-          ql[s][k] = lo;
-        }
+      for (int s = 0; s < S::Steps; ++s) {
+        q[s] = bf16x8{};
+        if (row_ok) q[s] = *(const bf16x8*)(qrow + element_of<NG, MT>(s, part));
+      }
     }
 
     Acc o[S::DT];
 #pragma unroll
     for (int t = 0; t < S::DT; ++t) o[t] = Acc{};
-    float m = kNegInf, l = 0.0f;
+    float ref = kRefFloor, l = 0.0f;   // weights are 2^(c s - ref), l their sum
 
     // ---- the pages ----
-    int buf = 0;
-    for (int pg = page0 + wk;; pg += S::WK) {
-      // sets of waves without a page left go along while others' barriers run
-      const bool active = pg < page1;
-      if (WR == 1 ? !active : pg - wk >= page1) break;
-      const int32_t page = active && pg * kPage < seq.len ? a.table[(size_t)b * a.table_w + pg] : -1;
-      const bool there = page >= 0 && page < a.n_pages;
-      const uint8_t* tile = a.cache + ((size_t)(there ? page : 0) * a.Hk + h) * tile_bytes(D);
+    const int32_t* table = a.table + (size_t)b * a.table_w;
+    // of a page whose tokens all lie past the sequence's end the table says nothing
+    const auto page_id = [&](int pg) { return pg < page1 && pg * kPage < seq.len ? table[pg] : -1; };
+    PageRegs<NG, MT, WR> next;
+    next.load(a, page_id(page0 + wk), h, lane, wr);
+    int next_id = page_id(page0 + wk + WK);
+    // sets of waves without a page left go along while others' barriers run
+    for (int pg = page0 + wk; WR == 1 ? pg < page1 : pg - wk < page1; pg += WK) {
       const int base = pg * kPage;
-      const int limit = there ? seq.len - base : 0;          // keys of the page that exist
+      const bool there = next.there;
+      uint8_t* lds = s_mem + (wk * S::Buffers + buf) * S::PageBytes;
+      if (S::Buffers > 1) buf ^= 1;
+
+      // values: a lane unpacks 32 elements of a key.  Keys past the end get a
+      // scale of next to nothing: their weight is 0, and a code is finite.
+#pragma unroll
+      for (int i = 0; i < S::VPer; ++i) {
+        const int w = (i * WR + wr) * kWave + lane, key = w % kPage, g = w / kPage;
+        if (S::VPairs % (WR * kWave) != 0 && w >= S::VPairs) break;
+        const float sv = scale_of(there && base + key < seq.len ? next.vs[i] : 1u);
+        u32x4* dst = (u32x4*)(lds + key * S::RowBytes + g * 64);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dst[j] = unpack8(next.v[i][j], sv);
+      }
 
       // scores
       Acc sc[SPT];
 #pragma unroll
-      for (int s = 0; s < SPT; ++s) {
-        const int key = s * MT + col;
-        uint32_t ks = *(const uint32_t*)(tile + k_scales_at(D) + key * scale_stride(D));
-        if (NG == 3) ks = (ks & 0x00ffffffu) | 0x7f000000u;
-        if (NG == 2) ks = (ks & 0x0000ffffu) | 0x7f7f0000u;
-        const int kb = (int)(ks >> (8 * part));
-        sc[s] = Acc{};
+      for (int x = 0; x < SPT; ++x) {
+        sc[x] = Acc{};
 #pragma unroll
-        for (int t = 0; t < S::QS; ++t) {
-          const int g = MT == 32 ? 2 * t + part : part;
-          i32x8 k = {};
-          if (g < NG) {
-            const u32x4 c = *(const u32x4*)(tile + (g * kPage + key) * kCodeBytes);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) k[i] = (int)c[i];
-          }
-          if constexpr (MT == 32) {
-            // byte 0 of the shifted scales is group `part`, byte 2 group 2 + part
-            if (t == 0) {
-              sc[s] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, qh[t], sc[s], 4, 0, 0, kb, 0, ps.hi);
-              sc[s] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, ql[t], sc[s], 4, 0, 0, kb, 0, ps.lo);
-            } else {
-              sc[s] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, qh[t], sc[s], 4, 0, 2, kb, 0, ps.hi);
-              sc[s] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, ql[t], sc[s], 4, 0, 2, kb, 0, ps.lo);
-            }
-          } else {
-            sc[s] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, qh[t], sc[s], 4, 0, 0, kb, 0, ps.hi);
-            sc[s] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, ql[t], sc[s], 4, 0, 0, kb, 0, ps.lo);
-          }
+        for (int s = 0; s < S::Steps; ++s) {
+          const int g = MT == 32 ? (NG % 2 == 0 || s < 4 * (NG / 2) ? 2 * (s / 4) + part : NG - 1)
+                                 : NG == 4 ? part : NG == 2 ? part / 2 : s;
+          const float ksv = scale_of((next.ks[x] >> (8 * g)) & 255u);
+          const bf16x8 kf = __builtin_bit_cast(bf16x8, unpack8(next.k[x][s], ksv));
+          if constexpr (MT == 32) sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[s], sc[x], 0, 0, 0);
+          else sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[s], sc[x], 0, 0, 0);
         }
       }
+      next.load(a, next_id, h, lane, wr);
+      next_id = page_id(pg + 2 * WK);
+
       // keys that a row does not see
-      const int seen = there ? end - base : 0;
+      if (!there || base + kPage > all_see) {
+        const int seen = there ? end - base : 0;
 #pragma unroll
-      for (int s = 0; s < SPT; ++s)
+        for (int x = 0; x < SPT; ++x)
 #pragma unroll
-        for (int i = 0; i < S::OR; ++i) {
-          const int key = s * MT + (MT == 32 ? i % 4 + 8 * (i / 4) + 4 * part : 4 * part + i);
-          sc[s][i] = key < seen ? sc[s][i] : kNegInf;
-        }
-      // running maximum and sum
+          for (int i = 0; i < S::OR; ++i) {
+            const int key = x * MT + (MT == 32 ? i % 4 + 8 * (i / 4) + 4 * part : 4 * part + i);
+            sc[x][i] = key < seen ? sc[x][i] : kNegInf;
+          }
+      }
+      // The running reference follows the maximum only where that has grown by
+      // more than 2^8: weights up to 256 lose nothing in floating point, and
+      // the sums are rescaled a few times instead of with every page.
       float top = kNegInf;
 #pragma unroll
-      for (int s = 0; s < SPT; ++s)
+      for (int x = 0; x < SPT; ++x)
 #pragma unroll
-        for (int i = 0; i < S::OR; ++i) top = fmaxf(top, sc[s][i]);
-      top = max_row<MT>(top);
-      const float mn = fmaxf(m, top);
-      const float ref = fmaxf(mn * a.c, kRefFloor);          // finite while nothing was seen
-      const float alpha = __builtin_amdgcn_exp2f(m * a.c - ref);
-      m = mn;
+        for (int i = 0; i < S::OR; ++i) top = fmaxf(top, sc[x][i]);
+      top = max_row<MT>(top) * a.c;
+      if (__any(top > ref + 8.0f)) {
+        const float to = fmaxf(ref, top);
+        const float f = __builtin_amdgcn_exp2f(ref - to);
+        ref = to;
+        l *= f;
+#pragma unroll
+        for (int t = 0; t < S::DT; ++t)
+#pragma unroll
+          for (int i = 0; i < S::OR; ++i) o[t][i] *= f;
+      }
       float sum = 0.0f;
       uint32_t p[SPT][S::OR / 2];
 #pragma unroll
-      for (int s = 0; s < SPT; ++s)
+      for (int x = 0; x < SPT; ++x)
 #pragma unroll
         for (int i = 0; i < S::OR; i += 2) {
-          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[s][i], a.c, -ref));
-          const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[s][i + 1], a.c, -ref));
-          sum += x + y;
-          p[s][i / 2] = pack_bf16(x, y);   // weights in (0, 1] to 8 bits, as the values they meet
+          const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][i], a.c, -ref));
+          const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][i + 1], a.c, -ref));
+          sum += y + z;
+          p[x][i / 2] = pack_bf16(y, z);   // to 8 bits, as the values they meet
         }
-      l = l * alpha + sum;
-#pragma unroll
-      for (int t = 0; t < S::DT; ++t)
-#pragma unroll
-        for (int i = 0; i < S::OR; ++i) o[t][i] *= alpha;
+      l += sum;
 
-      // values, half a page at a time
+      if (WR > 1) __syncthreads();
+      else __builtin_amdgcn_wave_barrier();
+      // a group of 16 lanes reads four keys by 16 elements, transposed
+      const uint8_t* vp = lds + (4 * part + (lane % 16) / 4) * S::RowBytes +
+                          (MT == 32 ? 16 * ((lane / 16) % 2) + 4 * (lane % 4) : 4 * (lane % 4)) * 2;
+      constexpr int KS = MT == 32 ? 4 : 2;   // steps of the second product
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        uint8_t* lds = s_mem + (wk * S::Buffers + buf) * S::HalfBytes;
-        if (S::Buffers > 1) buf ^= 1;
-        // unpack: 32 keys x NG groups, a lane each
-        for (int w = wr * kWave + lane; w < kHalf * NG; w += WR * kWave) {
-          const int key = w % kHalf, g = w / kHalf;
-          const int kp = half * kHalf + key;
-          u32x4 c = *(const u32x4*)(tile + codes_bytes(D) + (g * kPage + kp) * kCodeBytes);
-          const uint32_t byte = tile[v_scales_at(D) + kp * scale_stride(D) + g];
-          const bool ok = kp < limit;
-          const float sv = scale_of(ok ? byte : kUnitScale);
-          u32x4* dst = (u32x4*)(lds + key * S::RowBytes + g * 64);
+      for (int k = 0; k < KS; ++k) {
+        u32x4 pk;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t ci = ok ? c[i] : 0u;
-            u32x4 y;
-            y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(ci, sv, 0));
-            y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(ci, sv, 1));
-            y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(ci, sv, 2));
-            y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(ci, sv, 3));
-            dst[i] = y;
-          }
+        for (int i = 0; i < 4; ++i)
+          pk[i] = MT == 32 ? p[k / 2][(4 * (k % 2) + i) % (S::OR / 2)] : p[(2 * k + i / 2) % SPT][i % 2];
+        const bf16x8 pf = __builtin_bit_cast(bf16x8, pk);
+#pragma unroll
+        for (int t = 0; t < S::DT; ++t) {
+          const uint8_t* at = vp + k * (MT == 32 ? 16 : 32) * S::RowBytes + t * MT * 2;
+          const i16x4 v0 = read_transposed(at);
+          const i16x4 v1 = read_transposed(at + (MT == 32 ? 8 : 16) * S::RowBytes);
+          const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+          if constexpr (MT == 32) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[t], 0, 0, 0);
+          else o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[t], 0, 0, 0);
         }
-        if (WR > 1) __syncthreads();
-        else __builtin_amdgcn_wave_barrier();
-        // a group of 16 lanes reads four keys by 16 elements, transposed
-        const int quad = (lane % 16) / 4, four = lane % 4;
-        if constexpr (MT == 32) {
-          const uint8_t* base_p = lds + (4 * part + quad) * S::RowBytes + (16 * ((lane / 16) % 2) + 4 * four) * 2;
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            u32x4 pk;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pk[i] = p[half][4 * k + i];
-            const bf16x8 pf = __builtin_bit_cast(bf16x8, pk);
-#pragma unroll
-            for (int t = 0; t < S::DT; ++t) {
-              const i16x4 v0 = read_transposed(base_p + (16 * k) * S::RowBytes + t * 64);
-              const i16x4 v1 = read_transposed(base_p + (16 * k + 8) * S::RowBytes + t * 64);
-              const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-              o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[t], 0, 0, 0);
-            }
-          }
-        } else {
-          const uint8_t* base_p = lds + (4 * part + quad) * S::RowBytes + (4 * four) * 2;
-          u32x4 pk;
-          pk[0] = p[2 * half][0], pk[1] = p[2 * half][1], pk[2] = p[2 * half + 1][0], pk[3] = p[2 * half + 1][1];
-          const bf16x8 pf = __builtin_bit_cast(bf16x8, pk);
-#pragma unroll
-          for (int t = 0; t < S::DT; ++t) {
-            const i16x4 v0 = read_transposed(base_p + t * 32);
-            const i16x4 v1 = read_transposed(base_p + 16 * S::RowBytes + t * 32);
-            const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-            o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[t], 0, 0, 0);
-          }
-        }
-        __builtin_amdgcn_wave_barrier();
       }
+      __builtin_amdgcn_wave_barrier();
     }
     l = sum_row<MT>(l);
 
+    // element of register i of tile t
+    const auto d_of = [&](int t, int i) { return MT == 32 ? t * 32 + 2 * i + 4 * part : t * 16 + 4 * part; };
+
     // ---- the sets of waves join, two by two ----
-    if constexpr (S::WK > 1) {
+    if constexpr (WK > 1) {
 #pragma unroll
-      for (int n = S::WK / 2; n >= 1; n /= 2) {
+      for (int n = WK / 2; n >= 1; n /= 2) {
         __syncthreads();
         float* mem = (float*)s_mem;
         if (wk >= n && wk < 2 * n) {
           float* mine = mem + ((wk - n) * WR + wr) * MT * (D + 4);
-          if (part == 0) s_ml[wave][col][0] = m, s_ml[wave][col][1] = l;
+          if (part == 0) s_ml[wave][col][0] = ref, s_ml[wave][col][1] = l;
 #pragma unroll
           for (int t = 0; t < S::DT; ++t)
 #pragma unroll
-            for (int i = 0; i < S::OR; i += 4) {
-              const int d = MT == 32 ? t * 32 + 2 * i + 4 * part : t * 16 + 4 * part;
-              *(f32x4*)(mine + col * (D + 4) + d) = f32x4{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
-            }
+            for (int i = 0; i < S::OR; i += 4)
+              *(f32x4*)(mine + col * (D + 4) + d_of(t, i)) = f32x4{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
         }
         __syncthreads();
         if (wk < n) {
           const int other = (wk + n) * WR + wr;
           const float* theirs = mem + (wk * WR + wr) * MT * (D + 4);
-          const float m2 = s_ml[other][col][0], l2 = s_ml[other][col][1];
-          const float mn = fmaxf(m, m2);
-          const float ref = fmaxf(mn * a.c, kRefFloor);
-          const float f1 = __builtin_amdgcn_exp2f(m * a.c - ref), f2 = __builtin_amdgcn_exp2f(m2 * a.c - ref);
-          m = mn;
+          const float ref2 = s_ml[other][col][0], l2 = s_ml[other][col][1];
+          const float to = fmaxf(ref, ref2);
+          const float f1 = __builtin_amdgcn_exp2f(ref - to), f2 = __builtin_amdgcn_exp2f(ref2 - to);
+          ref = to;
           l = l * f1 + l2 * f2;
 #pragma unroll
           for (int t = 0; t < S::DT; ++t)
 #pragma unroll
             for (int i = 0; i < S::OR; i += 4) {
-              const int d = MT == 32 ? t * 32 + 2 * i + 4 * part : t * 16 + 4 * part;
-              const f32x4 x = *(const f32x4*)(theirs + col * (D + 4) + d);
+              const f32x4 x = *(const f32x4*)(theirs + col * (D + 4) + d_of(t, i));
 #pragma unroll
               for (int k = 0; k < 4; ++k) o[t][i + k] = o[t][i + k] * f1 + x[k] * f2;
             }
@@ -446,81 +435,115 @@ k_cache_attn(const CacheAttnArgs a) {
 #pragma unroll
           for (int t = 0; t < S::DT; ++t)
 #pragma unroll
-            for (int i = 0; i < S::OR; i += 4) {
-              const int d = MT == 32 ? t * 32 + 2 * i + 4 * part : t * 16 + 4 * part;
-              *(u32x2*)(a.out + at * D + d) = u32x2{pack_bf16(o[t][i] * inv, o[t][i + 1] * inv),
-                                                    pack_bf16(o[t][i + 2] * inv, o[t][i + 3] * inv)};
-            }
-          if (a.lse && part == 0)
-            a.lse[at] = l > 0.0f ? (m * a.c + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+            for (int i = 0; i < S::OR; i += 4)
+              *(u32x2*)(a.out + at * D + d_of(t, i)) = u32x2{pack_bf16(o[t][i] * inv, o[t][i + 1] * inv),
+                                                             pack_bf16(o[t][i + 2] * inv, o[t][i + 3] * inv)};
+          if (a.lse && part == 0) a.lse[at] = l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
         }
       } else {
-        float* mine = a.part + (((size_t)blockIdx.x * 2 + slot) * S::Rows + wr * MT + col) * (D + kCaRowFloats);
+        const size_t row = ((size_t)blockIdx.x * 2 + slot) * S::Rows + wr * MT + col;
 #pragma unroll
         for (int t = 0; t < S::DT; ++t)
 #pragma unroll
-          for (int i = 0; i < S::OR; i += 2) {
-            const int d = MT == 32 ? t * 32 + i % 4 + 8 * (i / 4) + 4 * part : t * 16 + 4 * part + i;
-            *(float2*)(mine + d) = float2{o[t][i], o[t][i + 1]};
-          }
-        if (part == 0) *(float2*)(mine + D) = float2{m, l};
+          for (int i = 0; i < S::OR; i += 4)
+            *(f32x4*)(a.part + row * D + d_of(t, i)) = f32x4{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+        if (part == 0) *(float2*)(a.part_ml + row * 2) = float2{ref, l};
       }
     }
     slot = 1;
   }
 }
 
-// Joins the partial results of an item that several workgroups share, in the
-// order of its pages.  One workgroup per (item of the widest sequence).
+// Joins the partial results of an item that several workgroups share, always
+// in the same order.  A workgroup takes four rows, 16 lanes a row, and divides
+// the parts of a row among its waves: what a part costs is a round trip to
+// memory, so as many as possible are under way at once.
+constexpr int kCaJoinRows = 4;
+
 template <int NG, int Rows>
 __global__ void __launch_bounds__(kCaThreads)
 k_cache_join(const CacheAttnArgs a, int wgs) {
-  constexpr int D = NG * kGroup;
-  __shared__ int s_sum[kCaWaves];
+  constexpr int D = NG * kGroup, Lanes = 16;
+  constexpr int Blocks = Rows / kCaJoinRows;   // of a group of rows
+  __shared__ float s_acc[kCaWaves][kCaJoinRows][D];
+  __shared__ float s_ml[kCaWaves][kCaJoinRows][2];
   const int b = blockIdx.y;
+  const int item = blockIdx.x / Blocks;
   const Seq seq = sequence<Rows>(a, b);
-  if ((int)blockIdx.x >= seq.groups * a.Hk) return;
-  const int units = total_units<Rows>(a, s_sum);
-  const int u0 = units_before<Rows>(a, b, s_sum) + (int)blockIdx.x * seq.pages;
+  if (item >= seq.groups * a.Hk) return;
+  const int h = item % a.Hk, group = item / a.Hk;
+  const int x0 = (blockIdx.x % Blocks) * kCaJoinRows;
+  if (group * Rows + x0 >= seq.n * a.R) return;
+  const int units = a.plan[0];
+  const int u0 = a.plan[1 + b] + item * seq.pages;
   const int g0 = share_of(u0, wgs, units), g1 = share_of(u0 + seq.pages - 1, wgs, units);
   if (g0 == g1) return;
-  const int h = blockIdx.x % a.Hk, group = blockIdx.x / a.Hk;
-  // rows by quarter waves: 16 lanes of NG * 2 elements
-  const int lane = threadIdx.x % 16;
-  for (int x = threadIdx.x / 16; x < Rows; x += kCaThreads / 16) {
-    const int r = group * Rows + x;
-    if (r >= seq.n * a.R) break;
-    float acc[2 * NG];
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % Lanes, xr = threadIdx.x % kWave / Lanes;
+  const int x = x0 + xr;
+  // Part i of the row.  An item that begins inside a share is that workgroup's
+  // second result; a share may be empty (it weighs nothing then, and the first
+  // part's address stands in for its own).
+  const auto part_of = [&](int g, bool* there) {
+    const int begin = share_begin(g, wgs, units);
+    *there = g <= g1 && begin < share_begin(g + 1, wgs, units);
+    const int gg = *there ? g : g0;
+    return ((size_t)gg * 2 + (share_begin(gg, wgs, units) < u0 ? 1 : 0)) * Rows + x;
+  };
+  float acc[2 * NG], l = 0.0f, ref = kRefFloor;
 #pragma unroll
-    for (int i = 0; i < 2 * NG; ++i) acc[i] = 0.0f;
-    float m = kNegInf, l = 0.0f;
-    for (int g = g0; g <= g1; ++g) {
-      const int begin = share_begin(g, wgs, units);
-      if (begin == share_begin(g + 1, wgs, units)) continue;
-      // an item that begins inside a share is that workgroup's second result
-      const int slot = begin < u0 ? 1 : 0;
-      const float* p = a.part + (((size_t)g * 2 + slot) * Rows + x) * (D + kCaRowFloats);
-      const float m2 = p[D], l2 = p[D + 1];
-      const float mn = fmaxf(m, m2);
-      const float ref = fmaxf(mn * a.c, kRefFloor);
-      const float f1 = __builtin_amdgcn_exp2f(m * a.c - ref), f2 = __builtin_amdgcn_exp2f(m2 * a.c - ref);
-      m = mn;
-      l = l * f1 + l2 * f2;
+  for (int i = 0; i < 2 * NG; ++i) acc[i] = 0.0f;
+  // 16 parts at a time of every 64: a lane each for their references and sums
+  for (int c = g0 + wave * Lanes; c <= g1; c += kCaWaves * Lanes) {
+    bool there;
+    const size_t row = part_of(c + lane, &there);
+    const float2 ml = *(const float2*)(a.part_ml + row * 2);
+    float to = there ? fmaxf(ref, ml.x) : ref;
+#pragma unroll
+    for (int s = 1; s < Lanes; s <<= 1) to = fmaxf(to, __shfl_xor(to, s));
+    const float f0 = __builtin_amdgcn_exp2f(ref - to);
+    ref = to;
+    const float f = there ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.0f;
+    l = l * f0 + f * ml.y;     // of this lane's parts
+#pragma unroll
+    for (int i = 0; i < 2 * NG; ++i) acc[i] *= f0;
+    const int n = min(Lanes, g1 + 1 - c);
+#pragma unroll 8
+    for (int k = 0; k < n; ++k) {
+      const float fk = __shfl(f, k, Lanes);
+      const float* src = a.part + (size_t)__shfl((int)row, k, Lanes) * D + 2 * lane;
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
-        const float2 v = *(const float2*)(p + 32 * i + 2 * lane);
-        acc[2 * i] = acc[2 * i] * f1 + v.x * f2;
-        acc[2 * i + 1] = acc[2 * i + 1] * f1 + v.y * f2;
+        const float2 v = *(const float2*)(src + 32 * i);
+        acc[2 * i] += fk * v.x;
+        acc[2 * i + 1] += fk * v.y;
       }
     }
-    const int tok = r / a.R, head = h * a.R + r % a.R;
-    const size_t at = (size_t)(seq.first + tok) * a.H + head;
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-#pragma unroll
-    for (int i = 0; i < NG; ++i)
-      *(uint32_t*)(a.out + at * D + 32 * i + 2 * lane) = pack_bf16(acc[2 * i] * inv, acc[2 * i + 1] * inv);
-    if (a.lse && lane == 0) a.lse[at] = l > 0.0f ? (m * a.c + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
   }
+#pragma unroll
+  for (int s = 1; s < Lanes; s <<= 1) l += __shfl_xor(l, s);
+#pragma unroll
+  for (int i = 0; i < NG; ++i) *(float2*)&s_acc[wave][xr][32 * i + 2 * lane] = float2{acc[2 * i], acc[2 * i + 1]};
+  if (lane == 0) s_ml[wave][xr][0] = ref, s_ml[wave][xr][1] = l;
+  __syncthreads();
+  // a wave a row, two elements a lane
+  const int r = group * Rows + x0 + wave;
+  if (r >= seq.n * a.R) return;
+  float m = kRefFloor;
+#pragma unroll
+  for (int w = 0; w < kCaWaves; ++w) m = fmaxf(m, s_ml[w][wave][0]);
+  float sum = 0.0f, y = 0.0f, z = 0.0f;
+  const int e = 2 * (threadIdx.x % kWave);
+#pragma unroll
+  for (int w = 0; w < kCaWaves; ++w) {
+    const float f = __builtin_amdgcn_exp2f(s_ml[w][wave][0] - m);
+    sum += f * s_ml[w][wave][1];
+    if (e < D) y += f * s_acc[w][wave][e], z += f * s_acc[w][wave][e + 1];
+  }
+  const int tok = r / a.R, head = h * a.R + r % a.R;
+  const size_t at = (size_t)(seq.first + tok) * a.H + head;
+  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  if (e < D) *(uint32_t*)(a.out + at * D + e) = pack_bf16(y * inv, z * inv);
+  if (a.lse && e == 0) a.lse[at] = sum > 0.0f ? (m + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
 }
 
 // ---------------------------------------------------------------------------
@@ -530,7 +553,7 @@ struct CaPlan {
   int mt, wr;        // variant
   int wgs;           // workgroups
   int items;         // items of a sequence with max_q query tokens
-  size_t bytes;      // of partial results
+  size_t at_ml, at_part, bytes;
 };
 
 static bool ca_sizes_ok(int B, int H, int Hk, int D, int max_q, int table_w, int n_pages) {
@@ -558,26 +581,43 @@ static CaPlan ca_plan(int B, int H, int Hk, int D, int max_q, int table_w) {
   const long long most = (long long)B * p.items * ((table_w + wk - 1) / wk);
   p.wgs = (int)(most < 512 ? most : 512);
   if (p.wgs < 1) p.wgs = 1;
-  p.bytes = (size_t)p.wgs * 2 * per * (D + kCaRowFloats) * sizeof(float);
+  const size_t rows_out = (size_t)p.wgs * 2 * per;
+  p.at_ml = align256(((size_t)B + 1) * 4);
+  p.at_part = p.at_ml + align256(rows_out * 8);
+  p.bytes = p.at_part + rows_out * D * sizeof(float);
   return p;
 }
 
-template <int NG>
-static void ca_launch(const CacheAttnArgs& a, const CaPlan& p, hipStream_t st) {
-  const dim3 grid((unsigned)p.wgs), block(kCaThreads), join((unsigned)p.items, (unsigned)a.B);
-  if (p.mt == 16) {
-    hipLaunchKernelGGL((k_cache_attn<NG, 16, 1>), grid, block, 0, st, a);
-    hipLaunchKernelGGL((k_cache_join<NG, 16>), join, block, 0, st, a, p.wgs);
-  } else if (p.wr == 1) {
-    hipLaunchKernelGGL((k_cache_attn<NG, 32, 1>), grid, block, 0, st, a);
-    hipLaunchKernelGGL((k_cache_join<NG, 32>), join, block, 0, st, a, p.wgs);
-  } else if (p.wr == 2) {
-    hipLaunchKernelGGL((k_cache_attn<NG, 32, 2>), grid, block, 0, st, a);
-    hipLaunchKernelGGL((k_cache_join<NG, 64>), join, block, 0, st, a, p.wgs);
-  } else {
-    hipLaunchKernelGGL((k_cache_attn<NG, 32, 4>), grid, block, 0, st, a);
-    hipLaunchKernelGGL((k_cache_join<NG, 128>), join, block, 0, st, a, p.wgs);
+// The attention kernels' LDS is above the default limit; the limit is raised
+// once per device and kernel, before the first launch there.
+constexpr int kCaMaxDevices = 64;
+
+template <int NG, int MT, int WR>
+static hipError_t ca_launch_one(const CacheAttnArgs& a, const CaPlan& p, hipStream_t st) {
+  typedef CaShape<NG, MT, WR> S;
+  static std::atomic<bool> allowed[kCaMaxDevices];
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= kCaMaxDevices || !allowed[dev].load(std::memory_order_acquire)) {
+    e = hipFuncSetAttribute((const void*)k_cache_attn<NG, MT, WR>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                            S::LdsBytes);
+    if (e != hipSuccess) return e;
+    if (dev >= 0 && dev < kCaMaxDevices) allowed[dev].store(true, std::memory_order_release);
   }
+  hipLaunchKernelGGL((k_cache_attn<NG, MT, WR>), dim3((unsigned)p.wgs), dim3(kCaThreads), S::LdsBytes, st, a);
+  if (p.wgs > 1)
+    hipLaunchKernelGGL((k_cache_join<NG, S::Rows>), dim3((unsigned)(p.items * (S::Rows / kCaJoinRows)), (unsigned)a.B),
+                       dim3(kCaThreads), 0, st, a, p.wgs);
+  return hipGetLastError();
+}
+
+template <int NG>
+static hipError_t ca_launch(const CacheAttnArgs& a, const CaPlan& p, hipStream_t st) {
+  if (p.mt == 16) return ca_launch_one<NG, 16, 1>(a, p, st);
+  if (p.wr == 1) return ca_launch_one<NG, 32, 1>(a, p, st);
+  if (p.wr == 2) return ca_launch_one<NG, 32, 2>(a, p, st);
+  return ca_launch_one<NG, 32, 4>(a, p, st);
 }
 
 }  // namespace fdllm
@@ -610,14 +650,13 @@ fdllm_status fdllm_cache_attention(const void* q, int64_t q_stride, int T, const
     if ((uintptr_t)p & 15) return FDLLM_ERR_INVALID_ARG;
   const CaPlan p = ca_plan(B, H, Hk, D, max_q, table_width);
   if (!workspace || workspace_bytes < p.bytes) return FDLLM_ERR_WORKSPACE;
+  char* ws = (char*)workspace;
   const CacheAttnArgs a{(const uint16_t*)q, q_stride, T, cache, n_pages, page_table, table_width, kv_len, cu_q,
-                        q_start, B, H, Hk, H / Hk, max_q, blk, scale * kLog2e, (uint16_t*)out, lse,
-                        (float*)workspace};
+                        q_start, B, H, Hk, H / Hk, max_q, blk, scale * kLog2e, (uint16_t*)out, lse, (int32_t*)ws,
+                        (float*)(ws + p.at_ml), (float*)(ws + p.at_part)};
   hipStream_t st = (hipStream_t)stream;
-  if (D == 64) ca_launch<2>(a, p, st);
-  else if (D == 96) ca_launch<3>(a, p, st);
-  else ca_launch<4>(a, p, st);
-  return hipGetLastError() == hipSuccess ? FDLLM_OK : FDLLM_ERR_HIP;
+  const hipError_t e = D == 64 ? ca_launch<2>(a, p, st) : D == 96 ? ca_launch<3>(a, p, st) : ca_launch<4>(a, p, st);
+  return e == hipSuccess ? FDLLM_OK : FDLLM_ERR_HIP;
 }
 
 }  // extern "C"
