@@ -11,6 +11,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "attn_common.h"
 #include "fdllm.h"
@@ -62,23 +63,57 @@ __device__ __forceinline__ PaTile pa_tile(const PromptArgs& a, int b, int tile) 
   return t;
 }
 
-// LDS rows of keys and values, with room behind each so that 16 lanes of a
-// 16-byte read (keys), or of a transposed read (values), meet no bank twice.
+// A tile's rows in LDS lie RowBytes apart, two buffers each of keys and values.
+// Within a row the 16-byte pieces are exchanged by the row's number, so that 16
+// lanes meet all banks when they read a piece of 16 rows (keys) or 32 bytes of
+// four rows transposed (values); the loads that write LDS fetch the piece that
+// belongs where they write.
 template <int NG>
 struct PaShape {
   static constexpr int D = NG * 32;
-  static constexpr int KRow = 2 * D + 16, VRow = 2 * D + 32;
-  static constexpr int Buffer = kPaKeys * (KRow + VRow);
-  static constexpr int LdsBytes = 2 * Buffer;
-  static constexpr int Loads = kPaKeys * D * 2 / 16 / kPaThreads;   // 16-byte loads a thread, per operand
+  static constexpr int RowBytes = NG == 2 ? 128 : 256;
+  static constexpr int Pieces = RowBytes / 16;
+  static constexpr int Tile = kPaKeys * RowBytes;
+  static constexpr int LdsBytes = 4 * Tile;
+  static constexpr int RowsPerLoad = kWave / Pieces;                    // of a wave's load of 1 KiB
+  static constexpr int Loads = kPaKeys / kPaWaves / RowsPerLoad;        // a wave, per operand and tile
+  __device__ static int swap_k(int row) { return NG == 2 ? row / 2 % 8 : row % 16; }
+  __device__ static int swap_v(int row) { return NG == 2 ? row / 2 % 4 * 2 : row % 8 * 2; }
 };
+
+typedef __attribute__((address_space(3))) void* pa_lds_t;
+
+// Rows [first, first + rows) of one head of a packed operand as a resource:
+// what is beyond reads as zero.
+__device__ __forceinline__ i32x4 pa_rows(const uint16_t* p, int rows, long long stride, int D) {
+  const uint64_t at = (uint64_t)p;
+  i32x4 r;
+  r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)at);
+  r[1] = __builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xffffu));
+  r[2] = __builtin_amdgcn_readfirstlane(rows > 0 ? (int)((uint32_t)(rows - 1) * (uint32_t)(2 * stride) + 2u * D) : 0);
+  r[3] = 0x00020000;
+  return r;
+}
+
+// 16 bytes a lane from rsrc + voff to LDS byte lds + 16 lane.  As inline
+// assembly, since the compiler would wait for it before every later LDS read;
+// pa_arrive is what waits.
+__device__ __forceinline__ void pa_dma(i32x4 rsrc, uint32_t lds, uint32_t voff) {
+  uint32_t keep;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
+               "s_mov_b32 m0, %0"
+               : "=&s"(keep) : "s"(lds), "v"(voff), "s"(rsrc) : "memory");
+}
+
+// All of this wave's loads to LDS have landed, then everybody's.
+__device__ __forceinline__ void pa_arrive() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 template <int NG>
 __global__ void __launch_bounds__(kPaThreads, 2)
 k_prompt_attn(const PromptArgs a) {
   typedef PaShape<NG> S;
   constexpr int D = S::D;
-  extern __shared__ __align__(16) uint8_t s_mem[];
+  extern __shared__ __align__(1024) uint8_t s_mem[];
 
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int col = lane % 32, part = lane / 32;
@@ -110,72 +145,72 @@ k_prompt_attn(const PromptArgs a) {
   for (int t = 0; t < NG; ++t) o[t] = f32x16{};
   float ref = kRefFloor, l = 0.0f;   // weights are 2^(c s - ref), l their sum
 
-  // staging: registers first, LDS when the other buffer is free
+  // ---- loads to LDS ----
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(pa_lds_t)s_mem;
   const uint16_t* kbase = a.k + (size_t)pt.firstk * a.k_stride + (size_t)h * D;
   const uint16_t* vbase = a.v + (size_t)pt.firstk * a.v_stride + (size_t)h * D;
-  u32x4 kr[S::Loads], vr[S::Loads];
-  const auto fetch = [&](int t) {
-    const int base = t * kPaKeys;
+  uint32_t k_at[S::Loads], v_at[S::Loads];
 #pragma unroll
-    for (int i = 0; i < S::Loads; ++i) {
-      const int x = i * kPaThreads + tid, key = x / (D / 8), d = x % (D / 8);
-      kr[i] = u32x4{};
-      vr[i] = u32x4{};
-      if (base + key < pt.len) {   // past the end of the sequence: zeros
-        kr[i] = *(const u32x4*)(kbase + (size_t)(base + key) * a.k_stride + 8 * d);
-        vr[i] = *(const u32x4*)(vbase + (size_t)(base + key) * a.v_stride + 8 * d);
-      }
-    }
-  };
-  const auto stage = [&](int buf) {
-    uint8_t* sk = s_mem + buf * S::Buffer;
-    uint8_t* sv = sk + kPaKeys * S::KRow;
-#pragma unroll
-    for (int i = 0; i < S::Loads; ++i) {
-      const int x = i * kPaThreads + tid, key = x / (D / 8), d = x % (D / 8);
-      *(u32x4*)(sk + key * S::KRow + 16 * d) = kr[i];
-      *(u32x4*)(sv + key * S::VRow + 16 * d) = vr[i];
-    }
-  };
-  if (t0 < t1) {
-    fetch(t0);
-    stage(0);
+  for (int i = 0; i < S::Loads; ++i) {
+    const int row = (wave * S::Loads + i) * S::RowsPerLoad + lane / S::Pieces, piece = lane % S::Pieces;
+    const int pk = piece ^ S::swap_k(row), pv = piece ^ S::swap_v(row);
+    // pieces that a row has no elements for are out of the resource's range
+    k_at[i] = 8 * pk < D ? (uint32_t)(row * 2 * a.k_stride) + 16u * pk : 0x7ffffff0u;
+    v_at[i] = 8 * pv < D ? (uint32_t)(row * 2 * a.v_stride) + 16u * pv : 0x7ffffff0u;
   }
-  __syncthreads();
+  const auto load = [&](const uint16_t* base, long long stride, const uint32_t* at, int t, int lds) {
+    const i32x4 rsrc = pa_rows(base + (size_t)t * kPaKeys * stride, min(pt.len - t * kPaKeys, kPaKeys), stride, D);
+#pragma unroll
+    for (int i = 0; i < S::Loads; ++i)
+      pa_dma(rsrc, lds0 + (uint32_t)(lds + (wave * S::Loads + i) * 1024), at[i]);
+  };
+  const auto load_k = [&](int t, int buf) { load(kbase, a.k_stride, k_at, t, buf * S::Tile); };
+  const auto load_v = [&](int t, int buf) { load(vbase, a.v_stride, v_at, t, (2 + buf) * S::Tile); };
 
-  for (int t = t0; t < t1; ++t) {
+  // ---- reads from LDS ----
+  const uint8_t* k_from[2 * NG];
+  const uint8_t* v_from[NG];
+#pragma unroll
+  for (int k = 0; k < 2 * NG; ++k)
+    k_from[k] = s_mem + col * S::RowBytes + 16 * ((2 * k + part) ^ S::swap_k(col));
+  {
+    const int row = 4 * part + (lane % 16) / 4, piece = 2 * ((lane / 16) % 2) + (lane % 4) / 2;
+#pragma unroll
+    for (int x = 0; x < NG; ++x)
+      v_from[x] = s_mem + 2 * S::Tile + row * S::RowBytes + 16 * ((4 * x + piece) ^ S::swap_v(row)) + 8 * (lane % 2);
+  }
+
+  // S^T of a tile
+  f32x16 s[2], sn[2];
+  const auto scores = [&](f32x16* to, int x, int k, int buf) {
+    const bf16x8 kf = *(const bf16x8*)(k_from[k] + buf * S::Tile + x * 32 * S::RowBytes);
+    to[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[k], to[x], 0, 0, 0);
+  };
+  // keys that a row does not see
+  const auto hide = [&](f32x16* to, int t) {
     const int base = t * kPaKeys;
-    const uint8_t* sk = s_mem + ((t - t0) & 1) * S::Buffer;
-    const uint8_t* sv = sk + kPaKeys * S::KRow;
-    if (t + 1 < t1) fetch(t + 1);
-    f32x16 s[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      s[x] = f32x16{};
-#pragma unroll
-      for (int k = 0; k < 2 * NG; ++k) {
-        const bf16x8 kf = *(const bf16x8*)(sk + (32 * x + col) * S::KRow + 32 * k + 16 * part);
-        s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[k], s[x], 0, 0, 0);
-      }
-    }
-    if (base + kPaKeys > all_see) {   // keys that a row does not see
+    if (base + kPaKeys > all_see) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int key = base + 32 * x + i % 4 + 8 * (i / 4) + 4 * part;
-          s[x][i] = key < end ? s[x][i] : kNegInf;
+          to[x][i] = key < end ? to[x][i] : kNegInf;
         }
     }
-    // the running reference follows the maximum where that has grown by more
-    // than 2^8: weights up to 256 lose nothing in floating point, and the sums
-    // are rescaled a few times instead of with every tile
+  };
+  const auto largest = [&](const f32x16* of) {
     float top = kNegInf;
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[x][i]);
-    top = max_halves(top) * a.c;
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, of[x][i]);
+    return max_halves(top) * a.c;
+  };
+  // The running reference follows the maximum where that has grown by more than
+  // 2^8: weights up to 256 lose nothing in floating point, and the sums are
+  // rescaled a few times instead of with every tile.
+  const auto follow = [&](float top) {
     if (__any(top > ref + 8.0f)) {
       const float to = fmaxf(ref, top);
       const float f = __builtin_amdgcn_exp2f(ref - to);
@@ -186,36 +221,88 @@ k_prompt_attn(const PromptArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[x][i] *= f;
     }
-    float sum = 0.0f;
-    uint32_t p[2][8];
+  };
+  // weights of 16 keys, to 8 bits, as the values they meet
+  const auto weights = [&](const f32x16* of, int k) {
+    u32x4 p;
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int i = 0; i < 8; i += 2) {
+      const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(of[k / 2][8 * (k % 2) + i], a.c, -ref));
+      const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(of[k / 2][8 * (k % 2) + i + 1], a.c, -ref));
+      l += y + z;
+      p[i / 2] = pack_bf16(y, z);
+    }
+    return __builtin_bit_cast(bf16x8, p);
+  };
+  const auto values = [&](bf16x8 p, int k, int x, int buf) {
+    const uint8_t* at = v_from[x] + buf * S::Tile + 16 * k * S::RowBytes;
+    const i16x4 v0 = read_transposed(at);
+    const i16x4 v1 = read_transposed(at + 8 * S::RowBytes);
+    const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+    o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p, o[x], 0, 0, 0);
+  };
+
+  // One tile: the next one's scores are formed while this one's weights are,
+  // and the loads of the tile after land behind both.
+  const auto step = [&](int t, auto buf_) {
+    constexpr int buf = decltype(buf_)::value;
+    if (t + 2 < t1) load_k(t + 2, buf);
+    load_v(t + 1, buf ^ 1);
+    bf16x8 p[4];
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][i], a.c, -ref));
-        const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][i + 1], a.c, -ref));
-        sum += y + z;
-        p[x][i / 2] = pack_bf16(y, z);   // to 8 bits, as the values they meet
-      }
-    l += sum;
-    const uint8_t* vp =
-        sv + (4 * part + (lane % 16) / 4) * S::VRow + (16 * ((lane / 16) % 2) + 4 * (lane % 4)) * 2;
+    for (int x = 0; x < 2; ++x) {
+      sn[x] = f32x16{};
+#pragma unroll
+      for (int k = 0; k < 2 * NG; ++k) scores(sn, x, k, buf ^ 1);
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) p[k] = weights(s, k);
+    hide(sn, t + 1);
+    p[3] = weights(s, 3);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int x = 0; x < NG; ++x) values(p[k], k, x, buf);
+    const float top = largest(sn);
+    follow(top);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) s[x] = sn[x];
+    pa_arrive();
+  };
+  const auto last = [&](int buf) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      u32x4 pk;
+      const bf16x8 p = weights(s, k);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) pk[i] = p[k / 2][4 * (k % 2) + i];
-      const bf16x8 pf = __builtin_bit_cast(bf16x8, pk);
-#pragma unroll
-      for (int x = 0; x < NG; ++x) {
-        const i16x4 v0 = read_transposed(vp + (16 * k) * S::VRow + x * 64);
-        const i16x4 v1 = read_transposed(vp + (16 * k + 8) * S::VRow + x * 64);
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-        o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[x], 0, 0, 0);
-      }
+      for (int x = 0; x < NG; ++x) values(p, k, x, buf);
     }
-    if (t + 1 < t1) stage((t + 1 - t0) & 1);
-    __syncthreads();
+  };
+
+  if (t0 < t1) {
+    load_k(t0, 0);
+    load_v(t0, 0);
+    if (t0 + 1 < t1) load_k(t0 + 1, 1);
+    pa_arrive();
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      s[x] = f32x16{};
+#pragma unroll
+      for (int k = 0; k < 2 * NG; ++k) scores(s, x, k, 0);
+    }
+    hide(s, t0);
+    follow(largest(s));
+    pa_arrive();   // everybody has read the first keys
+    int t = t0;
+    for (; t + 2 < t1; t += 2) {
+      step(t, std::integral_constant<int, 0>{});
+      step(t + 1, std::integral_constant<int, 1>{});
+    }
+    if (t + 1 < t1) {
+      step(t, std::integral_constant<int, 0>{});
+      last(1);
+    } else {
+      last(0);
+    }
   }
   l = sum_halves(l);
 
@@ -289,6 +376,9 @@ struct PaPlan {
   int tiles, splits;
   size_t at_part, bytes;
 };
+
+// a tile's rows are addressed by 32-bit byte offsets
+constexpr int64_t kPaMaxStride = INT32_MAX / (2 * kPaKeys) - 256;
 
 static bool pa_sizes_ok(int B, int H, int Hk, int D, int max_q) {
   if ((D != 64 && D != 96 && D != 128) || H % Hk || H > (1 << 15)) return false;
@@ -365,6 +455,7 @@ fdllm_status fdllm_prompt_attention(const void* q, int64_t q_stride, const void*
   if (q_stride < (int64_t)H * D || k_stride < (int64_t)Hk * D || v_stride < (int64_t)Hk * D || q_stride % 8 ||
       k_stride % 8 || v_stride % 8)
     return FDLLM_ERR_INVALID_ARG;
+  if (k_stride > kPaMaxStride || v_stride > kPaMaxStride) return FDLLM_ERR_SIZE;
   for (const void* p : {q, k, v, (const void*)out, (const void*)workspace})
     if ((uintptr_t)p & 15) return FDLLM_ERR_INVALID_ARG;
   const PaPlan p = pa_plan(B, Tk, H, Hk, D, max_q);
