@@ -65,7 +65,7 @@ __device__ __forceinline__ PaTile pa_tile(const PromptArgs& a, int b, int tile) 
 
 // A tile's rows in LDS lie RowBytes apart, two buffers each of keys and values.
 // Within a row the 16-byte pieces are exchanged by the row's number, so that 16
-// lanes meet all banks when they read a piece of 16 rows (keys) or 32 bytes of
+// lanes meet all banks when they read a piece of 16 rows (keys), and 32 when they read 64 bytes of
 // four rows transposed (values); the loads that write LDS fetch the piece that
 // belongs where they write.
 template <int NG>
@@ -78,7 +78,7 @@ struct PaShape {
   static constexpr int RowsPerLoad = kWave / Pieces;                    // of a wave's load of 1 KiB
   static constexpr int Loads = kPaKeys / kPaWaves / RowsPerLoad;        // a wave, per operand and tile
   __device__ static int swap_k(int row) { return NG == 2 ? row / 2 % 8 : row % 16; }
-  __device__ static int swap_v(int row) { return NG == 2 ? row / 2 % 4 * 2 : row % 8 * 2; }
+  __device__ static int swap_v(int row) { return NG == 2 ? row / 2 % 2 * 4 : row % 4 * 4; }
 };
 
 typedef __attribute__((address_space(3))) void* pa_lds_t;
@@ -104,6 +104,8 @@ __device__ __forceinline__ void pa_dma(i32x4 rsrc, uint32_t lds, uint32_t voff) 
                "s_mov_b32 m0, %0"
                : "=&s"(keep) : "s"(lds), "v"(voff), "s"(rsrc) : "memory");
 }
+
+#define PA_FENCE() __builtin_amdgcn_sched_barrier(0)
 
 // All of this wave's loads to LDS have landed, then everybody's.
 __device__ __forceinline__ void pa_arrive() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -143,7 +145,7 @@ k_prompt_attn(const PromptArgs a) {
   f32x16 o[NG];
 #pragma unroll
   for (int t = 0; t < NG; ++t) o[t] = f32x16{};
-  float ref = kRefFloor, l = 0.0f;   // weights are 2^(c s - ref), l their sum
+  float ref = kRefFloor, l = 0.0f, l2 = 0.0f;   // weights are 2^(c s - ref), l and l2 their sums
 
   // ---- loads to LDS ----
   const uint32_t lds0 = (uint32_t)(uintptr_t)(pa_lds_t)s_mem;
@@ -180,12 +182,16 @@ k_prompt_attn(const PromptArgs a) {
       v_from[x] = s_mem + 2 * S::Tile + row * S::RowBytes + 16 * ((4 * x + piece) ^ S::swap_v(row)) + 8 * (lane % 2);
   }
 
-  // S^T of a tile
-  f32x16 s[2], sn[2];
-  const auto scores = [&](f32x16* to, int x, int k, int buf) {
-    const bf16x8 kf = *(const bf16x8*)(k_from[k] + buf * S::Tile + x * 32 * S::RowBytes);
-    to[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[k], to[x], 0, 0, 0);
+  const auto key_operand = [&](int i, int buf) {   // of product i of a tile's scores
+    return *(const bf16x8*)(k_from[i % (2 * NG)] + buf * S::Tile + (i / (2 * NG)) * 32 * S::RowBytes);
   };
+  const auto value_operand = [&](int i, int buf) {   // of product i of a tile's outputs
+    const uint8_t* at = v_from[i % NG] + buf * S::Tile + 16 * (i / NG) * S::RowBytes;
+    const i16x4 v0 = read_transposed(at);
+    const i16x4 v1 = read_transposed(at + 8 * S::RowBytes);
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  f32x16 s[2], sn[2];   // S^T of a tile and of the next
   // keys that a row does not see
   const auto hide = [&](f32x16* to, int t) {
     const int base = t * kPaKeys;
@@ -216,66 +222,79 @@ k_prompt_attn(const PromptArgs a) {
       const float f = __builtin_amdgcn_exp2f(ref - to);
       ref = to;
       l *= f;
+      l2 *= f;
 #pragma unroll
       for (int x = 0; x < NG; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[x][i] *= f;
     }
   };
-  // weights of 16 keys, to 8 bits, as the values they meet
-  const auto weights = [&](const f32x16* of, int k) {
-    u32x4 p;
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(of[k / 2][8 * (k % 2) + i], a.c, -ref));
-      const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(of[k / 2][8 * (k % 2) + i + 1], a.c, -ref));
-      l += y + z;
-      p[i / 2] = pack_bf16(y, z);
-    }
-    return __builtin_bit_cast(bf16x8, p);
+  // Pair i of a tile's 16 pairs of weights, rounded to 8 bits as the values
+  // they meet; four pairs make the operand of one product of outputs and NG - 1
+  // more.
+  u32x4 p[4];
+  const auto weigh = [&](const f32x16* of, int i) {
+    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(of[i / 8][2 * (i % 8)], a.c, -ref));
+    const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(of[i / 8][2 * (i % 8) + 1], a.c, -ref));
+    l += y;
+    l2 += z;
+    p[i / 4][i % 4] = pack_bf16(y, z);
   };
-  const auto values = [&](bf16x8 p, int k, int x, int buf) {
-    const uint8_t* at = v_from[x] + buf * S::Tile + 16 * k * S::RowBytes;
-    const i16x4 v0 = read_transposed(at);
-    const i16x4 v1 = read_transposed(at + 8 * S::RowBytes);
-    const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-    o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p, o[x], 0, 0, 0);
+  const auto output = [&](bf16x8 v, int i) {
+    o[i % NG] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, p[i / NG]), o[i % NG], 0, 0, 0);
   };
 
   // One tile: the next one's scores are formed while this one's weights are,
-  // and the loads of the tile after land behind both.
-  const auto step = [&](int t, auto buf_) {
-    constexpr int buf = decltype(buf_)::value;
+  // this one's outputs beside the next one's maximum, and the loads of the tile
+  // after land behind both.  The fences keep that order: a product of the
+  // matrix cores, then what the vector units do meanwhile, with LDS reads two
+  // products ahead.
+  const auto step = [&](int t, f32x16* s, f32x16* sn, auto buf_) {
+    constexpr int buf = decltype(buf_)::value, NP = 4 * NG;
     if (t + 2 < t1) load_k(t + 2, buf);
     load_v(t + 1, buf ^ 1);
-    bf16x8 p[4];
+    bf16x8 kf[3], vf[3];
+    kf[0] = key_operand(0, buf ^ 1);
+    kf[1] = key_operand(1, buf ^ 1);
+    PA_FENCE();
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      sn[x] = f32x16{};
+    for (int i = 0; i < NP; ++i) {
+      if (i + 2 < NP) kf[(i + 2) % 3] = key_operand(i + 2, buf ^ 1);
+      else vf[i + 2 - NP] = value_operand(i + 2 - NP, buf);
+      const int x = i / (2 * NG);
+      sn[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % 3], qf[i % (2 * NG)], i % (2 * NG) ? sn[x] : f32x16{}, 0, 0,
+                                                      0);
+      PA_FENCE();
+      // twelve of the sixteen pairs of weights
 #pragma unroll
-      for (int k = 0; k < 2 * NG; ++k) scores(sn, x, k, buf ^ 1);
+      for (int w = i * 12 / NP; w < (i + 1) * 12 / NP; ++w) weigh(s, w);
+      PA_FENCE();
     }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) p[k] = weights(s, k);
+    // (the weights stay on this side of the branch)
+    asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(p[2]), "+v"(l), "+v"(l2));
     hide(sn, t + 1);
-    p[3] = weights(s, 3);
+    float top = kNegInf;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int i = 0; i < NP; ++i) {
+      if (i + 2 < NP) vf[(i + 2) % 3] = value_operand(i + 2, buf);
+      output(vf[i % 3], i);
+      PA_FENCE();
+      // the last four pairs, before the products that need them, and the
+      // next tile's maximum
+      if (i < 2 * NG && i * 8 / NP != (i + 1) * 8 / NP) weigh(s, 12 + i * 8 / NP);
 #pragma unroll
-      for (int x = 0; x < NG; ++x) values(p[k], k, x, buf);
-    const float top = largest(sn);
-    follow(top);
-#pragma unroll
-    for (int x = 0; x < 2; ++x) s[x] = sn[x];
+      for (int m = i * 16 / NP; m < (i + 1) * 16 / NP; ++m)
+        top = fmaxf(fmaxf(top, sn[m / 8][2 * (m % 8)]), sn[m / 8][2 * (m % 8) + 1]);
+      PA_FENCE();
+    }
+    follow(max_halves(top) * a.c);
     pa_arrive();
   };
-  const auto last = [&](int buf) {
+  const auto last = [&](const f32x16* s, int buf) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const bf16x8 p = weights(s, k);
+    for (int i = 0; i < 16; ++i) weigh(s, i);
 #pragma unroll
-      for (int x = 0; x < NG; ++x) values(p, k, x, buf);
-    }
+    for (int i = 0; i < 4 * NG; ++i) output(value_operand(i, buf), i);
   };
 
   if (t0 < t1) {
@@ -284,27 +303,29 @@ k_prompt_attn(const PromptArgs a) {
     if (t0 + 1 < t1) load_k(t0 + 1, 1);
     pa_arrive();
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      s[x] = f32x16{};
+    for (int x = 0; x < 2; ++x) s[x] = f32x16{};
 #pragma unroll
-      for (int k = 0; k < 2 * NG; ++k) scores(s, x, k, 0);
-    }
+    for (int i = 0; i < 4 * NG; ++i)
+      s[i / (2 * NG)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand(i, 0), qf[i % (2 * NG)], s[i / (2 * NG)], 0,
+                                                                0, 0);
     hide(s, t0);
     follow(largest(s));
     pa_arrive();   // everybody has read the first keys
     int t = t0;
+    typedef std::integral_constant<int, 0> Even;
+    typedef std::integral_constant<int, 1> Odd;
     for (; t + 2 < t1; t += 2) {
-      step(t, std::integral_constant<int, 0>{});
-      step(t + 1, std::integral_constant<int, 1>{});
+      step(t, s, sn, Even{});
+      step(t + 1, sn, s, Odd{});
     }
     if (t + 1 < t1) {
-      step(t, std::integral_constant<int, 0>{});
-      last(1);
+      step(t, s, sn, Even{});
+      last(sn, 1);
     } else {
-      last(0);
+      last(s, 0);
     }
   }
-  l = sum_halves(l);
+  l = sum_halves(l + l2);
 
   if (pt.parts == 1) {
     if (!row_ok) return;
