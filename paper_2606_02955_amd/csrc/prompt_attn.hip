@@ -245,22 +245,18 @@ k_prompt_attn(const PromptArgs a) {
   };
 
   // One tile: the next one's scores are formed while this one's weights are,
-  // this one's outputs beside the next one's maximum, and the loads of the tile
-  // after land behind both.  The fences keep that order: a product of the
-  // matrix cores, then what the vector units do meanwhile, with LDS reads two
-  // products ahead.
+  // then this one's outputs beside the next one's maximum.  The workgroup meets
+  // once a tile, between the two: what a tile reads after the meeting has had a
+  // whole tile's time to land, and what it read before may be written over.
+  // The fences keep the order within: a product of the matrix cores, then what
+  // the vector units do meanwhile, with LDS reads two products ahead.
+  bf16x8 kf[3], vf[3];
   const auto step = [&](int t, f32x16* s, f32x16* sn, auto buf_) {
     constexpr int buf = decltype(buf_)::value, NP = 4 * NG;
-    if (t + 2 < t1) load_k(t + 2, buf);
-    load_v(t + 1, buf ^ 1);
-    bf16x8 kf[3], vf[3];
-    kf[0] = key_operand(0, buf ^ 1);
-    kf[1] = key_operand(1, buf ^ 1);
     PA_FENCE();
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       if (i + 2 < NP) kf[(i + 2) % 3] = key_operand(i + 2, buf ^ 1);
-      else vf[i + 2 - NP] = value_operand(i + 2 - NP, buf);
       const int x = i / (2 * NG);
       sn[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % 3], qf[i % (2 * NG)], i % (2 * NG) ? sn[x] : f32x16{}, 0, 0,
                                                       0);
@@ -273,33 +269,39 @@ k_prompt_attn(const PromptArgs a) {
     // (the weights stay on this side of the branch)
     asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(p[2]), "+v"(l), "+v"(l2));
     hide(sn, t + 1);
+    pa_arrive();
+    if (t + 3 < t1) load_k(t + 3, buf ^ 1);
+    load_v(t + 1, buf ^ 1);
+    vf[0] = value_operand(0, buf);
+    vf[1] = value_operand(1, buf);
+    PA_FENCE();
+#pragma unroll
+    for (int w = 12; w < 16; ++w) weigh(s, w);
     float top = kNegInf;
+    PA_FENCE();
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       if (i + 2 < NP) vf[(i + 2) % 3] = value_operand(i + 2, buf);
+      else kf[i + 2 - NP] = key_operand(i + 2 - NP, buf);   // of the tile after next
       output(vf[i % 3], i);
       PA_FENCE();
-      // the last four pairs, before the products that need them, and the
-      // next tile's maximum
-      if (i < 2 * NG && i * 8 / NP != (i + 1) * 8 / NP) weigh(s, 12 + i * 8 / NP);
 #pragma unroll
       for (int m = i * 16 / NP; m < (i + 1) * 16 / NP; ++m)
         top = fmaxf(fmaxf(top, sn[m / 8][2 * (m % 8)]), sn[m / 8][2 * (m % 8) + 1]);
       PA_FENCE();
     }
     follow(max_halves(top) * a.c);
-    pa_arrive();
   };
   const auto last = [&](const f32x16* s, int buf) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) weigh(s, i);
+    pa_arrive();
 #pragma unroll
     for (int i = 0; i < 4 * NG; ++i) output(value_operand(i, buf), i);
   };
 
   if (t0 < t1) {
     load_k(t0, 0);
-    load_v(t0, 0);
     if (t0 + 1 < t1) load_k(t0 + 1, 1);
     pa_arrive();
 #pragma unroll
@@ -310,7 +312,11 @@ k_prompt_attn(const PromptArgs a) {
                                                                 0, 0);
     hide(s, t0);
     follow(largest(s));
+    kf[0] = key_operand(0, 1);
+    kf[1] = key_operand(1, 1);
     pa_arrive();   // everybody has read the first keys
+    if (t0 + 2 < t1) load_k(t0 + 2, 0);
+    load_v(t0, 0);
     int t = t0;
     typedef std::integral_constant<int, 0> Even;
     typedef std::integral_constant<int, 1> Odd;
