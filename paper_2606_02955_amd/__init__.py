@@ -9,6 +9,7 @@ and loading fails loudly when the library has not been built.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -449,6 +450,65 @@ def select(selector: str, conf, eps, mask, block_start, block_end, param, commit
                                                     param, commit, n_commit)
 
 
+# The attention calls are made once a layer, on a few tokens at a time: their
+# checks look at each tensor once and pass plain numbers on.
+def _raw(t: torch.Tensor, dtype, shape, name: str) -> int:
+    """Address of a contiguous GPU tensor of this type and shape."""
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    _ptr(t, dtype, shape, name)
+    raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}")
+
+
+def _opt(t: Optional[torch.Tensor], dtype, shape, name: str) -> int:
+    return 0 if t is None else _raw(t, dtype, shape, name)
+
+
+def _heads(t: torch.Tensor, shape, dtype, name: str):
+    """Address and token stride of [T, heads, D] whose tokens may lie apart."""
+    s = t.stride()
+    if (t.dtype is dtype and t.is_cuda and t.shape == shape and (s[1] == shape[2] or shape[1] == 1)
+            and (s[2] == 1 or shape[2] == 1)):
+        return t.data_ptr(), s[0] if shape[0] > 1 else shape[1] * shape[2]
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    raise ValueError(f"{name}: the heads of a token must lie side by side")
+
+
+def _three(t: torch.Tensor, name: str):
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens, heads, head size], got {tuple(t.shape)}")
+    return t.shape
+
+
+# The current stream's handle; torch.cuda.current_stream builds an object first,
+# which takes 2 us, as long as a launch.
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(t: torch.Tensor) -> int:
+    if _current_stream is not None:
+        return _current_stream(t.get_device())
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _scratch(workspace: Optional[torch.Tensor], need: int, device):
+    """(workspace, its address, its bytes): the caller's, or a new one of the bytes needed."""
+    if workspace is None:
+        if need == 0:
+            return None, 0, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        return workspace, workspace.data_ptr(), need
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous GPU tensor")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+@functools.lru_cache(maxsize=None)
 def fdllm_cache_tile_bytes(head_dim: int) -> int:
     """Bytes of one page (64 tokens) of one key head in the 4-bit cache (layout in fdllm.h)."""
     n = ctypes.c_size_t(0)
@@ -462,52 +522,36 @@ def new_cache(n_pages: int, kv_heads: int, head_dim: int, device=None) -> torch.
                        device=device if device is not None else "cuda")
 
 
-def _heads(t: torch.Tensor, name: str, dtype=None):
-    """Pointer and token stride of [T, heads, D] whose tokens may lie apart."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor")
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be [tokens, heads, head size], got {tuple(t.shape)}")
-    T, h, D = t.shape
-    if t.numel() and ((D > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != D)):
-        raise ValueError(f"{name}: the heads of a token must lie side by side")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    return ctypes.c_void_p(t.data_ptr()), t.stride(0) if T > 1 else h * D
-
-
 def _cache(cache: torch.Tensor, kv_heads: int, head_dim: int):
-    if cache.dim() != 3 or tuple(cache.shape[1:]) != (kv_heads, fdllm_cache_tile_bytes(head_dim)):
-        raise ValueError(f"cache must be [pages, {kv_heads}, {fdllm_cache_tile_bytes(head_dim)}], "
-                         f"got {tuple(cache.shape)}")
-    return _ptr(cache, torch.uint8, name="cache"), cache.shape[0]
+    n_pages = cache.shape[0]
+    return _raw(cache, torch.uint8, (n_pages, kv_heads, fdllm_cache_tile_bytes(head_dim)), "cache"), n_pages
 
 
 def fdllm_qk_norm_rope(q, k, v, positions, cos_sin, q_out, k_out=None, q_weight=None, k_weight=None,
                        eps: float = 1e-6, interleaved: bool = False, cache=None, slots=None):
     """Head norm and rotation of q and k, keys and values into the cache, in one
     pass (see fdllm.h).  cos_sin None: no rotation; v is only read for a cache."""
-    T, H, D = q.shape
-    Hk = k.shape[1]
+    T, H, D = _three(q, "q")
+    Hk, dt = _three(k, "k")[1], q.dtype
     code = _dtype_code(q)
-    qp, qs = _heads(q, "q")
-    kp, ks = _heads(k, "k", q.dtype)
-    if tuple(k.shape) != (T, Hk, D):
-        raise ValueError(f"k must be [{T}, heads, {D}], got {tuple(k.shape)}")
-    vp, vs, cp, n_pages = None, 0, None, 0
+    qp, qs = _heads(q, (T, H, D), dt, "q")
+    kp, ks = _heads(k, (T, Hk, D), dt, "k")
+    vp, vs, cp, n_pages, sp = 0, 0, 0, 0, 0
     if cache is not None:
-        if v is None or tuple(v.shape) != (T, Hk, D):
-            raise ValueError(f"v must be [{T}, {Hk}, {D}] to go into the cache")
-        vp, vs = _heads(v, "v", q.dtype)
+        if v is None or slots is None:
+            raise ValueError("v and slots must be given with a cache")
+        vp, vs = _heads(v, (T, Hk, D), dt, "v")
         cp, n_pages = _cache(cache, Hk, D)
-    n_pos, rot = (0, 0) if cos_sin is None else tuple(cos_sin.shape)
+        sp = _raw(slots, torch.int32, (T,), "slots")
+    n_pos, rot, tp = 0, 0, 0
+    if cos_sin is not None:
+        n_pos, rot = cos_sin.shape
+        tp = _raw(cos_sin, torch.float32, (n_pos, rot), "cos_sin")
     st = load().fdllm_qk_norm_rope(
-        qp, qs, kp, ks, vp, vs, code, T, H, Hk, D, _ptr(q_weight, torch.float32, (D,), "q_weight"),
-        _ptr(k_weight, torch.float32, (D,), "k_weight"), float(eps),
-        _ptr(positions, torch.int32, (T,), "positions"), _ptr(cos_sin, torch.float32, name="cos_sin"), n_pos, rot,
-        int(bool(interleaved)), _ptr(q_out, q.dtype, (T, H, D), "q_out"),
-        _ptr(k_out, q.dtype, (T, Hk, D), "k_out"), cp, n_pages, _ptr(slots, torch.int32, (T,), "slots"),
-        _stream(q.device))
+        qp, qs, kp, ks, vp, vs, code, T, H, Hk, D, _opt(q_weight, torch.float32, (D,), "q_weight"),
+        _opt(k_weight, torch.float32, (D,), "k_weight"), eps, _raw(positions, torch.int32, (T,), "positions"),
+        tp, n_pos, rot, 1 if interleaved else 0, _raw(q_out, dt, (T, H, D), "q_out"),
+        _opt(k_out, dt, (T, Hk, D), "k_out"), cp, n_pages, sp, _stream_of(q))
     _check(st, "fdllm_qk_norm_rope")
 
 
@@ -516,17 +560,18 @@ def fdllm_cache_read(cache, slots, k_out=None, v_out=None):
     like = k_out if k_out is not None else v_out
     if like is None:
         raise ValueError("k_out or v_out must be given")
-    T, Hk, D = like.shape
-    if like.dtype not in (torch.bfloat16, torch.float8_e5m2):
-        raise ValueError(f"the cache is read as bfloat16 or float8_e5m2, got {like.dtype}")
+    T, Hk, D = _three(like, "k_out")
+    dt = like.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float8_e5m2:
+        raise ValueError(f"the cache is read as bfloat16 or float8_e5m2, got {dt}")
     cp, n_pages = _cache(cache, Hk, D)
     st = load().fdllm_cache_read(
-        cp, n_pages, Hk, D, _ptr(slots, torch.int32, (T,), "slots"), T,
-        OUT_BF16 if like.dtype == torch.bfloat16 else OUT_E5M2, _ptr(k_out, like.dtype, (T, Hk, D), "k_out"),
-        _ptr(v_out, like.dtype, (T, Hk, D), "v_out"), _stream(cache.device))
+        cp, n_pages, Hk, D, _raw(slots, torch.int32, (T,), "slots"), T, OUT_BF16 if dt is torch.bfloat16 else OUT_E5M2,
+        _opt(k_out, dt, (T, Hk, D), "k_out"), _opt(v_out, dt, (T, Hk, D), "v_out"), _stream_of(cache))
     _check(st, "fdllm_cache_read")
 
 
+@functools.lru_cache(maxsize=4096)
 def fdllm_cache_attention_workspace_size(B: int, H: int, Hk: int, D: int, max_q: int, table_width: int) -> int:
     n = ctypes.c_size_t(0)
     _check(load().fdllm_cache_attention_workspace_size(B, H, Hk, D, max_q, table_width, ctypes.byref(n)),
@@ -537,25 +582,26 @@ def fdllm_cache_attention_workspace_size(B: int, H: int, Hk: int, D: int, max_q:
 def fdllm_cache_attention(q, cache, page_table, kv_len, cu_q, out, max_q: int, lse=None,
                           scale: Optional[float] = None, blk: int = 0, q_start=None, workspace=None):
     """Attention of q's tokens over the 4-bit cache (see fdllm.h).  scale
-    defaults to 1 / sqrt(head size); returns the workspace for reuse."""
-    T, H, D = q.shape
-    Hk = cache.shape[1]
+    defaults to 1 / sqrt(head size); returns the workspace for reuse (None where
+    the call needs none)."""
+    T, H, D = _three(q, "q")
+    Hk, i32 = cache.shape[1], torch.int32
     B, width = page_table.shape
-    qp, qs = _heads(q, "q", torch.bfloat16)
+    qp, qs = _heads(q, (T, H, D), torch.bfloat16, "q")
     cp, n_pages = _cache(cache, Hk, D)
-    if workspace is None:
-        workspace = torch.empty(fdllm_cache_attention_workspace_size(B, H, Hk, D, int(max_q), width),
-                                dtype=torch.uint8, device=q.device)
+    workspace, wp, wb = _scratch(
+        workspace, 0 if workspace is not None else fdllm_cache_attention_workspace_size(B, H, Hk, D, max_q, width),
+        q.device)
     st = load().fdllm_cache_attention(
-        qp, qs, T, _ptr(cu_q, torch.int32, (B + 1,), "cu_q"), B, int(max_q), H, Hk, D, cp, n_pages,
-        _ptr(page_table, torch.int32, name="page_table"), width, _ptr(kv_len, torch.int32, (B,), "kv_len"),
-        _ptr(q_start, torch.int32, (B,), "q_start"), D ** -0.5 if scale is None else float(scale), int(blk),
-        _ptr(out, torch.bfloat16, (T, H, D), "out"), _ptr(lse, torch.float32, (T, H), "lse"),
-        _ptr(workspace, name="workspace"), workspace.numel() * workspace.element_size(), _stream(q.device))
+        qp, qs, T, _raw(cu_q, i32, (B + 1,), "cu_q"), B, max_q, H, Hk, D, cp, n_pages,
+        _raw(page_table, i32, (B, width), "page_table"), width, _raw(kv_len, i32, (B,), "kv_len"),
+        _opt(q_start, i32, (B,), "q_start"), D ** -0.5 if scale is None else scale, blk,
+        _raw(out, torch.bfloat16, (T, H, D), "out"), _opt(lse, torch.float32, (T, H), "lse"), wp, wb, _stream_of(q))
     _check(st, "fdllm_cache_attention")
     return workspace
 
 
+@functools.lru_cache(maxsize=4096)
 def fdllm_prompt_attention_workspace_size(B: int, Tk: int, H: int, Hk: int, D: int, max_q: int) -> int:
     n = ctypes.c_size_t(0)
     _check(load().fdllm_prompt_attention_workspace_size(B, Tk, H, Hk, D, max_q, ctypes.byref(n)),
@@ -566,25 +612,21 @@ def fdllm_prompt_attention_workspace_size(B: int, Tk: int, H: int, Hk: int, D: i
 def fdllm_prompt_attention(q, k, v, cu_q, cu_k, out, max_q: int, lse=None, scale: Optional[float] = None,
                            blk: int = 0, workspace=None):
     """Attention of packed sequences (see fdllm.h); scale defaults to 1 / sqrt(head
-    size); returns the workspace (None where the call needs none)."""
-    T, H, D = q.shape
-    Tk, Hk = k.shape[:2]
-    if tuple(k.shape) != (Tk, Hk, D) or tuple(v.shape) != (Tk, Hk, D):
-        raise ValueError(f"k and v must be [{Tk}, {Hk}, {D}], got {tuple(k.shape)} and {tuple(v.shape)}")
+    size); returns the workspace for reuse (None where the call needs none)."""
+    T, H, D = _three(q, "q")
+    Tk, Hk, _ = _three(k, "k")
+    bf16 = torch.bfloat16
+    qp, qs = _heads(q, (T, H, D), bf16, "q")
+    kp, ks = _heads(k, (Tk, Hk, D), bf16, "k")
+    vp, vs = _heads(v, (Tk, Hk, D), bf16, "v")
     B = cu_q.shape[0] - 1
-    qp, qs = _heads(q, "q", torch.bfloat16)
-    kp, ks = _heads(k, "k", torch.bfloat16)
-    vp, vs = _heads(v, "v", torch.bfloat16)
-    if workspace is None:
-        need = fdllm_prompt_attention_workspace_size(B, Tk, H, Hk, D, int(max_q))
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    workspace, wp, wb = _scratch(
+        workspace, 0 if workspace is not None else fdllm_prompt_attention_workspace_size(B, Tk, H, Hk, D, max_q),
+        q.device)
     st = load().fdllm_prompt_attention(
-        qp, qs, kp, ks, vp, vs, T, Tk, _ptr(cu_q, torch.int32, (B + 1,), "cu_q"),
-        _ptr(cu_k, torch.int32, (B + 1,), "cu_k"), B, int(max_q), H, Hk, D,
-        D ** -0.5 if scale is None else float(scale), int(blk), _ptr(out, torch.bfloat16, (T, H, D), "out"),
-        _ptr(lse, torch.float32, (T, H), "lse"),
-        _ptr(workspace, name="workspace"), ws_bytes, _stream(q.device))
+        qp, qs, kp, ks, vp, vs, T, Tk, _raw(cu_q, torch.int32, (B + 1,), "cu_q"),
+        _raw(cu_k, torch.int32, (B + 1,), "cu_k"), B, max_q, H, Hk, D, D ** -0.5 if scale is None else scale, blk,
+        _raw(out, bf16, (T, H, D), "out"), _opt(lse, torch.float32, (T, H), "lse"), wp, wb, _stream_of(q))
     _check(st, "fdllm_prompt_attention")
     return workspace
 

@@ -28,8 +28,7 @@
 
 namespace fdllm {
 
-constexpr int kCaThreads = 256;
-constexpr int kCaWaves = kCaThreads / kWave;
+constexpr int kCaMaxWaves = 8;
 
 struct CacheAttnArgs {
   const uint16_t* q;
@@ -67,48 +66,37 @@ __device__ __forceinline__ Seq sequence(const CacheAttnArgs& a, int b) {
   return s;
 }
 
-// Units of the sequences before b0, by all threads of a workgroup.
-template <int Rows>
-__device__ __forceinline__ int units_before(const CacheAttnArgs& a, int b0, int* s_sum) {
-  int n = 0;
-  for (int b = threadIdx.x; b < b0; b += kCaThreads) {
-    const Seq s = sequence<Rows>(a, b);
-    n += s.groups * s.pages;
+// The units are shared out evenly: share g begins at unit g * q + min(g, r), q
+// and r the units by the number of shares.  Only trailing shares are empty.
+struct Shares {
+  int q, r;
+  __device__ __forceinline__ Shares(int units, int n) : q(units / n), r(units % n) {}
+  __device__ __forceinline__ int begin(int g) const { return g * q + min(g, r); }
+  __device__ __forceinline__ int of(int u) const {
+    const int wide = r * (q + 1);   // units in the shares that are one longer
+    return u < wide ? u / (q + 1) : r + (u - wide) / q;
   }
-#pragma unroll
-  for (int x = 1; x < kWave; x <<= 1) n += __shfl_xor(n, x);
-  __syncthreads();
-  if (threadIdx.x % kWave == 0) s_sum[threadIdx.x / kWave] = n;
-  __syncthreads();
-  n = 0;
-#pragma unroll
-  for (int w = 0; w < kCaWaves; ++w) n += s_sum[w];
-  return n * a.Hk;
-}
-
-// First unit of workgroup g's share.
-__device__ __forceinline__ int share_begin(int g, int groups, int units) {
-  return (int)((long long)g * units / groups);
-}
-// The workgroup whose share holds unit u.
-__device__ __forceinline__ int share_of(int u, int groups, int units) {
-  int g = (int)(((long long)u * groups) / units);
-  while (g + 1 < groups && share_begin(g + 1, groups, units) <= u) ++g;
-  while (share_begin(g, groups, units) > u) --g;
-  return g;
-}
+};
 
 // ---------------------------------------------------------------------------
 // NG: groups of 32 elements of a head.  MT: rows of a wave's tile, 16 or 32.
-// WR: waves that hold different rows of an item; the 4 / WR sets of them take
+// WR: waves that hold different rows of an item; the sets of WR waves take
 // different pages.
 // ---------------------------------------------------------------------------
 template <int NG, int MT, int WR>
 struct CaShape {
   static constexpr int D = NG * kGroup;
-  static constexpr int WK = kCaWaves / WR;
+  static constexpr int Waves = WR == 1 ? 8 : 4;
+  static constexpr int Threads = Waves * kWave;
+  static constexpr int WK = Waves / WR;
   static constexpr int Rows = MT * WR;
-  static constexpr int RowBytes = 2 * D + 32;              // of a key's values in LDS: transposed reads meet no bank twice
+  // A key's values in LDS.  The 16-byte pieces of a row are exchanged by the
+  // row's number: 16 lanes that write the same piece of 16 rows, and 32 lanes
+  // that read 32 or 64 bytes of 8 or 4 rows transposed, meet every bank.
+  static constexpr int RowBytes = NG == 2 ? 128 : 256;
+  __device__ static int swap(int row) {
+    return 4 * (NG == 2 ? row / 2 % 2 : row % 4) ^ (2 * (row / 4 % 2) + row / 8 % 2);
+  }
   static constexpr int PageBytes = kPage * RowBytes;
   static constexpr int Buffers = WR > 1 ? 2 : 1;
   static constexpr int ValueBytes = WK * Buffers * PageBytes;
@@ -197,40 +185,60 @@ __device__ __forceinline__ u32x4 unpack8(uint32_t c, float s) {
 }
 
 template <int NG, int MT, int WR>
-__global__ void __launch_bounds__(kCaThreads, 2)
+__global__ void __launch_bounds__((CaShape<NG, MT, WR>::Threads), 2)
 k_cache_attn(const CacheAttnArgs a) {
   typedef CaShape<NG, MT, WR> S;
   constexpr int D = S::D, SPT = S::SPT, WK = S::WK;
   typedef typename std::conditional<MT == 32, f32x16, f32x4>::type Acc;
   extern __shared__ __align__(16) uint8_t s_mem[];
-  __shared__ int s_sum[kCaWaves];
-  __shared__ float s_ml[kCaWaves][MT][2];
+  __shared__ int s_sum[kCaMaxWaves], s_at[2];
+  __shared__ float s_ml[S::Waves][MT][2];
 
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int wr = wave % WR, wk = wave / WR;   // its rows, its pages
   const int col = lane % MT, part = lane / MT;
 
-  // this workgroup's share of the units
-  const int units = units_before<S::Rows>(a, a.B, s_sum);
+  // Units of all sequences, this workgroup's share of them, and the sequence of
+  // its first: a thread counts a few neighbouring sequences, a scan adds up.
+  const int per = (a.B + S::Threads - 1) / S::Threads, b0 = tid * per, b1 = min(b0 + per, a.B);
+  int mine = 0;
+  for (int i = b0; i < b1; ++i) {
+    const Seq s = sequence<S::Rows>(a, i);
+    mine += s.groups * s.pages * a.Hk;
+  }
+  int incl = mine;
+#pragma unroll
+  for (int x = 1; x < kWave; x <<= 1) {
+    const int y = __shfl_up(incl, x);
+    if (lane >= x) incl += y;
+  }
+  if (lane == kWave - 1) s_sum[wave] = incl;
+  __syncthreads();
+  int units = 0;
+#pragma unroll
+  for (int w = 0; w < S::Waves; ++w) {
+    if (w == wave) incl += units;
+    units += s_sum[w];
+  }
   if (units == 0) return;
-  const int u_begin = share_begin(blockIdx.x, gridDim.x, units);
-  const int u_end = share_begin(blockIdx.x + 1, gridDim.x, units);
+  const Shares shares(units, gridDim.x);
+  const int u_begin = shares.begin(blockIdx.x), u_end = shares.begin(blockIdx.x + 1);
   if (blockIdx.x == 0 && tid == 0) a.plan[0] = units;
   if (u_begin >= u_end) return;
-
-  // the sequence of its first unit: 256 at a time, then by steps
-  int b = 0, before = 0;
-  for (int chunk = kCaThreads; chunk < a.B; chunk += kCaThreads) {
-    const int n = units_before<S::Rows>(a, chunk, s_sum);
-    if (n > u_begin) break;
-    b = chunk;
-    before = n;
+  if (u_begin >= incl - mine && u_begin < incl) {
+    int i = b0, n = incl - mine;
+    for (;; ++i) {
+      const Seq s = sequence<S::Rows>(a, i);
+      const int k = s.groups * s.pages * a.Hk;
+      if (u_begin < n + k) break;
+      n += k;
+    }
+    s_at[0] = i;
+    s_at[1] = n;
   }
+  __syncthreads();
+  int b = __builtin_amdgcn_readfirstlane(s_at[0]), before = __builtin_amdgcn_readfirstlane(s_at[1]);
   Seq seq = sequence<S::Rows>(a, b);
-  while (before + seq.groups * seq.pages * a.Hk <= u_begin) {
-    before += seq.groups * seq.pages * a.Hk;
-    seq = sequence<S::Rows>(a, ++b);
-  }
 
   int u = u_begin;
   int slot = 0;                       // of the next partial result
@@ -293,9 +301,9 @@ k_cache_attn(const CacheAttnArgs a) {
         const int w = (i * WR + wr) * kWave + lane, key = w % kPage, g = w / kPage;
         if (S::VPairs % (WR * kWave) != 0 && w >= S::VPairs) break;
         const float sv = scale_of(there && base + key < seq.len ? next.vs[i] : 1u);
-        u32x4* dst = (u32x4*)(lds + key * S::RowBytes + g * 64);
+        uint8_t* dst = lds + key * S::RowBytes;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) dst[j] = unpack8(next.v[i][j], sv);
+        for (int j = 0; j < 4; ++j) *(u32x4*)(dst + 16 * ((4 * g + j) ^ S::swap(key))) = unpack8(next.v[i][j], sv);
       }
 
       // scores
@@ -362,8 +370,9 @@ k_cache_attn(const CacheAttnArgs a) {
       if (WR > 1) __syncthreads();
       else __builtin_amdgcn_wave_barrier();
       // a group of 16 lanes reads four keys by 16 elements, transposed
-      const uint8_t* vp = lds + (4 * part + (lane % 16) / 4) * S::RowBytes +
-                          (MT == 32 ? 16 * ((lane / 16) % 2) + 4 * (lane % 4) : 4 * (lane % 4)) * 2;
+      const int vrow = 4 * part + (lane % 16) / 4;
+      const int vpiece = (MT == 32 ? 2 * ((lane / 16) % 2) : 0) + (lane % 4) / 2;
+      const uint8_t* vp = lds + vrow * S::RowBytes + 8 * (lane % 2);
       constexpr int KS = MT == 32 ? 4 : 2;   // steps of the second product
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
@@ -374,9 +383,12 @@ k_cache_attn(const CacheAttnArgs a) {
         const bf16x8 pf = __builtin_bit_cast(bf16x8, pk);
 #pragma unroll
         for (int t = 0; t < S::DT; ++t) {
-          const uint8_t* at = vp + k * (MT == 32 ? 16 : 32) * S::RowBytes + t * MT * 2;
-          const i16x4 v0 = read_transposed(at);
-          const i16x4 v1 = read_transposed(at + (MT == 32 ? 8 : 16) * S::RowBytes);
+          // the second read's rows are 8 or 16 further on
+          const int piece = (vpiece + t * MT / 8) ^ S::swap(vrow);
+          const uint8_t* at = vp + k * (MT == 32 ? 16 : 32) * S::RowBytes;
+          const i16x4 v0 = read_transposed(at + 16 * piece);
+          const i16x4 v1 = MT == 32 ? read_transposed(at + 8 * S::RowBytes + 16 * (piece ^ 1))
+                                    : read_transposed(at + 16 * S::RowBytes + 16 * piece);
           const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
           if constexpr (MT == 32) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[t], 0, 0, 0);
           else o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[t], 0, 0, 0);
@@ -455,62 +467,57 @@ k_cache_attn(const CacheAttnArgs a) {
 }
 
 // Joins the partial results of an item that several workgroups share, always
-// in the same order.  A workgroup takes four rows, 16 lanes a row, and divides
-// the parts of a row among its waves: what a part costs is a round trip to
-// memory, so as many as possible are under way at once.
-constexpr int kCaJoinRows = 4;
+// in the same order.  16 lanes take a row.  Where items lie in many shares, the
+// Split sixteenths of a workgroup's waves divide the parts of a row (what a part
+// costs is a round trip to memory, so as many as possible are under way at
+// once); where they lie in two or so, every 16 lanes have a row of their own.
+constexpr int kCaJoinThreads = 256;
 
-template <int NG, int Rows>
-__global__ void __launch_bounds__(kCaThreads)
+template <int NG, int Rows, int Split>
+__global__ void __launch_bounds__(kCaJoinThreads)
 k_cache_join(const CacheAttnArgs a, int wgs) {
   constexpr int D = NG * kGroup, Lanes = 16;
-  constexpr int Blocks = Rows / kCaJoinRows;   // of a group of rows
-  __shared__ float s_acc[kCaWaves][kCaJoinRows][D];
-  __shared__ float s_ml[kCaWaves][kCaJoinRows][2];
+  constexpr int RowsHere = kCaJoinThreads / Lanes / Split;
+  constexpr int Blocks = Rows / RowsHere;   // of a group of rows
+  __shared__ float s_acc[Split > 1 ? Split : 1][RowsHere][Split > 1 ? D : 1];
+  __shared__ float s_ml[Split][RowsHere][2];
   const int b = blockIdx.y;
   const int item = blockIdx.x / Blocks;
   const Seq seq = sequence<Rows>(a, b);
   if (item >= seq.groups * a.Hk) return;
   const int h = item % a.Hk, group = item / a.Hk;
-  const int x0 = (blockIdx.x % Blocks) * kCaJoinRows;
+  const int x0 = (blockIdx.x % Blocks) * RowsHere;
   if (group * Rows + x0 >= seq.n * a.R) return;
-  const int units = a.plan[0];
+  const Shares shares(a.plan[0], wgs);
   const int u0 = a.plan[1 + b] + item * seq.pages;
-  const int g0 = share_of(u0, wgs, units), g1 = share_of(u0 + seq.pages - 1, wgs, units);
+  const int g0 = shares.of(u0), g1 = shares.of(u0 + seq.pages - 1);
   if (g0 == g1) return;
-  const int wave = threadIdx.x / kWave, lane = threadIdx.x % Lanes, xr = threadIdx.x % kWave / Lanes;
+  const int lane = threadIdx.x % Lanes, xr = threadIdx.x / Lanes % RowsHere, sp = threadIdx.x / Lanes / RowsHere;
   const int x = x0 + xr;
-  // Part i of the row.  An item that begins inside a share is that workgroup's
-  // second result; a share may be empty (it weighs nothing then, and the first
-  // part's address stands in for its own).
-  const auto part_of = [&](int g, bool* there) {
-    const int begin = share_begin(g, wgs, units);
-    *there = g <= g1 && begin < share_begin(g + 1, wgs, units);
-    const int gg = *there ? g : g0;
-    return ((size_t)gg * 2 + (share_begin(gg, wgs, units) < u0 ? 1 : 0)) * Rows + x;
-  };
+  // an item that begins inside a share is that workgroup's second result
+  const int first = (g0 * 2 + (shares.begin(g0) < u0 ? 1 : 0)) * Rows + x;
+  const auto row_of = [&](int g) { return g == g0 ? first : g * 2 * Rows + x; };
   float acc[2 * NG], l = 0.0f, ref = kRefFloor;
 #pragma unroll
   for (int i = 0; i < 2 * NG; ++i) acc[i] = 0.0f;
-  // 16 parts at a time of every 64: a lane each for their references and sums
-  for (int c = g0 + wave * Lanes; c <= g1; c += kCaWaves * Lanes) {
-    bool there;
-    const size_t row = part_of(c + lane, &there);
-    const float2 ml = *(const float2*)(a.part_ml + row * 2);
-    float to = there ? fmaxf(ref, ml.x) : ref;
+  for (int c = g0 + sp * Lanes; c <= g1; c += Split * Lanes) {
+    // a lane each for the references and sums of 16 parts
+    const int n = min(Lanes, g1 + 1 - c);
+    const int row = row_of(lane < n ? c + lane : g0);
+    const float2 ml = *(const float2*)(a.part_ml + (size_t)row * 2);
+    float to = lane < n ? fmaxf(ref, ml.x) : ref;
 #pragma unroll
     for (int s = 1; s < Lanes; s <<= 1) to = fmaxf(to, __shfl_xor(to, s));
     const float f0 = __builtin_amdgcn_exp2f(ref - to);
     ref = to;
-    const float f = there ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.0f;
+    const float f = lane < n ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.0f;
     l = l * f0 + f * ml.y;     // of this lane's parts
 #pragma unroll
     for (int i = 0; i < 2 * NG; ++i) acc[i] *= f0;
-    const int n = min(Lanes, g1 + 1 - c);
 #pragma unroll 8
     for (int k = 0; k < n; ++k) {
       const float fk = __shfl(f, k, Lanes);
-      const float* src = a.part + (size_t)__shfl((int)row, k, Lanes) * D + 2 * lane;
+      const float* src = a.part + (size_t)row_of(c + k) * D + 2 * lane;
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
         const float2 v = *(const float2*)(src + 32 * i);
@@ -521,29 +528,43 @@ k_cache_join(const CacheAttnArgs a, int wgs) {
   }
 #pragma unroll
   for (int s = 1; s < Lanes; s <<= 1) l += __shfl_xor(l, s);
+  if constexpr (Split > 1) {
+    if (sp > 0) {
 #pragma unroll
-  for (int i = 0; i < NG; ++i) *(float2*)&s_acc[wave][xr][32 * i + 2 * lane] = float2{acc[2 * i], acc[2 * i + 1]};
-  if (lane == 0) s_ml[wave][xr][0] = ref, s_ml[wave][xr][1] = l;
-  __syncthreads();
-  // a wave a row, two elements a lane
-  const int r = group * Rows + x0 + wave;
-  if (r >= seq.n * a.R) return;
-  float m = kRefFloor;
+      for (int i = 0; i < NG; ++i) *(float2*)&s_acc[sp][xr][32 * i + 2 * lane] = float2{acc[2 * i], acc[2 * i + 1]};
+      if (lane == 0) s_ml[sp][xr][0] = ref, s_ml[sp][xr][1] = l;
+    }
+    __syncthreads();
+    if (sp > 0) return;
+    float to = ref;
 #pragma unroll
-  for (int w = 0; w < kCaWaves; ++w) m = fmaxf(m, s_ml[w][wave][0]);
-  float sum = 0.0f, y = 0.0f, z = 0.0f;
-  const int e = 2 * (threadIdx.x % kWave);
+    for (int w = 1; w < Split; ++w) to = fmaxf(to, s_ml[w][xr][0]);
+    const float f0 = __builtin_amdgcn_exp2f(ref - to);
+    ref = to;
+    l *= f0;
 #pragma unroll
-  for (int w = 0; w < kCaWaves; ++w) {
-    const float f = __builtin_amdgcn_exp2f(s_ml[w][wave][0] - m);
-    sum += f * s_ml[w][wave][1];
-    if (e < D) y += f * s_acc[w][wave][e], z += f * s_acc[w][wave][e + 1];
+    for (int i = 0; i < 2 * NG; ++i) acc[i] *= f0;
+#pragma unroll
+    for (int w = 1; w < Split; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_ml[w][xr][0] - ref);
+      l += f * s_ml[w][xr][1];
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const float2 v = *(const float2*)&s_acc[w][xr][32 * i + 2 * lane];
+        acc[2 * i] += f * v.x;
+        acc[2 * i + 1] += f * v.y;
+      }
+    }
   }
+  const int r = group * Rows + x;
+  if (r >= seq.n * a.R) return;
   const int tok = r / a.R, head = h * a.R + r % a.R;
   const size_t at = (size_t)(seq.first + tok) * a.H + head;
-  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-  if (e < D) *(uint32_t*)(a.out + at * D + e) = pack_bf16(y * inv, z * inv);
-  if (a.lse && e == 0) a.lse[at] = sum > 0.0f ? (m + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+  for (int i = 0; i < NG; ++i)
+    *(uint32_t*)(a.out + at * D + 32 * i + 2 * lane) = pack_bf16(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+  if (a.lse && lane == 0) a.lse[at] = l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
 }
 
 // ---------------------------------------------------------------------------
@@ -553,6 +574,7 @@ struct CaPlan {
   int mt, wr;        // variant
   int wgs;           // workgroups
   int items;         // items of a sequence with max_q query tokens
+  bool join, split;  // whether items may lie in several shares; in many
   size_t at_ml, at_part, bytes;
 };
 
@@ -576,11 +598,14 @@ static CaPlan ca_plan(int B, int H, int Hk, int D, int max_q, int table_w) {
   const int per = p.mt * p.wr;
   const long long groups = (rows + per - 1) / per;
   p.items = (int)(groups * Hk);
-  const int wk = kCaWaves / p.wr;
-  // shares of at least one page for each set of waves, two workgroups a CU
-  const long long most = (long long)B * p.items * ((table_w + wk - 1) / wk);
-  p.wgs = (int)(most < 512 ? most : 512);
-  if (p.wgs < 1) p.wgs = 1;
+  const int waves = p.wr == 1 ? 8 : 4, wk = waves / p.wr;
+  // shares of at least one page for each set of waves, eight waves a CU
+  const long long items = (long long)B * p.items, most = items * ((table_w + wk - 1) / wk);
+  const int fill = 256 * 8 / waves;
+  p.wgs = (int)(most < fill ? (most < 1 ? 1 : most) : fill);
+  // equal items that the shares are a multiple of, or one share: none is split
+  p.join = p.wgs > 1 && !(B == 1 && p.wgs == items);
+  p.split = p.wgs >= 4 * items;
   const size_t rows_out = (size_t)p.wgs * 2 * per;
   p.at_ml = align256(((size_t)B + 1) * 4);
   p.at_part = p.at_ml + align256(rows_out * 8);
@@ -605,10 +630,13 @@ static hipError_t ca_launch_one(const CacheAttnArgs& a, const CaPlan& p, hipStre
     if (e != hipSuccess) return e;
     if (dev >= 0 && dev < kCaMaxDevices) allowed[dev].store(true, std::memory_order_release);
   }
-  hipLaunchKernelGGL((k_cache_attn<NG, MT, WR>), dim3((unsigned)p.wgs), dim3(kCaThreads), S::LdsBytes, st, a);
-  if (p.wgs > 1)
-    hipLaunchKernelGGL((k_cache_join<NG, S::Rows>), dim3((unsigned)(p.items * (S::Rows / kCaJoinRows)), (unsigned)a.B),
-                       dim3(kCaThreads), 0, st, a, p.wgs);
+  hipLaunchKernelGGL((k_cache_attn<NG, MT, WR>), dim3((unsigned)p.wgs), dim3(S::Threads), S::LdsBytes, st, a);
+  if (p.join && p.split)
+    hipLaunchKernelGGL((k_cache_join<NG, S::Rows, 4>), dim3((unsigned)(p.items * (S::Rows / 4)), (unsigned)a.B),
+                       dim3(kCaJoinThreads), 0, st, a, p.wgs);
+  else if (p.join)
+    hipLaunchKernelGGL((k_cache_join<NG, S::Rows, 1>), dim3((unsigned)(p.items * (S::Rows / 16)), (unsigned)a.B),
+                       dim3(kCaJoinThreads), 0, st, a, p.wgs);
   return hipGetLastError();
 }
 
