@@ -30,6 +30,9 @@ namespace fdllm {
 
 constexpr int kCaMaxWaves = 8;
 
+// keeps instructions on their side: the order of the loop below is the one written
+#define CA_FENCE() __builtin_amdgcn_sched_barrier(0)
+
 struct CacheAttnArgs {
   const uint16_t* q;
   long long q_stride;
@@ -135,11 +138,12 @@ struct PageRegs {
   uint32_t ks[S::SPT];            // scales of the lane's key of a subtile
   u32x4 v[S::VPer];
   uint32_t vs[S::VPer];
-  bool there;
 
-  __device__ __forceinline__ void load(const CacheAttnArgs& a, int page, int h, int lane, int wr) {
-    there = page >= 0 && page < a.n_pages;
-    const uint8_t* tile = a.cache + ((size_t)(there ? page : 0) * a.Hk + h) * tile_bytes(S::D);
+  __device__ __forceinline__ static const uint8_t* tile_of(const CacheAttnArgs& a, int page, int h) {
+    const bool there = page >= 0 && page < a.n_pages;
+    return a.cache + ((size_t)(there ? page : 0) * a.Hk + h) * tile_bytes(S::D);
+  }
+  __device__ __forceinline__ void load_k(const uint8_t* tile, int lane) {
     const int col = lane % MT, part = lane / MT;
 #pragma unroll
     for (int x = 0; x < S::SPT; ++x) {
@@ -166,6 +170,8 @@ struct PageRegs {
         for (int s = 0; s < S::Steps; ++s) k[x][s] = *(const uint32_t*)(codes + s * kPage * kCodeBytes + 4 * part);
       }
     }
+  }
+  __device__ __forceinline__ void load_v(const uint8_t* tile, int lane, int wr) {
 #pragma unroll
     for (int i = 0; i < S::VPer; ++i) {
       const int w = min((i * WR + wr) * kWave + lane, S::VPairs - 1), key = w % kPage, g = w / kPage;
@@ -240,6 +246,16 @@ k_cache_attn(const CacheAttnArgs a) {
   int b = __builtin_amdgcn_readfirstlane(s_at[0]), before = __builtin_amdgcn_readfirstlane(s_at[1]);
   Seq seq = sequence<S::Rows>(a, b);
 
+  // Where a lane reads its part of a page's values: a group of 16 lanes reads
+  // four keys by 16 elements, transposed.
+  int v_at[S::DT];
+  {
+    const int row = 4 * part + (lane % 16) / 4, piece = (MT == 32 ? 2 * ((lane / 16) % 2) : 0) + (lane % 4) / 2;
+#pragma unroll
+    for (int t = 0; t < S::DT; ++t)
+      v_at[t] = row * S::RowBytes + 16 * ((piece + t * MT / 8) ^ S::swap(row)) + 8 * (lane % 2);
+  }
+
   int u = u_begin;
   int slot = 0;                       // of the next partial result
   int buf = 0;                        // of values in LDS; goes on from item to item, so that one barrier a page will do
@@ -278,21 +294,64 @@ k_cache_attn(const CacheAttnArgs a) {
     Acc o[S::DT];
 #pragma unroll
     for (int t = 0; t < S::DT; ++t) o[t] = Acc{};
-    float ref = kRefFloor, l = 0.0f;   // weights are 2^(c s - ref), l their sum
+    float ref = kRefFloor, l = 0.0f, l2 = 0.0f;   // weights are 2^(c s - ref), l and l2 their sums
 
     // ---- the pages ----
     const int32_t* table = a.table + (size_t)b * a.table_w;
     // of a page whose tokens all lie past the sequence's end the table says nothing
-    const auto page_id = [&](int pg) { return pg < page1 && pg * kPage < seq.len ? table[pg] : -1; };
+    // The pages' numbers, 64 at a time, a lane each: a load for every page would
+    // have to be waited for behind the page before.
+    int ids_at = page0, ids = -1;
+    const auto load_ids = [&]() {
+      const int pg = ids_at + lane;
+      ids = pg < page1 && pg * kPage < seq.len ? table[pg] : -1;
+      // waited for here, so that nobody waits behind the branch
+      asm volatile("s_waitcnt vmcnt(0)" : "+v"(ids));
+    };
+    const auto page_id = [&](int pg) {
+      if (pg - ids_at >= kWave) {
+        ids_at = pg;
+        load_ids();
+      }
+      return __builtin_amdgcn_readlane(ids, pg - ids_at);
+    };
+    load_ids();
     PageRegs<NG, MT, WR> next;
-    next.load(a, page_id(page0 + wk), h, lane, wr);
-    int next_id = page_id(page0 + wk + WK);
+    int id = page_id(page0 + wk), next_id = page_id(page0 + wk + WK);
+    const uint8_t* tile = next.tile_of(a, id, h);
+    next.load_k(tile, lane);
+    CA_FENCE();
+    next.load_v(tile, lane, wr);   // after the keys here too: the loop waits for its loads in this order
+    CA_FENCE();
     // sets of waves without a page left go along while others' barriers run
     for (int pg = page0 + wk; WR == 1 ? pg < page1 : pg - wk < page1; pg += WK) {
       const int base = pg * kPage;
-      const bool there = next.there;
+      const bool there = id >= 0 && id < a.n_pages;
       uint8_t* lds = s_mem + (wk * S::Buffers + buf) * S::PageBytes;
       if (S::Buffers > 1) buf ^= 1;
+
+      // scores: a step's keys are unpacked while the one before is multiplied
+      Acc sc[SPT];
+#pragma unroll
+      for (int x = 0; x < SPT; ++x) {
+        bf16x8 kf;
+#pragma unroll
+        for (int s = 0; s < S::Steps; ++s) {
+          const int g = MT == 32 ? (NG % 2 == 0 || s < 4 * (NG / 2) ? 2 * (s / 4) + part : NG - 1)
+                                 : NG == 4 ? part : NG == 2 ? part / 2 : s;
+          const float ksv = scale_of((next.ks[x] >> (8 * g)) & 255u);
+          kf = __builtin_bit_cast(bf16x8, unpack8(next.k[x][s], ksv));
+          const Acc from = s ? sc[x] : Acc{};
+          if constexpr (MT == 32) sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[s], from, 0, 0, 0);
+          else sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[s], from, 0, 0, 0);
+          if (s % 2) CA_FENCE();
+        }
+      }
+      // the registers of what is used are loaded for the next page at once
+      id = next_id;
+      tile = next.tile_of(a, id, h);
+      next.load_k(tile, lane);
+      CA_FENCE();
 
       // values: a lane unpacks 32 elements of a key.  Keys past the end get a
       // scale of next to nothing: their weight is 0, and a code is finite.
@@ -304,25 +363,11 @@ k_cache_attn(const CacheAttnArgs a) {
         uint8_t* dst = lds + key * S::RowBytes;
 #pragma unroll
         for (int j = 0; j < 4; ++j) *(u32x4*)(dst + 16 * ((4 * g + j) ^ S::swap(key))) = unpack8(next.v[i][j], sv);
+        CA_FENCE();
       }
-
-      // scores
-      Acc sc[SPT];
-#pragma unroll
-      for (int x = 0; x < SPT; ++x) {
-        sc[x] = Acc{};
-#pragma unroll
-        for (int s = 0; s < S::Steps; ++s) {
-          const int g = MT == 32 ? (NG % 2 == 0 || s < 4 * (NG / 2) ? 2 * (s / 4) + part : NG - 1)
-                                 : NG == 4 ? part : NG == 2 ? part / 2 : s;
-          const float ksv = scale_of((next.ks[x] >> (8 * g)) & 255u);
-          const bf16x8 kf = __builtin_bit_cast(bf16x8, unpack8(next.k[x][s], ksv));
-          if constexpr (MT == 32) sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[s], sc[x], 0, 0, 0);
-          else sc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[s], sc[x], 0, 0, 0);
-        }
-      }
-      next.load(a, next_id, h, lane, wr);
+      next.load_v(tile, lane, wr);
       next_id = page_id(pg + 2 * WK);
+      CA_FENCE();
 
       // keys that a row does not see
       if (!there || base + kPage > all_see) {
@@ -342,61 +387,64 @@ k_cache_attn(const CacheAttnArgs a) {
 #pragma unroll
       for (int x = 0; x < SPT; ++x)
 #pragma unroll
-        for (int i = 0; i < S::OR; ++i) top = fmaxf(top, sc[x][i]);
+        for (int i = 0; i < S::OR; i += 2) top = fmaxf(fmaxf(top, sc[x][i]), sc[x][i + 1]);
       top = max_row<MT>(top) * a.c;
       if (__any(top > ref + 8.0f)) {
         const float to = fmaxf(ref, top);
         const float f = __builtin_amdgcn_exp2f(ref - to);
         ref = to;
         l *= f;
+        l2 *= f;
 #pragma unroll
         for (int t = 0; t < S::DT; ++t)
 #pragma unroll
           for (int i = 0; i < S::OR; ++i) o[t][i] *= f;
       }
-      float sum = 0.0f;
-      uint32_t p[SPT][S::OR / 2];
-#pragma unroll
-      for (int x = 0; x < SPT; ++x)
-#pragma unroll
-        for (int i = 0; i < S::OR; i += 2) {
-          const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][i], a.c, -ref));
-          const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][i + 1], a.c, -ref));
-          sum += y + z;
-          p[x][i / 2] = pack_bf16(y, z);   // to 8 bits, as the values they meet
-        }
-      l += sum;
-
       if (WR > 1) __syncthreads();
       else __builtin_amdgcn_wave_barrier();
-      // a group of 16 lanes reads four keys by 16 elements, transposed
-      const int vrow = 4 * part + (lane % 16) / 4;
-      const int vpiece = (MT == 32 ? 2 * ((lane / 16) % 2) : 0) + (lane % 4) / 2;
-      const uint8_t* vp = lds + vrow * S::RowBytes + 8 * (lane % 2);
-      constexpr int KS = MT == 32 ? 4 : 2;   // steps of the second product
+
+      // outputs: the weights of a step of 16 (32) keys are formed beside the
+      // products of the one before; to 8 bits, as the values they meet
+      u32x4 p[2];
+      const auto weigh = [&](int k, int i) {   // pair i of step k
+        const int x = MT == 32 ? k / 2 : 2 * k + i / 2, at = MT == 32 ? 8 * (k % 2) + 2 * i : 2 * (i % 2);
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][at], a.c, -ref));
+        const float z = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][at + 1], a.c, -ref));
+        l += y;
+        l2 += z;
+        p[k % 2][i] = pack_bf16(y, z);
+      };
+      constexpr int KS = MT == 32 ? 4 : 2, NP = KS * S::DT;
+      const auto value_operand = [&](int i) {   // of product i: transposed reads, the second 8 (16) keys on
+        const int k = i / S::DT, t = i % S::DT;
+        const uint8_t* at = lds + k * (MT == 32 ? 16 : 32) * S::RowBytes;
+        const i16x4 v0 = read_transposed(at + v_at[t]);
+        const i16x4 v1 = read_transposed(at + (MT == 32 ? 8 * S::RowBytes + (v_at[t] ^ 16) : 16 * S::RowBytes + v_at[t]));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+      bf16x8 vf[3];
+      vf[0] = value_operand(0);
+      vf[1] = value_operand(1);
+      CA_FENCE();
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        u32x4 pk;
+      for (int i = 0; i < 4; ++i) weigh(0, i);
+      CA_FENCE();
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          pk[i] = MT == 32 ? p[k / 2][(4 * (k % 2) + i) % (S::OR / 2)] : p[(2 * k + i / 2) % SPT][i % 2];
-        const bf16x8 pf = __builtin_bit_cast(bf16x8, pk);
+      for (int i = 0; i < NP; ++i) {
+        const int k = i / S::DT, t = i % S::DT;
+        if (i + 2 < NP) vf[(i + 2) % 3] = value_operand(i + 2);
+        const bf16x8 pf = __builtin_bit_cast(bf16x8, p[k % 2]);
+        if constexpr (MT == 32) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % 3], pf, o[t], 0, 0, 0);
+        else o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i % 3], pf, o[t], 0, 0, 0);
+        CA_FENCE();
+        if (k + 1 < KS) {
 #pragma unroll
-        for (int t = 0; t < S::DT; ++t) {
-          // the second read's rows are 8 or 16 further on
-          const int piece = (vpiece + t * MT / 8) ^ S::swap(vrow);
-          const uint8_t* at = vp + k * (MT == 32 ? 16 : 32) * S::RowBytes;
-          const i16x4 v0 = read_transposed(at + 16 * piece);
-          const i16x4 v1 = MT == 32 ? read_transposed(at + 8 * S::RowBytes + 16 * (piece ^ 1))
-                                    : read_transposed(at + 16 * S::RowBytes + 16 * piece);
-          const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-          if constexpr (MT == 32) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[t], 0, 0, 0);
-          else o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[t], 0, 0, 0);
+          for (int w = t * 4 / S::DT; w < (t + 1) * 4 / S::DT; ++w) weigh(k + 1, w);
         }
+        CA_FENCE();
       }
-      __builtin_amdgcn_wave_barrier();
     }
-    l = sum_row<MT>(l);
+    l = sum_row<MT>(l + l2);
 
     // element of register i of tile t
     const auto d_of = [&](int t, int i) { return MT == 32 ? t * 32 + 2 * i + 4 * part : t * 16 + 4 * part; };
