@@ -33,6 +33,13 @@ constexpr int kCaMaxWaves = 8;
 // keeps instructions on their side: the order of the loop below is the one written
 #define CA_FENCE() __builtin_amdgcn_sched_barrier(0)
 
+// What an item costs beside its pages (its queries, the way to its first page,
+// its results), in pages: half as many units before its pages and half behind
+// stand for that, so that a share of many short items takes no longer than one
+// of a few long ones.  (Ragged spans of 1 to 4099 tokens, 24 blocks of 32
+// queries: 63 us at 0, 44 at 3 or 4.)
+constexpr int kItemEnds = 2, kItemUnits = 2 * kItemEnds;
+
 struct CacheAttnArgs {
   const uint16_t* q;
   long long q_stride;
@@ -56,6 +63,7 @@ struct CacheAttnArgs {
 // A sequence as the plan sees it: its query rows, pages and groups of rows.
 struct Seq {
   int first, n, len, groups, pages;
+  __device__ __forceinline__ int units(int Hk) const { return groups * Hk * (pages + kItemUnits); }
 };
 
 template <int Rows>
@@ -109,8 +117,7 @@ struct CaShape {
   static constexpr int OR = MT == 32 ? 16 : 4;             // registers of one
   static constexpr int SPT = kPage / MT;                   // subtiles of MT keys in a page
   static constexpr int Steps = MT == 32 ? 2 * NG : NG;     // steps of the first product
-  static constexpr int VPairs = kPage * NG;                // (key, group) pairs of a page's values
-  static constexpr int VPer = (VPairs + WR * kWave - 1) / (WR * kWave);   // of them a lane unpacks
+  static constexpr int VPer = (NG + WR - 1) / WR;          // groups of values a wave unpacks
 };
 
 // Where in a head's row the first product's operand of step s begins for a
@@ -130,53 +137,58 @@ __device__ __forceinline__ int element_of(int s, int part) {
   }
 }
 
-// Codes and scales of one page for one lane.
+// Codes and scales of one page for one lane: addresses are a uniform base and a
+// 32-bit offset of the lane's.
 template <int NG, int MT, int WR>
 struct PageRegs {
   typedef CaShape<NG, MT, WR> S;
   uint32_t k[S::SPT][S::Steps];   // eight codes a step
   uint32_t ks[S::SPT];            // scales of the lane's key of a subtile
-  u32x4 v[S::VPer];
-  uint32_t vs[S::VPer];
+  u32x4 v[S::VPer];               // 32 codes of the values of key `lane`, a group each
+  uint32_t vs;                    // and its scales
 
   __device__ __forceinline__ static const uint8_t* tile_of(const CacheAttnArgs& a, int page, int h) {
     const bool there = page >= 0 && page < a.n_pages;
     return a.cache + ((size_t)(there ? page : 0) * a.Hk + h) * tile_bytes(S::D);
   }
   __device__ __forceinline__ void load_k(const uint8_t* tile, int lane) {
-    const int col = lane % MT, part = lane / MT;
+    const uint32_t col = (uint32_t)lane % MT, part = (uint32_t)lane / MT;
+    constexpr uint32_t kGroupBytes = kPage * kCodeBytes;
 #pragma unroll
     for (int x = 0; x < S::SPT; ++x) {
-      const uint8_t* codes = tile + (x * MT + col) * kCodeBytes;
-      ks[x] = *(const uint32_t*)(tile + k_scales_at(S::D) + (x * MT + col) * scale_stride(S::D));
+      const uint8_t* codes = tile + x * MT * kCodeBytes;
+      ks[x] = *(const uint32_t*)(tile + k_scales_at(S::D) + x * MT * scale_stride(S::D) + col * scale_stride(S::D));
       if constexpr (MT == 32 || NG == 4) {
+        const uint32_t at = col * kCodeBytes + part * kGroupBytes;
 #pragma unroll
         for (int i = 0; i < S::Steps / 4; ++i) {
-          const u32x4 c = *(const u32x4*)(codes + (MT == 32 ? 2 * i + part : part) * kPage * kCodeBytes);
+          const u32x4 c = *(const u32x4*)(codes + i * 2 * kGroupBytes + at);
 #pragma unroll
           for (int j = 0; j < 4; ++j) k[x][4 * i + j] = c[j];
         }
         if constexpr (S::Steps % 4 != 0) {
-          const u32x2 c = *(const u32x2*)(codes + (NG - 1) * kPage * kCodeBytes + 8 * part);
+          const u32x2 c = *(const u32x2*)(codes + (NG - 1) * kGroupBytes + (col * kCodeBytes + 8 * part));
           k[x][S::Steps - 2] = c[0];
           k[x][S::Steps - 1] = c[1];
         }
       } else if constexpr (NG == 2) {
-        const u32x2 c = *(const u32x2*)(codes + (part / 2) * kPage * kCodeBytes + 8 * (part % 2));
+        const u32x2 c = *(const u32x2*)(codes + (col * kCodeBytes + (part / 2) * kGroupBytes + 8 * (part % 2)));
         k[x][0] = c[0];
         k[x][1] = c[1];
       } else {
 #pragma unroll
-        for (int s = 0; s < S::Steps; ++s) k[x][s] = *(const uint32_t*)(codes + s * kPage * kCodeBytes + 4 * part);
+        for (int s = 0; s < S::Steps; ++s)
+          k[x][s] = *(const uint32_t*)(codes + s * kGroupBytes + (col * kCodeBytes + 4 * part));
       }
     }
   }
   __device__ __forceinline__ void load_v(const uint8_t* tile, int lane, int wr) {
+    static_assert(kPage == kWave, "a lane a key");
+    vs = *(const uint32_t*)(tile + v_scales_at(S::D) + (uint32_t)lane * scale_stride(S::D));
 #pragma unroll
     for (int i = 0; i < S::VPer; ++i) {
-      const int w = min((i * WR + wr) * kWave + lane, S::VPairs - 1), key = w % kPage, g = w / kPage;
-      v[i] = *(const u32x4*)(tile + codes_bytes(S::D) + (g * kPage + key) * kCodeBytes);
-      vs[i] = tile[v_scales_at(S::D) + key * scale_stride(S::D) + g];
+      const int g = min(i * WR + wr, NG - 1);
+      v[i] = *(const u32x4*)(tile + codes_bytes(S::D) + g * kPage * kCodeBytes + (uint32_t)lane * kCodeBytes);
     }
   }
 };
@@ -209,8 +221,7 @@ k_cache_attn(const CacheAttnArgs a) {
   const int per = (a.B + S::Threads - 1) / S::Threads, b0 = tid * per, b1 = min(b0 + per, a.B);
   int mine = 0;
   for (int i = b0; i < b1; ++i) {
-    const Seq s = sequence<S::Rows>(a, i);
-    mine += s.groups * s.pages * a.Hk;
+    mine += sequence<S::Rows>(a, i).units(a.Hk);
   }
   int incl = mine;
 #pragma unroll
@@ -234,8 +245,7 @@ k_cache_attn(const CacheAttnArgs a) {
   if (u_begin >= incl - mine && u_begin < incl) {
     int i = b0, n = incl - mine;
     for (;; ++i) {
-      const Seq s = sequence<S::Rows>(a, i);
-      const int k = s.groups * s.pages * a.Hk;
+      const int k = sequence<S::Rows>(a, i).units(a.Hk);
       if (u_begin < n + k) break;
       n += k;
     }
@@ -260,16 +270,17 @@ k_cache_attn(const CacheAttnArgs a) {
   int slot = 0;                       // of the next partial result
   int buf = 0;                        // of values in LDS; goes on from item to item, so that one barrier a page will do
   while (u < u_end) {
-    while (u >= before + seq.groups * seq.pages * a.Hk) {
-      before += seq.groups * seq.pages * a.Hk;
+    while (u >= before + seq.units(a.Hk)) {
+      before += seq.units(a.Hk);
       seq = sequence<S::Rows>(a, ++b);
     }
-    const int item = (u - before) / seq.pages;
-    const int page0 = (u - before) % seq.pages;
-    const int page1 = min(seq.pages, page0 + (u_end - u));
+    const int each = seq.pages + kItemUnits, item = (u - before) / each;
+    const int at = u - before - item * each, upto = min(each, at + (u_end - u));
+    if (u == before && tid == 0) a.plan[1 + b] = before;   // for the join
+    u += upto - at;
+    const int page0 = max(0, at - kItemEnds), page1 = min(seq.pages, upto - kItemEnds);
+    if (page1 <= page0) continue;
     const int h = item % a.Hk, group = item / a.Hk;
-    u += page1 - page0;
-    if (item == 0 && page0 == 0 && tid == 0) a.plan[1 + b] = before;   // for the join
 
     // ---- the item's rows ----
     const int r = (group * WR + wr) * MT + col;             // row of this lane
@@ -281,16 +292,6 @@ k_cache_attn(const CacheAttnArgs a) {
 #pragma unroll
     for (int x = 1; x < MT; x <<= 1) all_see = min(all_see, __shfl_xor(all_see, x));
     all_see = __builtin_amdgcn_readfirstlane(all_see);
-    bf16x8 q[S::Steps];
-    {
-      const uint16_t* qrow = a.q + (size_t)(seq.first + tok) * a.q_stride + (size_t)head * D;
-#pragma unroll
-      for (int s = 0; s < S::Steps; ++s) {
-        q[s] = bf16x8{};
-        if (row_ok) q[s] = *(const bf16x8*)(qrow + element_of<NG, MT>(s, part));
-      }
-    }
-
     Acc o[S::DT];
 #pragma unroll
     for (int t = 0; t < S::DT; ++t) o[t] = Acc{};
@@ -323,6 +324,15 @@ k_cache_attn(const CacheAttnArgs a) {
     CA_FENCE();
     next.load_v(tile, lane, wr);   // after the keys here too: the loop waits for its loads in this order
     CA_FENCE();
+    bf16x8 q[S::Steps];
+    {
+      const uint16_t* qrow = a.q + (size_t)(seq.first + tok) * a.q_stride + (size_t)head * D;
+#pragma unroll
+      for (int s = 0; s < S::Steps; ++s) {
+        q[s] = bf16x8{};
+        if (row_ok) q[s] = *(const bf16x8*)(qrow + element_of<NG, MT>(s, part));
+      }
+    }
     // sets of waves without a page left go along while others' barriers run
     for (int pg = page0 + wk; WR == 1 ? pg < page1 : pg - wk < page1; pg += WK) {
       const int base = pg * kPage;
@@ -357,12 +367,12 @@ k_cache_attn(const CacheAttnArgs a) {
       // scale of next to nothing: their weight is 0, and a code is finite.
 #pragma unroll
       for (int i = 0; i < S::VPer; ++i) {
-        const int w = (i * WR + wr) * kWave + lane, key = w % kPage, g = w / kPage;
-        if (S::VPairs % (WR * kWave) != 0 && w >= S::VPairs) break;
-        const float sv = scale_of(there && base + key < seq.len ? next.vs[i] : 1u);
-        uint8_t* dst = lds + key * S::RowBytes;
+        const int g = i * WR + wr;
+        if (NG % WR != 0 && g >= NG) break;
+        const float sv = scale_of(there && base + lane < seq.len ? (next.vs >> (8 * g)) & 255u : 1u);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) *(u32x4*)(dst + 16 * ((4 * g + j) ^ S::swap(key))) = unpack8(next.v[i][j], sv);
+        for (int j = 0; j < 4; ++j)
+          *(u32x4*)(lds + lane * S::RowBytes + 16 * ((4 * g + j) ^ S::swap(lane))) = unpack8(next.v[i][j], sv);
         CA_FENCE();
       }
       next.load_v(tile, lane, wr);
@@ -537,13 +547,13 @@ k_cache_join(const CacheAttnArgs a, int wgs) {
   const int x0 = (blockIdx.x % Blocks) * RowsHere;
   if (group * Rows + x0 >= seq.n * a.R) return;
   const Shares shares(a.plan[0], wgs);
-  const int u0 = a.plan[1 + b] + item * seq.pages;
-  const int g0 = shares.of(u0), g1 = shares.of(u0 + seq.pages - 1);
+  const int u0 = a.plan[1 + b] + item * (seq.pages + kItemUnits);
+  const int g0 = shares.of(u0 + kItemEnds), g1 = shares.of(u0 + kItemEnds + seq.pages - 1);
   if (g0 == g1) return;
   const int lane = threadIdx.x % Lanes, xr = threadIdx.x / Lanes % RowsHere, sp = threadIdx.x / Lanes / RowsHere;
   const int x = x0 + xr;
-  // an item that begins inside a share is that workgroup's second result
-  const int first = (g0 * 2 + (shares.begin(g0) < u0 ? 1 : 0)) * Rows + x;
+  // it is its first share's second result where that holds pages of the item before
+  const int first = (g0 * 2 + (shares.begin(g0) < u0 - kItemEnds ? 1 : 0)) * Rows + x;
   const auto row_of = [&](int g) { return g == g0 ? first : g * 2 * Rows + x; };
   float acc[2 * NG], l = 0.0f, ref = kRefFloor;
 #pragma unroll
@@ -634,7 +644,7 @@ static bool ca_sizes_ok(int B, int H, int Hk, int D, int max_q, int table_w, int
   const long long groups = (rows + 15) / 16;
   if (rows > (1 << 24) || groups * Hk > INT32_MAX / 2) return false;
   // units of work are counted in 32 bits
-  const double units = (double)B * (table_w > 1 ? table_w : 1) * (double)groups * Hk;
+  const double units = (double)B * (table_w + 1.0 + kItemUnits) * (double)groups * Hk;
   return units < 2.0e9;
 }
 
