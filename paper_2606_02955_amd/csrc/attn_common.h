@@ -109,6 +109,29 @@ __device__ __forceinline__ i16x4 read_transposed(const uint8_t* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
 }
 
+// ---------------------------------------------------------------------------
+// outputs.  A wave's tile of MT rows by D lies transposed in its registers: lane
+// (col, part) holds row col, and quad q of its registers the four elements from
+// quad_element on.  Partial sums are stored as they lie, a quad of all lanes at
+// a time: [tile][quads][64 lanes][4].
+// ---------------------------------------------------------------------------
+template <int MT>
+__device__ __forceinline__ int quad_element(int q, int part) {
+  return MT == 32 ? (q / 4) * 32 + (q % 4) * 8 + 4 * part : q * 16 + 4 * part;
+}
+__host__ __device__ constexpr int quads_of(int MT, int NG) { return MT == 32 ? 4 * NG : 2 * NG; }
+
+// Rows of bfloat16 in LDS on their way out, 16-byte pieces exchanged by the
+// row's number, so that 16 lanes that hold an element of 16 rows meet all banks.
+template <int NG>
+struct OutRows {
+  static constexpr int RowBytes = NG == 2 ? 128 : 256;
+  __device__ static int at(int row, int d) {
+    const int swap = NG == 2 ? row / 2 % 8 : row % 16;
+    return row * RowBytes + 16 * ((d / 8) ^ swap) + 2 * (d % 8);
+  }
+};
+
 constexpr float kLn2 = 0.69314718055994530942f;
 
 }  // namespace fdllm

@@ -56,8 +56,8 @@ struct CacheAttnArgs {
   uint16_t* out;
   float* lse;
   int32_t* plan;              // units of all sequences, then those before each
-  float* part_ml;             // [workgroups][2][rows][2]: reference and sum of a partial result
-  float* part;                // [workgroups][2][rows][D]
+  float* part_ml;             // [workgroups][2][WR][MT][2]: reference and sum of a row's partial result
+  float* part;                // [workgroups][2][WR] tiles of partial sums (attn_common.h)
 };
 
 // A sequence as the plan sees it: its query rows, pages and groups of rows.
@@ -111,7 +111,13 @@ struct CaShape {
   static constexpr int PageBytes = kPage * RowBytes;
   static constexpr int Buffers = WR > 1 ? 2 : 1;
   static constexpr int ValueBytes = WK * Buffers * PageBytes;
-  static constexpr int JoinBytes = WK > 1 ? (WK / 2) * Rows * (D + 4) * 4 : 0;
+  // Sums of a wave's rows on their way to be added to others': 16-byte pieces,
+  // exchanged by the row's number as above.
+  static constexpr int JoinRow = NG == 2 ? 256 : 512;
+  __device__ static int join_at(int wave, int row, int d) {
+    return (wave * MT + row) * JoinRow + 16 * ((d / 4) ^ (row % 16));
+  }
+  static constexpr int JoinBytes = WK > 1 ? Waves * MT * JoinRow : 4 * MT * OutRows<NG>::RowBytes;
   static constexpr int LdsBytes = ValueBytes > JoinBytes ? ValueBytes : JoinBytes;
   static constexpr int DT = MT == 32 ? NG : 2 * NG;        // tiles of D of the second product
   static constexpr int OR = MT == 32 ? 16 : 4;             // registers of one
@@ -217,43 +223,55 @@ k_cache_attn(const CacheAttnArgs a) {
   const int col = lane % MT, part = lane / MT;
 
   // Units of all sequences, this workgroup's share of them, and the sequence of
-  // its first: a thread counts a few neighbouring sequences, a scan adds up.
-  const int per = (a.B + S::Threads - 1) / S::Threads, b0 = tid * per, b1 = min(b0 + per, a.B);
+  // its first: a lane (of all waves, from 65 sequences on) counts a few
+  // neighbouring sequences, a scan adds up.
+  const bool apart = a.B <= kWave;   // every wave by itself
+  const int who = apart ? lane : tid, per = apart ? 1 : (a.B + S::Threads - 1) / S::Threads;
+  const int b0 = who * per, b1 = min(b0 + per, a.B);
   int mine = 0;
-  for (int i = b0; i < b1; ++i) {
-    mine += sequence<S::Rows>(a, i).units(a.Hk);
-  }
+  for (int i = b0; i < b1; ++i) mine += sequence<S::Rows>(a, i).units(a.Hk);
   int incl = mine;
 #pragma unroll
   for (int x = 1; x < kWave; x <<= 1) {
     const int y = __shfl_up(incl, x);
     if (lane >= x) incl += y;
   }
-  if (lane == kWave - 1) s_sum[wave] = incl;
-  __syncthreads();
-  int units = 0;
+  int units = __builtin_amdgcn_readlane(incl, kWave - 1);
+  if (!apart) {
+    if (lane == kWave - 1) s_sum[wave] = incl;
+    __syncthreads();
+    units = 0;
 #pragma unroll
-  for (int w = 0; w < S::Waves; ++w) {
-    if (w == wave) incl += units;
-    units += s_sum[w];
+    for (int w = 0; w < S::Waves; ++w) {
+      if (w == wave) incl += units;
+      units += s_sum[w];
+    }
   }
   if (units == 0) return;
   const Shares shares(units, gridDim.x);
   const int u_begin = shares.begin(blockIdx.x), u_end = shares.begin(blockIdx.x + 1);
   if (blockIdx.x == 0 && tid == 0) a.plan[0] = units;
   if (u_begin >= u_end) return;
-  if (u_begin >= incl - mine && u_begin < incl) {
-    int i = b0, n = incl - mine;
-    for (;; ++i) {
-      const int k = sequence<S::Rows>(a, i).units(a.Hk);
-      if (u_begin < n + k) break;
-      n += k;
+  int b, before;
+  const bool here = u_begin >= incl - mine && u_begin < incl;
+  if (apart) {
+    b = __ffsll((unsigned long long)__ballot(here)) - 1;
+    before = __builtin_amdgcn_readlane(incl - mine, b);
+  } else {
+    if (here) {
+      int i = b0, n = incl - mine;
+      for (;; ++i) {
+        const int k = sequence<S::Rows>(a, i).units(a.Hk);
+        if (u_begin < n + k) break;
+        n += k;
+      }
+      s_at[0] = i;
+      s_at[1] = n;
     }
-    s_at[0] = i;
-    s_at[1] = n;
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(s_at[0]);
+    before = __builtin_amdgcn_readfirstlane(s_at[1]);
   }
-  __syncthreads();
-  int b = __builtin_amdgcn_readfirstlane(s_at[0]), before = __builtin_amdgcn_readfirstlane(s_at[1]);
   Seq seq = sequence<S::Rows>(a, b);
 
   // Where a lane reads its part of a page's values: a group of 16 lanes reads
@@ -456,173 +474,205 @@ k_cache_attn(const CacheAttnArgs a) {
     }
     l = sum_row<MT>(l + l2);
 
-    // element of register i of tile t
-    const auto d_of = [&](int t, int i) { return MT == 32 ? t * 32 + 2 * i + 4 * part : t * 16 + 4 * part; };
-
-    // ---- the sets of waves join, two by two ----
+    // ---- results: final where the item is whole, a partial sum otherwise ----
+    const bool whole = page0 == 0 && page1 == seq.pages;
+    const size_t tile0 = ((size_t)blockIdx.x * 2 + slot) * WR;   // of partial results
+    constexpr int Quads = quads_of(MT, NG);
     if constexpr (WK > 1) {
+      // the sets of waves join: every row's sums brought to one reference, added
+      // up out of LDS
+      if (part == 0) s_ml[wave][col][0] = ref, s_ml[wave][col][1] = l;
+      __syncthreads();
+      float to = ref;
 #pragma unroll
-      for (int n = WK / 2; n >= 1; n /= 2) {
-        __syncthreads();
-        float* mem = (float*)s_mem;
-        if (wk >= n && wk < 2 * n) {
-          float* mine = mem + ((wk - n) * WR + wr) * MT * (D + 4);
-          if (part == 0) s_ml[wave][col][0] = ref, s_ml[wave][col][1] = l;
+      for (int w = 0; w < WK; ++w) to = fmaxf(to, s_ml[w * WR + wr][col][0]);
+      const float f = __builtin_amdgcn_exp2f(ref - to);
 #pragma unroll
-          for (int t = 0; t < S::DT; ++t)
+      for (int q = 0; q < Quads; ++q) {
+        const int i = 4 * q % S::OR, t = 4 * q / S::OR;
+        *(f32x4*)(s_mem + S::join_at(wave, col, quad_element<MT>(q, part))) =
+            f32x4{o[t][i] * f, o[t][i + 1] * f, o[t][i + 2] * f, o[t][i + 3] * f};
+      }
+      __syncthreads();
+      const auto joined = [&](int w0, int row, int d) {
+        f32x4 v = *(const f32x4*)(s_mem + S::join_at(w0, row, d));
 #pragma unroll
-            for (int i = 0; i < S::OR; i += 4)
-              *(f32x4*)(mine + col * (D + 4) + d_of(t, i)) = f32x4{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+        for (int w = 1; w < WK; ++w) v += *(const f32x4*)(s_mem + S::join_at(w * WR + w0, row, d));
+        return v;
+      };
+      const auto joined_ml = [&](int w0, int row) {
+        float m = kRefFloor, n = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WK; ++w) m = fmaxf(m, s_ml[w * WR + w0][row][0]);
+#pragma unroll
+        for (int w = 0; w < WK; ++w)
+          n += s_ml[w * WR + w0][row][1] * __builtin_amdgcn_exp2f(s_ml[w * WR + w0][row][0] - m);
+        return float2{m, n};
+      };
+      if (whole) {
+        for (int x = tid; x < S::Rows * (D / 4); x += S::Threads) {
+          const int row = x / (D / 4), d = 4 * (x % (D / 4)), rr = group * S::Rows + row;
+          if (rr >= seq.n * a.R) break;
+          const f32x4 v = joined(row / MT, row % MT, d);
+          const float2 ml = joined_ml(row / MT, row % MT);
+          const float inv = ml.y > 0.0f ? 1.0f / ml.y : 0.0f;
+          const size_t to_row = (size_t)(seq.first + rr / a.R) * a.H + h * a.R + rr % a.R;
+          *(u32x2*)(a.out + to_row * D + d) = u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
+          if (a.lse && d == 0) a.lse[to_row] = ml.y > 0.0f ? (ml.x + __builtin_amdgcn_logf(ml.y)) * kLn2 : kNegInf;
         }
-        __syncthreads();
-        if (wk < n) {
-          const int other = (wk + n) * WR + wr;
-          const float* theirs = mem + (wk * WR + wr) * MT * (D + 4);
-          const float ref2 = s_ml[other][col][0], l2 = s_ml[other][col][1];
-          const float to = fmaxf(ref, ref2);
-          const float f1 = __builtin_amdgcn_exp2f(ref - to), f2 = __builtin_amdgcn_exp2f(ref2 - to);
-          ref = to;
-          l = l * f1 + l2 * f2;
-#pragma unroll
-          for (int t = 0; t < S::DT; ++t)
-#pragma unroll
-            for (int i = 0; i < S::OR; i += 4) {
-              const f32x4 x = *(const f32x4*)(theirs + col * (D + 4) + d_of(t, i));
-#pragma unroll
-              for (int k = 0; k < 4; ++k) o[t][i + k] = o[t][i + k] * f1 + x[k] * f2;
-            }
+      } else {
+        for (int x = wave; x < WR * Quads; x += S::Waves) {
+          const int w0 = x / Quads, q = x % Quads;
+          *(f32x4*)(a.part + ((tile0 * Quads + x) * kWave + lane) * 4) = joined(w0, col, quad_element<MT>(q, part));
+          if (q == 0 && part == 0) *(float2*)(a.part_ml + ((tile0 + w0) * MT + col) * 2) = joined_ml(w0, col);
         }
       }
       __syncthreads();
-    }
-
-    // ---- results: final where the item is whole, a partial sum otherwise ----
-    if (wk == 0) {
-      if (page0 == 0 && page1 == seq.pages) {
-        if (row_ok) {
-          const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-          const size_t at = (size_t)(seq.first + tok) * a.H + head;
+    } else if (whole) {
+      // through LDS, so that a row leaves in one piece
+      __syncthreads();
+      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+      uint8_t* lds = s_mem + wave * MT * OutRows<NG>::RowBytes;
 #pragma unroll
-          for (int t = 0; t < S::DT; ++t)
-#pragma unroll
-            for (int i = 0; i < S::OR; i += 4)
-              *(u32x2*)(a.out + at * D + d_of(t, i)) = u32x2{pack_bf16(o[t][i] * inv, o[t][i + 1] * inv),
-                                                             pack_bf16(o[t][i + 2] * inv, o[t][i + 3] * inv)};
-          if (a.lse && part == 0) a.lse[at] = l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
-        }
-      } else {
-        const size_t row = ((size_t)blockIdx.x * 2 + slot) * S::Rows + wr * MT + col;
-#pragma unroll
-        for (int t = 0; t < S::DT; ++t)
-#pragma unroll
-          for (int i = 0; i < S::OR; i += 4)
-            *(f32x4*)(a.part + row * D + d_of(t, i)) = f32x4{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
-        if (part == 0) *(float2*)(a.part_ml + row * 2) = float2{ref, l};
+      for (int q = 0; q < Quads; ++q) {
+        const int i = 4 * q % S::OR, t = 4 * q / S::OR;
+        *(u32x2*)(lds + OutRows<NG>::at(col, quad_element<MT>(q, part))) =
+            u32x2{pack_bf16(o[t][i] * inv, o[t][i + 1] * inv), pack_bf16(o[t][i + 2] * inv, o[t][i + 3] * inv)};
       }
+      __builtin_amdgcn_wave_barrier();
+      const size_t at = (size_t)(seq.first + tok) * a.H + head;
+      if (row_ok && a.lse && part == 0) a.lse[at] = l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+      for (int x = lane; x < MT * (D / 8); x += kWave) {
+        const int row = x / (D / 8), d = 8 * (x % (D / 8)), rr = (group * WR + wr) * MT + row;
+        if (rr >= seq.n * a.R) break;
+        const size_t to_row = (size_t)(seq.first + rr / a.R) * a.H + h * a.R + rr % a.R;
+        *(u32x4*)(a.out + to_row * D + d) = *(const u32x4*)(lds + OutRows<NG>::at(row, d));
+      }
+      __syncthreads();
+    } else {
+#pragma unroll
+      for (int q = 0; q < Quads; ++q) {
+        const int i = 4 * q % S::OR, t = 4 * q / S::OR;
+        *(f32x4*)(a.part + (((tile0 + wr) * Quads + q) * kWave + lane) * 4) =
+            f32x4{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+      }
+      if (part == 0) *(float2*)(a.part_ml + ((tile0 + wr) * MT + col) * 2) = float2{ref, l};
     }
     slot = 1;
   }
 }
 
 // Joins the partial results of an item that several workgroups share, always
-// in the same order.  16 lanes take a row.  Where items lie in many shares, the
-// Split sixteenths of a workgroup's waves divide the parts of a row (what a part
-// costs is a round trip to memory, so as many as possible are under way at
-// once); where they lie in two or so, every 16 lanes have a row of their own.
-constexpr int kCaJoinThreads = 256;
+// in the same order.  A workgroup takes the MT rows of a wave's tile, as they
+// lay in its registers.  Where items lie in many shares, Split sets of its
+// waves divide the parts (a part costs a round trip to memory, so as many as
+// possible are under way at once); where they lie in two or so, every wave has
+// quads of its own.
+constexpr int kCaJoinWaves = 8;
 
-template <int NG, int Rows, int Split>
-__global__ void __launch_bounds__(kCaJoinThreads)
+template <int NG, int MT, int WR, int Split>
+__global__ void __launch_bounds__(kCaJoinWaves* kWave)
 k_cache_join(const CacheAttnArgs a, int wgs) {
-  constexpr int D = NG * kGroup, Lanes = 16;
-  constexpr int RowsHere = kCaJoinThreads / Lanes / Split;
-  constexpr int Blocks = Rows / RowsHere;   // of a group of rows
-  __shared__ float s_acc[Split > 1 ? Split : 1][RowsHere][Split > 1 ? D : 1];
-  __shared__ float s_ml[Split][RowsHere][2];
+  constexpr int D = NG * kGroup, Quads = quads_of(MT, NG), Rows = MT * WR;
+  constexpr int Sets = kCaJoinWaves / Split;              // of waves, by quads
+  constexpr int QPer = (Quads + Sets - 1) / Sets;
+  __shared__ __align__(16) uint8_t s_out[MT * OutRows<NG>::RowBytes];
+  __shared__ f32x4 s_acc[Split > 1 ? Sets * (Split - 1) : 1][QPer][kWave];
+  __shared__ float s_ml[kCaJoinWaves][MT][2];
   const int b = blockIdx.y;
-  const int item = blockIdx.x / Blocks;
+  const int item = blockIdx.x / WR, wr = blockIdx.x % WR;
   const Seq seq = sequence<Rows>(a, b);
   if (item >= seq.groups * a.Hk) return;
   const int h = item % a.Hk, group = item / a.Hk;
-  const int x0 = (blockIdx.x % Blocks) * RowsHere;
-  if (group * Rows + x0 >= seq.n * a.R) return;
+  const int r0 = (group * WR + wr) * MT;                  // the tile's first row
+  if (r0 >= seq.n * a.R) return;
   const Shares shares(a.plan[0], wgs);
   const int u0 = a.plan[1 + b] + item * (seq.pages + kItemUnits);
   const int g0 = shares.of(u0 + kItemEnds), g1 = shares.of(u0 + kItemEnds + seq.pages - 1);
   if (g0 == g1) return;
-  const int lane = threadIdx.x % Lanes, xr = threadIdx.x / Lanes % RowsHere, sp = threadIdx.x / Lanes / RowsHere;
-  const int x = x0 + xr;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int col = lane % MT, part = lane / MT;
+  const int sp = wave % Split, set = wave / Split;
   // it is its first share's second result where that holds pages of the item before
-  const int first = (g0 * 2 + (shares.begin(g0) < u0 - kItemEnds ? 1 : 0)) * Rows + x;
-  const auto row_of = [&](int g) { return g == g0 ? first : g * 2 * Rows + x; };
-  float acc[2 * NG], l = 0.0f, ref = kRefFloor;
+  const int first = (g0 * 2 + (shares.begin(g0) < u0 - kItemEnds ? 1 : 0)) * WR + wr;
+  const auto tile_of = [&](int g) { return (size_t)(g == g0 ? first : g * 2 * WR + wr); };
+  f32x4 acc[QPer];
 #pragma unroll
-  for (int i = 0; i < 2 * NG; ++i) acc[i] = 0.0f;
-  for (int c = g0 + sp * Lanes; c <= g1; c += Split * Lanes) {
-    // a lane each for the references and sums of 16 parts
-    const int n = min(Lanes, g1 + 1 - c);
-    const int row = row_of(lane < n ? c + lane : g0);
-    const float2 ml = *(const float2*)(a.part_ml + (size_t)row * 2);
-    float to = lane < n ? fmaxf(ref, ml.x) : ref;
+  for (int i = 0; i < QPer; ++i) acc[i] = f32x4{};
+  float ref = kRefFloor, l = 0.0f;
+  constexpr int Ahead = 4;
+  for (int g = g0 + sp * Ahead; g <= g1; g += Split * Ahead) {
+    float2 ml[Ahead];
+    f32x4 v[Ahead][QPer];
 #pragma unroll
-    for (int s = 1; s < Lanes; s <<= 1) to = fmaxf(to, __shfl_xor(to, s));
-    const float f0 = __builtin_amdgcn_exp2f(ref - to);
-    ref = to;
-    const float f = lane < n ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.0f;
-    l = l * f0 + f * ml.y;     // of this lane's parts
+    for (int k = 0; k < Ahead; ++k) {
+      const size_t tile = tile_of(min(g + k, g1));
+      ml[k] = *(const float2*)(a.part_ml + (tile * MT + col) * 2);
 #pragma unroll
-    for (int i = 0; i < 2 * NG; ++i) acc[i] *= f0;
-#pragma unroll 8
-    for (int k = 0; k < n; ++k) {
-      const float fk = __shfl(f, k, Lanes);
-      const float* src = a.part + (size_t)row_of(c + k) * D + 2 * lane;
-#pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const float2 v = *(const float2*)(src + 32 * i);
-        acc[2 * i] += fk * v.x;
-        acc[2 * i + 1] += fk * v.y;
-      }
+      for (int i = 0; i < QPer; ++i)
+        v[k][i] = *(const f32x4*)(a.part + ((tile * Quads + min(set * QPer + i, Quads - 1)) * kWave + lane) * 4);
     }
-  }
-#pragma unroll
-  for (int s = 1; s < Lanes; s <<= 1) l += __shfl_xor(l, s);
-  if constexpr (Split > 1) {
-    if (sp > 0) {
-#pragma unroll
-      for (int i = 0; i < NG; ++i) *(float2*)&s_acc[sp][xr][32 * i + 2 * lane] = float2{acc[2 * i], acc[2 * i + 1]};
-      if (lane == 0) s_ml[sp][xr][0] = ref, s_ml[sp][xr][1] = l;
-    }
-    __syncthreads();
-    if (sp > 0) return;
     float to = ref;
 #pragma unroll
-    for (int w = 1; w < Split; ++w) to = fmaxf(to, s_ml[w][xr][0]);
+    for (int k = 0; k < Ahead; ++k) to = fmaxf(to, ml[k].x);
     const float f0 = __builtin_amdgcn_exp2f(ref - to);
     ref = to;
     l *= f0;
 #pragma unroll
-    for (int i = 0; i < 2 * NG; ++i) acc[i] *= f0;
+    for (int i = 0; i < QPer; ++i) acc[i] *= f0;
 #pragma unroll
-    for (int w = 1; w < Split; ++w) {
-      const float f = __builtin_amdgcn_exp2f(s_ml[w][xr][0] - ref);
-      l += f * s_ml[w][xr][1];
+    for (int k = 0; k < Ahead; ++k) {
+      const float f = g + k <= g1 ? __builtin_amdgcn_exp2f(ml[k].x - ref) : 0.0f;
+      l += f * ml[k].y;
 #pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const float2 v = *(const float2*)&s_acc[w][xr][32 * i + 2 * lane];
-        acc[2 * i] += f * v.x;
-        acc[2 * i + 1] += f * v.y;
-      }
+      for (int i = 0; i < QPer; ++i) acc[i] += v[k][i] * f;
     }
   }
-  const int r = group * Rows + x;
-  if (r >= seq.n * a.R) return;
-  const int tok = r / a.R, head = h * a.R + r % a.R;
-  const size_t at = (size_t)(seq.first + tok) * a.H + head;
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  if constexpr (Split > 1) {
+    if (part == 0) s_ml[wave][col][0] = ref, s_ml[wave][col][1] = l;
+    if (sp > 0) {
 #pragma unroll
-  for (int i = 0; i < NG; ++i)
-    *(uint32_t*)(a.out + at * D + 32 * i + 2 * lane) = pack_bf16(acc[2 * i] * inv, acc[2 * i + 1] * inv);
-  if (a.lse && lane == 0) a.lse[at] = l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+      for (int i = 0; i < QPer; ++i) s_acc[set * (Split - 1) + sp - 1][i][lane] = acc[i];
+    }
+    __syncthreads();
+    float to = kRefFloor;
+#pragma unroll
+    for (int w = 0; w < Split; ++w) to = fmaxf(to, s_ml[set * Split + w][col][0]);
+    const float f0 = __builtin_amdgcn_exp2f(ref - to);
+    l *= f0;
+#pragma unroll
+    for (int i = 0; i < QPer; ++i) acc[i] *= f0;
+#pragma unroll
+    for (int w = 1; w < Split; ++w) {   // (of use to the first wave of a set)
+      const float f = __builtin_amdgcn_exp2f(s_ml[set * Split + w][col][0] - to);
+      l += f * s_ml[set * Split + w][col][1];
+#pragma unroll
+      for (int i = 0; i < QPer; ++i) acc[i] += s_acc[set * (Split - 1) + w - 1][i][lane] * f;
+    }
+    ref = to;
+  }
+  // out through LDS, so that a row leaves in one piece
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  if (sp == 0) {
+#pragma unroll
+    for (int i = 0; i < QPer; ++i) {
+      const int q = set * QPer + i;
+      if (q < Quads)
+        *(u32x2*)(s_out + OutRows<NG>::at(col, quad_element<MT>(q, part))) =
+            u32x2{pack_bf16(acc[i][0] * inv, acc[i][1] * inv), pack_bf16(acc[i][2] * inv, acc[i][3] * inv)};
+    }
+    const int r = r0 + col;
+    if (set == 0 && part == 0 && a.lse && r < seq.n * a.R)
+      a.lse[(size_t)(seq.first + r / a.R) * a.H + h * a.R + r % a.R] =
+          l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < MT * (D / 8); x += kCaJoinWaves * kWave) {
+    const int row = x / (D / 8), d = 8 * (x % (D / 8)), r = r0 + row;
+    if (r >= seq.n * a.R) break;
+    const size_t at = (size_t)(seq.first + r / a.R) * a.H + h * a.R + r % a.R;
+    *(u32x4*)(a.out + at * D + d) = *(const u32x4*)(s_out + OutRows<NG>::at(row, d));
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -689,12 +739,9 @@ static hipError_t ca_launch_one(const CacheAttnArgs& a, const CaPlan& p, hipStre
     if (dev >= 0 && dev < kCaMaxDevices) allowed[dev].store(true, std::memory_order_release);
   }
   hipLaunchKernelGGL((k_cache_attn<NG, MT, WR>), dim3((unsigned)p.wgs), dim3(S::Threads), S::LdsBytes, st, a);
-  if (p.join && p.split)
-    hipLaunchKernelGGL((k_cache_join<NG, S::Rows, 4>), dim3((unsigned)(p.items * (S::Rows / 4)), (unsigned)a.B),
-                       dim3(kCaJoinThreads), 0, st, a, p.wgs);
-  else if (p.join)
-    hipLaunchKernelGGL((k_cache_join<NG, S::Rows, 1>), dim3((unsigned)(p.items * (S::Rows / 16)), (unsigned)a.B),
-                       dim3(kCaJoinThreads), 0, st, a, p.wgs);
+  const dim3 join((unsigned)(p.items * WR), (unsigned)a.B), threads(kCaJoinWaves * kWave);
+  if (p.join && p.split) hipLaunchKernelGGL((k_cache_join<NG, MT, WR, 4>), join, threads, 0, st, a, p.wgs);
+  else if (p.join) hipLaunchKernelGGL((k_cache_join<NG, MT, WR, 1>), join, threads, 0, st, a, p.wgs);
   return hipGetLastError();
 }
 

@@ -37,8 +37,8 @@ struct PromptArgs {
   uint16_t* out;
   float* lse;
   int tiles, splits;   // row tiles of max_q tokens; workgroups for the keys of one
-  float* part_ml;      // [(b, h), tile, split][rows][2]: reference and sum of a partial result
-  float* part;         // [(b, h), tile, split][rows][D]
+  float* part_ml;      // [(b, h), tile, split, wave][32][2]: reference and sum of a row's partial result
+  float* part;         // [(b, h), tile, split, wave] tiles of partial sums (attn_common.h)
 };
 
 // A tile of rows: 128 of a sequence's query tokens times the heads of a key head.
@@ -333,67 +333,103 @@ k_prompt_attn(const PromptArgs a) {
   }
   l = sum_halves(l + l2);
 
+  constexpr int Quads = quads_of(32, NG);
   if (pt.parts == 1) {
-    if (!row_ok) return;
+    // through LDS (where the keys were: nobody reads them any more), so that a
+    // row leaves in one piece
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    const size_t at = (size_t)(pt.first + tok) * a.H + head;
+    uint8_t* lds = s_mem + wave * 32 * OutRows<NG>::RowBytes;
 #pragma unroll
-    for (int t = 0; t < NG; ++t)
+    for (int q = 0; q < Quads; ++q) {
+      const int x = q / 4, i = 4 * (q % 4);
+      *(u32x2*)(lds + OutRows<NG>::at(col, quad_element<32>(q, part))) =
+          u32x2{pack_bf16(o[x][i] * inv, o[x][i + 1] * inv), pack_bf16(o[x][i + 2] * inv, o[x][i + 3] * inv)};
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (row_ok && a.lse && part == 0)
+      a.lse[(size_t)(pt.first + tok) * a.H + head] = l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *(u32x2*)(a.out + at * D + t * 32 + 2 * i + 4 * part) =
-            u32x2{pack_bf16(o[t][i] * inv, o[t][i + 1] * inv), pack_bf16(o[t][i + 2] * inv, o[t][i + 3] * inv)};
-    if (a.lse && part == 0) a.lse[at] = l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+    for (int j = 0; j < 32 * (D / 8) / kWave; ++j) {
+      const int x = j * kWave + lane, row = x / (D / 8), d = 8 * (x % (D / 8)), rr = tile * kPaRows + wave * 32 + row;
+      if (rr < pt.rows) {
+        const size_t at = (size_t)(pt.first + rr / a.R) * a.H + h * a.R + rr % a.R;
+        *(u32x4*)(a.out + at * D + d) = *(const u32x4*)(lds + OutRows<NG>::at(row, d));
+      }
+    }
   } else {
-    const size_t row =
-        (((size_t)blockIdx.x * a.tiles + tile) * a.splits + blockIdx.z) * kPaRows + wave * 32 + col;
+    const size_t part_tile = (((size_t)blockIdx.x * a.tiles + tile) * a.splits + blockIdx.z) * kPaWaves + wave;
 #pragma unroll
-    for (int t = 0; t < NG; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *(f32x4*)(a.part + row * D + t * 32 + 2 * i + 4 * part) = f32x4{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
-    if (part == 0) *(float2*)(a.part_ml + row * 2) = float2{ref, l};
+    for (int q = 0; q < Quads; ++q) {
+      const int x = q / 4, i = 4 * (q % 4);
+      *(f32x4*)(a.part + ((part_tile * Quads + q) * kWave + lane) * 4) =
+          f32x4{o[x][i], o[x][i + 1], o[x][i + 2], o[x][i + 3]};
+    }
+    if (part == 0) *(float2*)(a.part_ml + (part_tile * 32 + col) * 2) = float2{ref, l};
   }
 }
 
-// Joins the parts of a row tile in the order of their keys: 16 rows a
-// workgroup, 16 lanes a row.
+// Joins the parts of a row tile in the order of their keys: a workgroup for the
+// 32 rows of a wave, as they lay in its registers, a few quads a wave.
 template <int NG>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kPaThreads)
 k_prompt_join(const PromptArgs a) {
-  constexpr int D = NG * 32, Groups = kPaRows / 16;
+  constexpr int D = NG * 32, Quads = quads_of(32, NG), QPer = Quads / kPaWaves;
+  __shared__ __align__(16) uint8_t s_out[32 * OutRows<NG>::RowBytes];
   const int b = blockIdx.x / a.Hk, h = blockIdx.x % a.Hk;
-  const int tile = blockIdx.y / Groups;
-  const int x = (blockIdx.y % Groups) * 16 + threadIdx.x / 16, lane = threadIdx.x % 16;
+  const int tile = blockIdx.y / kPaWaves, wr = blockIdx.y % kPaWaves;
   const PaTile pt = pa_tile(a, b, tile);
-  const int r = tile * kPaRows + x;
-  if (r >= pt.rows || pt.parts == 1) return;
-  const size_t row = (((size_t)blockIdx.x * a.tiles + tile) * a.splits) * kPaRows + x;
-  float ref = kRefFloor;
-  for (int z = 0; z < pt.parts; ++z) ref = fmaxf(ref, a.part_ml[(row + (size_t)z * kPaRows) * 2]);
-  float acc[2 * NG], l = 0.0f;
+  const int r0 = tile * kPaRows + wr * 32;
+  if (r0 >= pt.rows || pt.parts == 1) return;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int col = lane % 32, part = lane / 32;
+  const size_t first = (((size_t)blockIdx.x * a.tiles + tile) * a.splits) * kPaWaves + wr;
+  f32x4 acc[QPer];
 #pragma unroll
-  for (int i = 0; i < 2 * NG; ++i) acc[i] = 0.0f;
-#pragma unroll 4
-  for (int z = 0; z < pt.parts; ++z) {
-    const size_t at = row + (size_t)z * kPaRows;
-    const float2 ml = *(const float2*)(a.part_ml + at * 2);
-    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-    l += f * ml.y;
+  for (int i = 0; i < QPer; ++i) acc[i] = f32x4{};
+  float ref = kRefFloor, l = 0.0f;
+  constexpr int Ahead = 4;   // parts under way at once
+  for (int z = 0; z < pt.parts; z += Ahead) {
+    float2 ml[Ahead];
+    f32x4 v[Ahead][QPer];
 #pragma unroll
-    for (int i = 0; i < NG; ++i) {
-      const float2 v = *(const float2*)(a.part + at * D + 32 * i + 2 * lane);
-      acc[2 * i] += f * v.x;
-      acc[2 * i + 1] += f * v.y;
+    for (int k = 0; k < Ahead; ++k) {
+      const size_t at = first + (size_t)min(z + k, pt.parts - 1) * kPaWaves;
+      ml[k] = *(const float2*)(a.part_ml + (at * 32 + col) * 2);
+#pragma unroll
+      for (int i = 0; i < QPer; ++i)
+        v[k][i] = *(const f32x4*)(a.part + ((at * Quads + wave * QPer + i) * kWave + lane) * 4);
+    }
+    float to = ref;
+#pragma unroll
+    for (int k = 0; k < Ahead; ++k) to = fmaxf(to, ml[k].x);
+    const float f0 = __builtin_amdgcn_exp2f(ref - to);
+    ref = to;
+    l *= f0;
+#pragma unroll
+    for (int i = 0; i < QPer; ++i) acc[i] *= f0;
+#pragma unroll
+    for (int k = 0; k < Ahead; ++k) {
+      const float f = z + k < pt.parts ? __builtin_amdgcn_exp2f(ml[k].x - ref) : 0.0f;
+      l += f * ml[k].y;
+#pragma unroll
+      for (int i = 0; i < QPer; ++i) acc[i] += v[k][i] * f;
     }
   }
-  const int tok = r / a.R, head = h * a.R + r % a.R;
-  const size_t at = (size_t)(pt.first + tok) * a.H + head;
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
-  for (int i = 0; i < NG; ++i)
-    *(uint32_t*)(a.out + at * D + 32 * i + 2 * lane) = pack_bf16(acc[2 * i] * inv, acc[2 * i + 1] * inv);
-  if (a.lse && lane == 0) a.lse[at] = l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+  for (int i = 0; i < QPer; ++i)
+    *(u32x2*)(s_out + OutRows<NG>::at(col, quad_element<32>(wave * QPer + i, part))) =
+        u32x2{pack_bf16(acc[i][0] * inv, acc[i][1] * inv), pack_bf16(acc[i][2] * inv, acc[i][3] * inv)};
+  if (wave == 0 && part == 0 && a.lse && r0 + col < pt.rows)
+    a.lse[(size_t)(pt.first + (r0 + col) / a.R) * a.H + h * a.R + (r0 + col) % a.R] =
+        l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+  __syncthreads();
+  for (int x = threadIdx.x; x < 32 * (D / 8); x += kPaThreads) {
+    const int row = x / (D / 8), d = 8 * (x % (D / 8)), r = r0 + row;
+    if (r >= pt.rows) break;
+    const size_t at = (size_t)(pt.first + r / a.R) * a.H + h * a.R + r % a.R;
+    *(u32x4*)(a.out + at * D + d) = *(const u32x4*)(s_out + OutRows<NG>::at(row, d));
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -409,7 +445,7 @@ constexpr int64_t kPaMaxStride = INT32_MAX / (2 * kPaKeys) - 256;
 
 static bool pa_sizes_ok(int B, int H, int Hk, int D, int max_q) {
   if ((D != 64 && D != 96 && D != 128) || H % Hk || H > (1 << 15)) return false;
-  return (long long)B * Hk <= INT32_MAX && (long long)max_q * (H / Hk) <= 65535ll / (kPaRows / 16) * kPaRows;
+  return (long long)B * Hk <= INT32_MAX && (long long)max_q * (H / Hk) <= 65535ll / kPaWaves * kPaRows;
 }
 
 // Row tiles alone where they fill the chip; otherwise their keys are divided
@@ -453,7 +489,7 @@ static hipError_t pa_launch(const PromptArgs& a, hipStream_t st) {
   hipLaunchKernelGGL(k_prompt_attn<NG>, dim3(bh, (unsigned)a.tiles, (unsigned)a.splits), dim3(kPaThreads), S::LdsBytes,
                      st, a);
   if (a.splits > 1)
-    hipLaunchKernelGGL(k_prompt_join<NG>, dim3(bh, (unsigned)(a.tiles * (kPaRows / 16))), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_prompt_join<NG>, dim3(bh, (unsigned)(a.tiles * kPaWaves)), dim3(kPaThreads), 0, st, a);
   return hipGetLastError();
 }
 
