@@ -38,16 +38,31 @@ struct RopeArgs {
 constexpr int kRopeThreads = 256;
 constexpr int kRopeMaxD = 256;
 
-// Eight elements as floats.
+// Eight elements as they lie in memory, and as floats.
+template <typename Elem>
+struct Octet;
+template <>
+struct Octet<float> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = *(const f32x4*)p, b = *(const f32x4*)(p + 4); }
+  __device__ __forceinline__ void to(float* x) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+  }
+};
+template <>
+struct Octet<__bf16> {
+  bf16x8 a;
+  __device__ __forceinline__ void load(const __bf16* p) { a = *(const bf16x8*)p; }
+  __device__ __forceinline__ void to(float* x) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
+  }
+};
 __device__ __forceinline__ void load8(const float* p, float* x) {
-  const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-}
-__device__ __forceinline__ void load8(const __bf16* p, float* x) {
-  const bf16x8 a = *(const bf16x8*)p;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
+  Octet<float> o;
+  o.load(p);
+  o.to(x);
 }
 __device__ __forceinline__ void store8(float* p, const float* x) {
   *(f32x4*)p = f32x4{x[0], x[1], x[2], x[3]};
@@ -101,8 +116,8 @@ __device__ __forceinline__ void write_octet(uint8_t* tile, int D, bool value, in
 
 // A workgroup takes 256 / lanes tokens of a few heads; `lanes` (8 up to D =
 // 128, 16 beyond) share a row.  A lane holds two octets of its row that rotate
-// against each other, with the cosines and sines, which it keeps over the
-// heads.  Keys reach the cache through LDS, where they change hands from
+// against each other, with the cosines and sines and the norm's weights, which
+// it keeps over the heads; the next head's row is on its way meanwhile.  Keys reach the cache through LDS, where they change hands from
 // octets that rotate together to octets that share a scale.
 template <typename Elem, bool Interleaved>
 __global__ void __launch_bounds__(kRopeThreads)
@@ -146,28 +161,46 @@ k_rope(const RopeArgs a) {
   const int heads = a.H + a.Hk + (a.cache ? a.Hk : 0);
   const int first = blockIdx.y * a.heads_per_wg;
   const int last = min(first + a.heads_per_wg, heads);
+  // consecutive octets, of values and of keys on their way to the cache: lanes
+  // 4 i .. 4 i + 3 hold the groups 2 i and 2 i + 1
+  const int va = (j / 4) * 8 + j % 4, vb = va + 4;
+  const int la = va < octets ? va : 0, lb = vb < octets ? vb : 0;
+  const size_t page_of_slot = kept ? slot / kPage : 0;
+  const int in_page = kept ? slot % kPage : 0;
+  const Elem* qrow = (const Elem*)a.q + (size_t)tc * a.q_stride;
+  const Elem* krow = (const Elem*)a.k + (size_t)tc * a.k_stride;
+  const Elem* vrow = (const Elem*)a.v + (size_t)tc * a.v_stride;
+  Octet<Elem> na, nb;   // the next head's
+  const auto fetch = [&](int hh) {
+    const bool is_q = hh < a.H, is_v = hh >= a.H + a.Hk;
+    const Elem* src = is_q ? qrow + (size_t)hh * D
+                    : is_v ? vrow + (size_t)(hh - a.H - a.Hk) * D : krow + (size_t)(hh - a.H) * D;
+    na.load(src + 8 * (is_v ? la : oa));
+    nb.load(src + 8 * (is_v ? lb : ob));
+  };
+  float wa[8], wb[8];
+  const float* w = nullptr;   // the weights that wa and wb hold
+  fetch(first);
   for (int hh = first; hh < last; ++hh) {
     const bool is_q = hh < a.H, is_v = hh >= a.H + a.Hk;
     const int h = is_q ? hh : is_v ? hh - a.H - a.Hk : hh - a.H;
-    const Elem* src = is_q ? (const Elem*)a.q + (size_t)tc * a.q_stride
-                    : is_v ? (const Elem*)a.v + (size_t)tc * a.v_stride
-                           : (const Elem*)a.k + (size_t)tc * a.k_stride;
-    src += (size_t)h * D;
     float xa[8], xb[8];
+    na.to(xa);
+    nb.to(xb);
+    if (hh + 1 < last) fetch(hh + 1);
+    uint8_t* tile = a.cache + (page_of_slot * a.Hk + h) * tile_bytes(D);
     if (is_v) {
-      // consecutive octets: lanes 4 i .. 4 i + 3 hold the groups 2 i and 2 i + 1
-      const int va = (j / 4) * 8 + j % 4, vb = va + 4;
-      uint8_t* tile = a.cache + ((size_t)(kept ? slot / kPage : 0) * a.Hk + h) * tile_bytes(D);
-      load8(src + 8 * (va < octets ? va : 0), xa);
-      load8(src + 8 * (vb < octets ? vb : 0), xb);
-      if (kept && va < octets) write_octet(tile, D, true, slot % kPage, va, xa);
-      if (kept && vb < octets) write_octet(tile, D, true, slot % kPage, vb, xb);
+      if (kept && va < octets) write_octet(tile, D, true, in_page, va, xa);
+      if (kept && vb < octets) write_octet(tile, D, true, in_page, vb, xb);
       continue;
     }
-    load8(src + 8 * oa, xa);
-    load8(src + 8 * ob, xb);
-    const float* w = is_q ? a.q_weight : a.k_weight;
-    if (w) {
+    const float* weight = is_q ? a.q_weight : a.k_weight;
+    if (weight) {
+      if (weight != w) {
+        load8(weight + 8 * oa, wa);
+        load8(weight + 8 * ob, wb);
+        w = weight;
+      }
       float ss = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(xa[i], xa[i], __builtin_fmaf(xb[i], xb[i], ss));
@@ -177,9 +210,6 @@ k_rope(const RopeArgs a) {
       ss += partner_f32<2>(ss);
       if (lanes == 16) ss += partner_f32<3>(ss);
       const float r = 1.0f / __builtin_sqrtf(ss / (float)D + a.eps);
-      float wa[8], wb[8];
-      load8(w + 8 * oa, wa);
-      load8(w + 8 * ob, wb);
 #pragma unroll
       for (int i = 0; i < 8; ++i) xa[i] = xa[i] * r * wa[i], xb[i] = xb[i] * r * wb[i];
     }
@@ -216,47 +246,48 @@ k_rope(const RopeArgs a) {
         store8(row + 8 * ob, xb);
       }
       __builtin_amdgcn_wave_barrier();   // the lanes of a row are in one wave
-      const int va = (j / 4) * 8 + j % 4, vb = va + 4;
-      uint8_t* tile = a.cache + ((size_t)(kept ? slot / kPage : 0) * a.Hk + h) * tile_bytes(D);
       float ya[8], yb[8];
-      load8(row + 8 * (va < octets ? va : 0), ya);
-      load8(row + 8 * (vb < octets ? vb : 0), yb);
+      load8(row + 8 * la, ya);
+      load8(row + 8 * lb, yb);
       __builtin_amdgcn_wave_barrier();
-      if (kept && va < octets) write_octet(tile, D, false, slot % kPage, va, ya);
-      if (kept && vb < octets) write_octet(tile, D, false, slot % kPage, vb, yb);
+      if (kept && va < octets) write_octet(tile, D, false, in_page, va, ya);
+      if (kept && vb < octets) write_octet(tile, D, false, in_page, vb, yb);
     }
   }
 }
 
 // ---------------------------------------------------------------------------
-// what the cache holds: a thread per eight elements of a token's head
+// what the cache holds: a thread per sixteen elements of a token's head
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void store_held(__bf16* p, const bf16x2* x, bool nan) {
-  u32x4 o;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = nan ? 0x7fc07fc0u : __builtin_bit_cast(uint32_t, x[i]);
-  *(u32x4*)p = o;
+  for (int k = 0; k < 2; ++k) {
+    u32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = nan ? 0x7fc07fc0u : __builtin_bit_cast(uint32_t, x[4 * k + i]);
+    *(u32x4*)(p + 8 * k) = o;
+  }
 }
 __device__ __forceinline__ void store_held(uint8_t* p, const bf16x2* x, bool nan) {
-  u32x2 o;
+  u32x4 o;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < 4; ++i) {
     int w = 0;
     w = __builtin_amdgcn_cvt_pk_bf8_f32((float)x[2 * i][0], (float)x[2 * i][1], w, false);
     w = __builtin_amdgcn_cvt_pk_bf8_f32((float)x[2 * i + 1][0], (float)x[2 * i + 1][1], w, true);
     o[i] = nan ? 0x7f7f7f7fu : (uint32_t)w;
   }
-  *(u32x2*)p = o;
+  *(u32x4*)p = o;
 }
 
 template <typename Out>
 __global__ void __launch_bounds__(256)
 k_cache_read(const uint8_t* __restrict__ cache, int n_pages, int Hk, int D, const int32_t* __restrict__ slots,
              long long n, Out* __restrict__ k_out, Out* __restrict__ v_out) {
-  const int octets = D / 8;
+  const int pieces = D / 16;
   for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-    const int o = (int)(i % octets);
-    const long long th = i / octets;
+    const int o = (int)(i % pieces);
+    const long long th = i / pieces;
     const int h = (int)(th % Hk);
     const int slot = slots[th / Hk];
     const bool there = slot >= 0 && slot / kPage < n_pages;
@@ -266,16 +297,19 @@ k_cache_read(const uint8_t* __restrict__ cache, int n_pages, int Hk, int D, cons
     for (int kv = 0; kv < 2; ++kv) {
       Out* out = kv ? v_out : k_out;
       if (!out) continue;
-      const uint32_t byte = tile[(kv ? v_scales_at(D) : k_scales_at(D)) + token * scale_stride(D) + o / 4];
-      uint32_t c = *(const uint32_t*)(tile + kv * codes_bytes(D) + (o / 4 * kPage + token) * kCodeBytes + o % 4 * 4);
-      c = there ? c : 0u;
+      const uint32_t byte = tile[(kv ? v_scales_at(D) : k_scales_at(D)) + token * scale_stride(D) + o / 2];
+      u32x2 c = *(const u32x2*)(tile + kv * codes_bytes(D) + (o / 2 * kPage + token) * kCodeBytes + o % 2 * 8);
       const float s = scale_of(there && byte != 255 ? byte : kUnitScale);
-      bf16x2 x[4];
-      x[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0);
-      x[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1);
-      x[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2);
-      x[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3);
-      store_held(out + 8 * i, x, there && byte == 255);
+      bf16x2 x[8];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t ck = there ? c[k] : 0u;
+        x[4 * k + 0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(ck, s, 0);
+        x[4 * k + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(ck, s, 1);
+        x[4 * k + 2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(ck, s, 2);
+        x[4 * k + 3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(ck, s, 3);
+      }
+      store_held(out + 16 * i, x, there && byte == 255);
     }
   }
 }
@@ -344,7 +378,7 @@ fdllm_status fdllm_cache_read(const uint8_t* cache, int n_pages, int Hk, int D, 
   if (T == 0) return FDLLM_OK;
   if (!cache || n_pages < 1 || !slots || (!k_out && !v_out)) return FDLLM_ERR_INVALID_ARG;
   if (!aligned16(cache) || !aligned16(k_out) || !aligned16(v_out)) return FDLLM_ERR_INVALID_ARG;
-  const long long n = (long long)T * Hk * (D / 8);
+  const long long n = (long long)T * Hk * (D / 16);
   const long long blocks = (n + 255) / 256;
   const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192));
   hipStream_t st = (hipStream_t)stream;
