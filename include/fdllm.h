@@ -529,8 +529,8 @@ fdllm_status fdllm_cache_read(const uint8_t* cache, int n_pages, int Hk, int D, 
  *   scale: > 0, usually 1 / sqrt(D);
  *   out [T, H, D] bf16; lse [T, H] float: log of the sum of exp(scale q.k) (may
  *   be NULL);
- *   workspace: fdllm_cache_attention_workspace_size() bytes, 16-byte aligned,
- *   scratch between calls.
+ *   workspace: fdllm_cache_attention_workspace_size() bytes, 16-byte aligned
+ *   (NULL where that is 0), scratch between calls.
  *   D: 64, 96 or 128.  bf16 rounding of the weights exp(s - max) and of out;
  *   scores, sums and maxima in float32.  For fixed sizes, lengths and tables a
  *   call is bitwise reproducible.

@@ -55,7 +55,7 @@ struct CacheAttnArgs {
   float c;                    // scale * log2 e
   uint16_t* out;
   float* lse;
-  int32_t* plan;              // units of all sequences, then those before each
+  int32_t* plan;              // units of all sequences, then those before each (null: no item is split)
   float* part_ml;             // [workgroups][2][WR][MT][2]: reference and sum of a row's partial result
   float* part;                // [workgroups][2][WR] tiles of partial sums (attn_common.h)
 };
@@ -250,7 +250,7 @@ k_cache_attn(const CacheAttnArgs a) {
   if (units == 0) return;
   const Shares shares(units, gridDim.x);
   const int u_begin = shares.begin(blockIdx.x), u_end = shares.begin(blockIdx.x + 1);
-  if (blockIdx.x == 0 && tid == 0) a.plan[0] = units;
+  if (a.plan && blockIdx.x == 0 && tid == 0) a.plan[0] = units;
   if (u_begin >= u_end) return;
   int b, before;
   const bool here = u_begin >= incl - mine && u_begin < incl;
@@ -294,7 +294,7 @@ k_cache_attn(const CacheAttnArgs a) {
     }
     const int each = seq.pages + kItemUnits, item = (u - before) / each;
     const int at = u - before - item * each, upto = min(each, at + (u_end - u));
-    if (u == before && tid == 0) a.plan[1 + b] = before;   // for the join
+    if (a.plan && u == before && tid == 0) a.plan[1 + b] = before;   // for the join
     u += upto - at;
     const int page0 = max(0, at - kItemEnds), page1 = min(seq.pages, upto - kItemEnds);
     if (page1 <= page0) continue;
@@ -714,6 +714,7 @@ static CaPlan ca_plan(int B, int H, int Hk, int D, int max_q, int table_w) {
   // equal items that the shares are a multiple of, or one share: none is split
   p.join = p.wgs > 1 && !(B == 1 && p.wgs == items);
   p.split = p.wgs >= 4 * items;
+  if (!p.join) return p;
   const size_t rows_out = (size_t)p.wgs * 2 * per;
   p.at_ml = align256(((size_t)B + 1) * 4);
   p.at_part = p.at_ml + align256(rows_out * 8);
@@ -782,11 +783,11 @@ fdllm_status fdllm_cache_attention(const void* q, int64_t q_stride, int T, const
   for (const void* p : {q, (const void*)cache, (const void*)out, (const void*)workspace})
     if ((uintptr_t)p & 15) return FDLLM_ERR_INVALID_ARG;
   const CaPlan p = ca_plan(B, H, Hk, D, max_q, table_width);
-  if (!workspace || workspace_bytes < p.bytes) return FDLLM_ERR_WORKSPACE;
+  if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return FDLLM_ERR_WORKSPACE;
   char* ws = (char*)workspace;
   const CacheAttnArgs a{(const uint16_t*)q, q_stride, T, cache, n_pages, page_table, table_width, kv_len, cu_q,
-                        q_start, B, H, Hk, H / Hk, max_q, blk, scale * kLog2e, (uint16_t*)out, lse, (int32_t*)ws,
-                        (float*)(ws + p.at_ml), (float*)(ws + p.at_part)};
+                        q_start, B, H, Hk, H / Hk, max_q, blk, scale * kLog2e, (uint16_t*)out, lse,
+                        p.join ? (int32_t*)ws : nullptr, (float*)(ws + p.at_ml), (float*)(ws + p.at_part)};
   hipStream_t st = (hipStream_t)stream;
   const hipError_t e = D == 64 ? ca_launch<2>(a, p, st) : D == 96 ? ca_launch<3>(a, p, st) : ca_launch<4>(a, p, st);
   return e == hipSuccess ? FDLLM_OK : FDLLM_ERR_HIP;

@@ -23,6 +23,7 @@ constexpr int kPaWaves = kPaThreads / kWave;
 constexpr int kPaRows = kPaWaves * 32;
 constexpr int kPaKeys = 64;
 constexpr int kPaSplitTiles = 4;   // tiles of keys that a part of a split row tile has at least
+constexpr int kPaWholeTiles = 8;   // and those up to which none is split: joining costs a launch and 4 us
 
 struct PromptArgs {
   const uint16_t* q;
@@ -59,7 +60,7 @@ __device__ __forceinline__ PaTile pa_tile(const PromptArgs& a, int b, int tile) 
   const int last = min(t.rows, (tile + 1) * kPaRows) - 1;
   t.far = visible_end(t.len - t.n + last / a.R, a.blk, t.len);
   const int nt = (t.far + kPaKeys - 1) / kPaKeys;
-  t.parts = max(1, min(a.splits, (nt + kPaSplitTiles - 1) / kPaSplitTiles));
+  t.parts = nt <= kPaWholeTiles ? 1 : min(a.splits, (nt + kPaSplitTiles - 1) / kPaSplitTiles);
   return t;
 }
 
@@ -455,7 +456,7 @@ static PaPlan pa_plan(int B, int Tk, int H, int Hk, int D, int max_q) {
   p.tiles = (int)(((long long)max_q * (H / Hk) + kPaRows - 1) / kPaRows);
   const long long base = (long long)B * Hk * p.tiles;
   p.splits = 1;
-  if (base > 0 && base < 256) {
+  if (base > 0 && base < 256 && Tk > kPaKeys * kPaWholeTiles) {
     const long long most = (Tk + kPaKeys * kPaSplitTiles - 1) / (kPaKeys * kPaSplitTiles);
     const long long want = 512 / base;
     p.splits = (int)(want < most ? want : most);
