@@ -551,7 +551,8 @@ fdllm_status fdllm_cache_attention(const void* q, int64_t q_stride, int T, const
  * fdllm_prompt_attention_workspace_size() bytes, 16-byte aligned (NULL where
  * that is 0).  Other arguments as above.
  */
-fdllm_status fdllm_prompt_attention_workspace_size(int B, int Tk, int H, int Hk, int D, int max_q, size_t* bytes);
+fdllm_status fdllm_prompt_attention_workspace_size(int B, int T, int Tk, int H, int Hk, int D, int max_q, int blk,
+                                                   size_t* bytes);
 fdllm_status fdllm_prompt_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                     int64_t v_stride, int T, int Tk, const int32_t* cu_q, const int32_t* cu_k, int B,
                                     int max_q, int H, int Hk, int D, float scale, int blk, void* out, float* lse,

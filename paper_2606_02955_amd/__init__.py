@@ -115,7 +115,7 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
                                           f32, i32, vp, vp, vp, sz, vp]
     lib.fdllm_prompt_attention.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, i32, i32, i32, i32, i32,
                                            f32, i32, vp, vp, vp, sz, vp]
-    lib.fdllm_prompt_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.fdllm_prompt_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
     for name in ("fdllm_cache_tile_bytes", "fdllm_qk_norm_rope", "fdllm_cache_read",
                  "fdllm_cache_attention_workspace_size", "fdllm_cache_attention",
                  "fdllm_prompt_attention_workspace_size", "fdllm_prompt_attention", "fdllm_confidence", "fdllm_reveal", "fdllm_decode_step", "fdllm_workspace_size",
@@ -602,9 +602,10 @@ def fdllm_cache_attention(q, cache, page_table, kv_len, cu_q, out, max_q: int, l
 
 
 @functools.lru_cache(maxsize=4096)
-def fdllm_prompt_attention_workspace_size(B: int, Tk: int, H: int, Hk: int, D: int, max_q: int) -> int:
+def fdllm_prompt_attention_workspace_size(B: int, T: int, Tk: int, H: int, Hk: int, D: int, max_q: int,
+                                          blk: int = 0) -> int:
     n = ctypes.c_size_t(0)
-    _check(load().fdllm_prompt_attention_workspace_size(B, Tk, H, Hk, D, max_q, ctypes.byref(n)),
+    _check(load().fdllm_prompt_attention_workspace_size(B, T, Tk, H, Hk, D, max_q, blk, ctypes.byref(n)),
            "fdllm_prompt_attention_workspace_size")
     return int(n.value)
 
@@ -621,7 +622,7 @@ def fdllm_prompt_attention(q, k, v, cu_q, cu_k, out, max_q: int, lse=None, scale
     vp, vs = _heads(v, (Tk, Hk, D), bf16, "v")
     B = cu_q.shape[0] - 1
     workspace, wp, wb = _scratch(
-        workspace, 0 if workspace is not None else fdllm_prompt_attention_workspace_size(B, Tk, H, Hk, D, max_q),
+        workspace, 0 if workspace is not None else fdllm_prompt_attention_workspace_size(B, T, Tk, H, Hk, D, max_q, blk),
         q.device)
     st = load().fdllm_prompt_attention(
         qp, qs, kp, ks, vp, vs, T, Tk, _raw(cu_q, torch.int32, (B + 1,), "cu_q"),

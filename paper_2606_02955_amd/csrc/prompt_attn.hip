@@ -24,6 +24,8 @@ constexpr int kPaRows = kPaWaves * 32;
 constexpr int kPaKeys = 64;
 constexpr int kPaSplitTiles = 4;   // tiles of keys that a part of a split row tile has at least
 constexpr int kPaWholeTiles = 8;   // and those up to which none is split: joining costs a launch and 4 us
+constexpr int kPaSlots = 512;      // workgroups that the chip runs at once
+constexpr int kPaMaxParts = 1536;  // that a call may have room for
 
 struct PromptArgs {
   const uint16_t* q;
@@ -37,9 +39,10 @@ struct PromptArgs {
   float c;
   uint16_t* out;
   float* lse;
-  int tiles, splits;   // row tiles of max_q tokens; workgroups for the keys of one
-  float* part_ml;      // [(b, h), tile, split, wave][32][2]: reference and sum of a row's partial result
-  float* part;         // [(b, h), tile, split, wave] tiles of partial sums (attn_common.h)
+  int tiles, splits;   // row tiles of max_q tokens; most parts that the keys of one are divided into
+  int share;           // tiles of keys that a part is to have
+  float* part_ml;      // [row tile, h, split, wave][32][2]: reference and sum of a row's partial result
+  float* part;         // [row tile, h, split, wave] tiles of partial sums (attn_common.h)
 };
 
 // A tile of rows: 128 of a sequence's query tokens times the heads of a key head.
@@ -47,6 +50,7 @@ struct PaTile {
   int first, firstk, n, len, rows;
   int far;      // the most keys that any row sees
   int parts;    // into which its keys are divided
+  int place;    // among the row tiles of all sequences (with gaps)
 };
 
 __device__ __forceinline__ PaTile pa_tile(const PromptArgs& a, int b, int tile) {
@@ -56,11 +60,13 @@ __device__ __forceinline__ PaTile pa_tile(const PromptArgs& a, int b, int tile) 
   t.rows = t.n * a.R;
   t.far = 0;
   t.parts = 1;
+  t.place = 0;
   if (tile * kPaRows >= t.rows) return t;
   const int last = min(t.rows, (tile + 1) * kPaRows) - 1;
   t.far = visible_end(t.len - t.n + last / a.R, a.blk, t.len);
   const int nt = (t.far + kPaKeys - 1) / kPaKeys;
-  t.parts = nt <= kPaWholeTiles ? 1 : min(a.splits, (nt + kPaSplitTiles - 1) / kPaSplitTiles);
+  t.parts = nt <= max(kPaWholeTiles, 2 * a.share) ? 1 : min(a.splits, (nt + a.share - 1) / a.share);
+  t.place = (int)((long long)t.first * a.R / kPaRows) + b + tile;
   return t;
 }
 
@@ -358,7 +364,7 @@ k_prompt_attn(const PromptArgs a) {
       }
     }
   } else {
-    const size_t part_tile = (((size_t)blockIdx.x * a.tiles + tile) * a.splits + blockIdx.z) * kPaWaves + wave;
+    const size_t part_tile = (((size_t)pt.place * a.Hk + h) * a.splits + blockIdx.z) * kPaWaves + wave;
 #pragma unroll
     for (int q = 0; q < Quads; ++q) {
       const int x = q / 4, i = 4 * (q % 4);
@@ -383,7 +389,7 @@ k_prompt_join(const PromptArgs a) {
   if (r0 >= pt.rows || pt.parts == 1) return;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int col = lane % 32, part = lane / 32;
-  const size_t first = (((size_t)blockIdx.x * a.tiles + tile) * a.splits) * kPaWaves + wr;
+  const size_t first = (((size_t)pt.place * a.Hk + h) * a.splits) * kPaWaves + wr;
   f32x4 acc[QPer];
 #pragma unroll
   for (int i = 0; i < QPer; ++i) acc[i] = f32x4{};
@@ -437,7 +443,7 @@ k_prompt_join(const PromptArgs a) {
 // host side
 // ---------------------------------------------------------------------------
 struct PaPlan {
-  int tiles, splits;
+  int tiles, splits, share;
   size_t at_part, bytes;
 };
 
@@ -449,24 +455,36 @@ static bool pa_sizes_ok(int B, int H, int Hk, int D, int max_q) {
   return (long long)B * Hk <= INT32_MAX && (long long)max_q * (H / Hk) <= 65535ll / kPaWaves * kPaRows;
 }
 
-// Row tiles alone where they fill the chip; otherwise their keys are divided
-// too, two workgroups a CU in all.
-static PaPlan pa_plan(int B, int Tk, int H, int Hk, int D, int max_q) {
+// A row tile's keys are divided where the longest tile would run on while the
+// rest of the chip is done: where it has more than twice the keys that fall to
+// one of the workgroups that run at once, as far as the host knows them (it
+// knows the sums of the lengths, not the lengths).  Three sequences of 1, 1937
+// and 3873 tokens with 5 heads on one: 61 us whole, 47 divided; 13 of 570
+// tokens: 18 whole, 31 divided, so what is merely uneven stays whole.
+static PaPlan pa_plan(int B, int T, int Tk, int H, int Hk, int D, int max_q, int blk) {
   PaPlan p{};
-  p.tiles = (int)(((long long)max_q * (H / Hk) + kPaRows - 1) / kPaRows);
-  const long long base = (long long)B * Hk * p.tiles;
+  const int R = H / Hk;
+  p.tiles = (int)(((long long)max_q * R + kPaRows - 1) / kPaRows);
   p.splits = 1;
-  if (base > 0 && base < 256 && Tk > kPaKeys * kPaWholeTiles) {
-    const long long most = (Tk + kPaKeys * kPaSplitTiles - 1) / (kPaKeys * kPaSplitTiles);
-    const long long want = 512 / base;
-    p.splits = (int)(want < most ? want : most);
-    if (p.splits < 1) p.splits = 1;
+  p.share = kPaSplitTiles;
+  if (B < 1 || p.tiles < 1) return p;
+  const long long places = (long long)T * R / kPaRows + B + 1;
+  const long long past = Tk > T ? (Tk - T) / B : 0;
+  const long long keys = Tk / B - (blk && T < Tk + B ? T / B / 2 : 0);   // of a row, in the middle
+  const long long units = ((long long)T * R + kPaRows - 1) / kPaRows * Hk * (keys / kPaKeys + 1);
+  const long long longest = ((blk ? max_q + past : Tk < max_q + past ? Tk : max_q + past) + kPaKeys - 1) / kPaKeys;
+  const long long share = units / kPaSlots;
+  p.share = (int)(share > kPaSplitTiles ? share : kPaSplitTiles);
+  if (longest <= kPaWholeTiles || longest <= 2ll * p.share) return p;
+  const long long room = kPaMaxParts / (places * Hk), want = (longest + p.share - 1) / p.share;
+  p.splits = (int)(room < want ? room : want);
+  if (p.splits < 2) {
+    p.splits = 1;
+    return p;
   }
-  if (p.splits > 1) {
-    const size_t rows = (size_t)base * p.splits * kPaRows;
-    p.at_part = align256(rows * 8);
-    p.bytes = p.at_part + rows * D * sizeof(float);
-  }
+  const size_t rows = (size_t)places * Hk * p.splits * kPaRows;
+  p.at_part = align256(rows * 8);
+  p.bytes = p.at_part + rows * D * sizeof(float);
   return p;
 }
 
@@ -500,10 +518,11 @@ using namespace fdllm;
 
 extern "C" {
 
-fdllm_status fdllm_prompt_attention_workspace_size(int B, int Tk, int H, int Hk, int D, int max_q, size_t* bytes) {
-  if (!bytes || B < 0 || Tk < 0 || H < 1 || Hk < 1 || max_q < 0) return FDLLM_ERR_INVALID_ARG;
+fdllm_status fdllm_prompt_attention_workspace_size(int B, int T, int Tk, int H, int Hk, int D, int max_q, int blk,
+                                                   size_t* bytes) {
+  if (!bytes || B < 0 || T < 0 || Tk < 0 || blk < 0 || H < 1 || Hk < 1 || max_q < 0) return FDLLM_ERR_INVALID_ARG;
   if (!pa_sizes_ok(B, H, Hk, D, max_q)) return FDLLM_ERR_SIZE;
-  *bytes = pa_plan(B, Tk, H, Hk, D, max_q).bytes;
+  *bytes = pa_plan(B, T, Tk, H, Hk, D, max_q, blk).bytes;
   return FDLLM_OK;
 }
 
@@ -522,11 +541,11 @@ fdllm_status fdllm_prompt_attention(const void* q, int64_t q_stride, const void*
   if (k_stride > kPaMaxStride || v_stride > kPaMaxStride) return FDLLM_ERR_SIZE;
   for (const void* p : {q, k, v, (const void*)out, (const void*)workspace})
     if ((uintptr_t)p & 15) return FDLLM_ERR_INVALID_ARG;
-  const PaPlan p = pa_plan(B, Tk, H, Hk, D, max_q);
+  const PaPlan p = pa_plan(B, T, Tk, H, Hk, D, max_q, blk);
   if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return FDLLM_ERR_WORKSPACE;
   char* ws = (char*)workspace;
   const PromptArgs a{(const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, q_stride, k_stride, v_stride, T, Tk,
-                     cu_q, cu_k, B, H, Hk, H / Hk, max_q, blk, scale * kLog2e, (uint16_t*)out, lse, p.tiles, p.splits,
+                     cu_q, cu_k, B, H, Hk, H / Hk, max_q, blk, scale * kLog2e, (uint16_t*)out, lse, p.tiles, p.splits, p.share,
                      (float*)ws, (float*)(ws + p.at_part)};
   hipStream_t st = (hipStream_t)stream;
   const hipError_t e = D == 64 ? pa_launch<2>(a, st) : D == 96 ? pa_launch<3>(a, st) : pa_launch<4>(a, st);

@@ -116,13 +116,13 @@ def test_prompt_attention_refuses(lib, kw, status):
 
 def test_workspace_sizes(lib):
     assert fd.fdllm_cache_attention_workspace_size(2, 8, 2, 128, 1, 100) > 0
-    assert fd.fdllm_prompt_attention_workspace_size(64, 1 << 16, 32, 8, 128, 1024) == 0     # row tiles fill the chip
-    assert fd.fdllm_prompt_attention_workspace_size(1, 1 << 16, 4, 1, 128, 1) > 0
+    assert fd.fdllm_prompt_attention_workspace_size(64, 1 << 16, 1 << 16, 32, 8, 128, 1024) == 0     # row tiles fill the chip
+    assert fd.fdllm_prompt_attention_workspace_size(1, 1, 1 << 16, 4, 1, 128, 1) > 0
     n = ctypes.c_size_t(0)
     assert lib.fdllm_cache_attention_workspace_size(2, 8, 2, 128, 1, 100, None) == fd.ERR_INVALID_ARG
     assert lib.fdllm_cache_attention_workspace_size(2, 8, 3, 128, 1, 100, ctypes.byref(n)) == fd.ERR_SIZE
-    assert lib.fdllm_prompt_attention_workspace_size(-1, 8, 2, 2, 128, 1, ctypes.byref(n)) == fd.ERR_INVALID_ARG
-    assert lib.fdllm_prompt_attention_workspace_size(1, 8, 2, 2, 80, 1, ctypes.byref(n)) == fd.ERR_SIZE
+    assert lib.fdllm_prompt_attention_workspace_size(-1, 8, 8, 2, 2, 128, 1, 0, ctypes.byref(n)) == fd.ERR_INVALID_ARG
+    assert lib.fdllm_prompt_attention_workspace_size(1, 8, 8, 2, 2, 80, 1, 0, ctypes.byref(n)) == fd.ERR_SIZE
 
 
 def test_binding_refuses(lib):

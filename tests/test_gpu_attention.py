@@ -454,7 +454,7 @@ def test_capture_into_a_graph(gpu):
     q_out, out, lse = torch.empty_like(x[0]), torch.empty_like(x[0]), torch.empty((T, H), device=DEV)
     own = torch.empty_like(x[0])
     ws = torch.empty(gpu.fdllm_cache_attention_workspace_size(B, H, Hk, D, n, pages), dtype=torch.uint8, device=DEV)
-    need = gpu.fdllm_prompt_attention_workspace_size(B, T, H, Hk, D, n)
+    need = gpu.fdllm_prompt_attention_workspace_size(B, T, T, H, Hk, D, n)
     ws2 = torch.empty(max(need, 16), dtype=torch.uint8, device=DEV)
 
     def step():
