@@ -279,6 +279,7 @@ k_prompt_attn(const PromptArgs a) {
     pa_arrive();
     if (t + 3 < t1) load_k(t + 3, buf ^ 1);
     load_v(t + 1, buf ^ 1);
+    __builtin_amdgcn_s_setprio(1);
     vf[0] = value_operand(0, buf);
     vf[1] = value_operand(1, buf);
     PA_FENCE();
@@ -297,6 +298,7 @@ k_prompt_attn(const PromptArgs a) {
         top = fmaxf(fmaxf(top, sn[m / 8][2 * (m % 8)]), sn[m / 8][2 * (m % 8) + 1]);
       PA_FENCE();
     }
+    __builtin_amdgcn_s_setprio(0);
     follow(max_halves(top) * a.c);
   };
   const auto last = [&](const f32x16* s, int buf) {
