@@ -711,8 +711,11 @@ static CaPlan ca_plan(int B, int H, int Hk, int D, int max_q, int table_w) {
   const long long items = (long long)B * p.items, most = items * ((table_w + wk - 1) / wk);
   const int fill = 256 * 8 / waves;
   p.wgs = (int)(most < fill ? (most < 1 ? 1 : most) : fill);
-  // equal items that the shares are a multiple of, or one share: none is split
-  p.join = p.wgs > 1 && !(B == 1 && p.wgs == items);
+  // None is split where there is one share, where an item has no more than a
+  // page, or where one sequence of one group of rows has an item a share.  (With
+  // more groups it may have fewer items than max_q stands for, and shares that
+  // begin inside one.)
+  p.join = p.wgs > 1 && table_w > 1 && !(B == 1 && groups == 1 && p.wgs == items);
   p.split = p.wgs >= 4 * items;
   if (!p.join) return p;
   const size_t rows_out = (size_t)p.wgs * 2 * per;

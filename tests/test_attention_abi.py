@@ -57,7 +57,7 @@ def _rope(lib, **kw):
     (dict(pages=-1), fd.ERR_INVALID_ARG), (dict(n_pos=-1), fd.ERR_INVALID_ARG),
     (dict(D=48), fd.ERR_SIZE), (dict(D=288), fd.ERR_SIZE), (dict(D=0), fd.ERR_SIZE),
     (dict(rot=72), fd.ERR_SIZE), (dict(rot=24), fd.ERR_SIZE), (dict(rot=-16), fd.ERR_SIZE),
-    (dict(pages=1 << 26), fd.ERR_SIZE),
+    (dict(pages=1 << 26), fd.ERR_SIZE), (dict(H=1 << 15, qs=1 << 21), fd.ERR_SIZE), (dict(T=1 << 28), fd.ERR_SIZE),
     (dict(eps=-1.0), fd.ERR_INVALID_ARG), (dict(eps=float("nan")), fd.ERR_INVALID_ARG),
     (dict(q=None), fd.ERR_INVALID_ARG), (dict(k=None), fd.ERR_INVALID_ARG), (dict(qo=None), fd.ERR_INVALID_ARG),
     (dict(pos=None), fd.ERR_INVALID_ARG), (dict(cs=None), fd.ERR_INVALID_ARG),
@@ -118,6 +118,9 @@ def test_workspace_sizes(lib):
     assert fd.fdllm_cache_attention_workspace_size(2, 8, 2, 128, 1, 100) > 0
     assert fd.fdllm_prompt_attention_workspace_size(64, 1 << 16, 1 << 16, 32, 8, 128, 1024) == 0     # row tiles fill the chip
     assert fd.fdllm_prompt_attention_workspace_size(1, 1, 1 << 16, 4, 1, 128, 1) > 0
+    # 64 groups of rows of 8 heads are an item a workgroup only where the sequence has all max_q queries
+    assert fd.fdllm_cache_attention_workspace_size(1, 32, 8, 128, 2048, 10) > 0
+    assert fd.fdllm_cache_attention_workspace_size(1, 32, 8, 128, 2048, 1) == 0                       # no item has two pages
     n = ctypes.c_size_t(0)
     assert lib.fdllm_cache_attention_workspace_size(2, 8, 2, 128, 1, 100, None) == fd.ERR_INVALID_ARG
     assert lib.fdllm_cache_attention_workspace_size(2, 8, 3, 128, 1, 100, ctypes.byref(n)) == fd.ERR_SIZE

@@ -334,6 +334,27 @@ def test_cache_attention_left_out_sequences_and_lengths(gpu):
     assert (out[:2] == 3.0).all()
 
 
+def test_cache_attention_fewer_queries_than_room(gpu):
+    # one sequence with a few of the max_q queries that the call has room for: as
+    # many items at max_q as workgroups, so a whole item's share is less than one
+    for n, max_q in ((100, 8192), (129, 8192), (5, 8192)):
+        q, kv, cu, out, lse, _, (cache, table) = _run_cache(gpu, 64, 8, 8, 1, [(n, 300)], n)
+        out.fill_(float("nan"))
+        lse.fill_(float("nan"))
+        gpu.fdllm_cache_attention(q, cache, _i32(table), _i32([300]), _i32(cu), out, max_q, lse=lse, blk=1)
+        torch.cuda.synchronize()
+        _check(out, lse, _want(q, kv, cu, 1, 64), 64)
+
+
+def test_cache_attention_one_page_each(gpu):
+    # items of one page are never divided, however many sequences: no workspace
+    seqs = [(n, m) for n, m in zip([1, 32, 7, 0, 20] * 9, [64, 5, 1, 64, 0, 33, 63] * 7)]
+    q, kv, cu, out, lse, ws, _ = _run_cache(gpu, 128, 8, 2, 1, seqs, 21, width_more=0)
+    torch.cuda.synchronize()
+    assert ws is None
+    _check(out, lse, _want(q, kv, cu, 1, 128), 128)
+
+
 def test_cache_attention_repeats_bit_for_bit(gpu):
     for D, H, Hk, n in ((128, 8, 2, 32), (64, 4, 1, 1)):
         seqs = [(n, 5000), (n, 77), (n, 1300)]
