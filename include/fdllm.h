@@ -494,7 +494,7 @@ fdllm_status fdllm_cache_tile_bytes(int D, size_t* bytes);
  *   such as -1, is not stored).  A call's slots must differ.
  *   A token whose position is outside [0, n_pos) gets zeros in q_out and k_out
  *   and is not stored (with rot = 0 positions are not looked at).
- *   D: a multiple of 32, 32 to 256.
+ *   D: a multiple of 32, 32 to 256; at most 2^27 tokens and 2^14 heads.
  */
 fdllm_status fdllm_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                 int64_t v_stride, fdllm_dtype dtype, int T, int H, int Hk, int D,

@@ -117,8 +117,9 @@ __device__ __forceinline__ void write_octet(uint8_t* tile, int D, bool value, in
 // A workgroup takes 256 / lanes tokens of a few heads; `lanes` (8 up to D =
 // 128, 16 beyond) share a row.  A lane holds two octets of its row that rotate
 // against each other, with the cosines and sines and the norm's weights, which
-// it keeps over the heads; the next head's row is on its way meanwhile.  Keys reach the cache through LDS, where they change hands from
-// octets that rotate together to octets that share a scale.
+// it keeps over the heads; the next head's row is on its way meanwhile.  Keys
+// reach the cache through LDS, where they change hands from octets that rotate
+// together to octets that share a scale.
 template <typename Elem, bool Interleaved>
 __global__ void __launch_bounds__(kRopeThreads)
 k_rope(const RopeArgs a) {
@@ -338,7 +339,8 @@ fdllm_status fdllm_qk_norm_rope(const void* q, int64_t q_stride, const void* k, 
   if (dtype != FDLLM_BF16 && dtype != FDLLM_F32) return FDLLM_ERR_UNSUPPORTED_DTYPE;
   if (T < 0 || H < 1 || Hk < 1 || n_pages < 0 || n_pos < 0) return FDLLM_ERR_INVALID_ARG;
   if (D < 32 || D > kRopeMaxD || D % 32 || rot < 0 || rot > D || rot % 16) return FDLLM_ERR_SIZE;
-  if (H > (1 << 15) || Hk > (1 << 15) || n_pages > INT32_MAX / kPage) return FDLLM_ERR_SIZE;
+  // a launch has at most 2^32 threads along the tokens, 65535 workgroups along the heads
+  if (H > (1 << 14) || Hk > (1 << 14) || T > (1 << 27) || n_pages > INT32_MAX / kPage) return FDLLM_ERR_SIZE;
   if (!(eps >= 0.0f)) return FDLLM_ERR_INVALID_ARG;
   if (T == 0) return FDLLM_OK;
   if (!q || !k || !positions || !q_out || (rot > 0 && !cos_sin) || (!k_out && !cache)) return FDLLM_ERR_INVALID_ARG;
