@@ -1,7 +1,7 @@
 """Python binding of libfdllm.so, the gfx950 Fast-dLLM++ commit selector.
 
-Thin ctypes marshalling of the C ABI declared in include/fdllm.h: every
-function takes torch tensors that already live on the GPU, checks their
+Thin marshalling of the C ABI declared in include/fdllm.h (by ctypes; the
+attention calls' by csrc/binding.cpp): every function takes torch tensors that already live on the GPU, checks their
 dtype/shape/contiguity, and passes raw device pointers plus the current HIP
 stream.  All arithmetic happens in the HIP kernels; there is no CPU fallback,
 and loading fails loudly when the library has not been built.
@@ -18,6 +18,7 @@ import torch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libfdllm.so")
 BENCH_LIB_PATH = os.path.join(_PKG, "libfdllm_bench.so")
+BINDING_PATH = os.path.join(_PKG, "_binding.so")
 
 BF16, F32 = 0, 1
 SEL_THRESHOLD, SEL_FACTOR, SEL_PROFILE, SEL_ROBUST = 0, 1, 2, 3
@@ -59,6 +60,7 @@ BENCH_EXPORTS = ("fdllm_stream_read",)
 
 _lib = None
 _bench_lib = None
+_native_module = None
 
 
 class FdllmError(RuntimeError):
@@ -118,7 +120,8 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.fdllm_prompt_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
     for name in ("fdllm_cache_tile_bytes", "fdllm_qk_norm_rope", "fdllm_cache_read",
                  "fdllm_cache_attention_workspace_size", "fdllm_cache_attention",
-                 "fdllm_prompt_attention_workspace_size", "fdllm_prompt_attention", "fdllm_confidence", "fdllm_reveal", "fdllm_decode_step", "fdllm_workspace_size",
+                 "fdllm_prompt_attention_workspace_size", "fdllm_prompt_attention",
+                 "fdllm_confidence", "fdllm_reveal", "fdllm_decode_step", "fdllm_workspace_size",
                  "fdllm_decode_step_static", "fdllm_check_inputs",
                  "fdllm_synth_logits", "fdllm_advance_blocks", "fdllm_generation_workspace_size",
                  "fdllm_lmhead_workspace_size", "fdllm_lmhead_confidence", "fdllm_lmhead_decode_step",
@@ -450,39 +453,26 @@ def select(selector: str, conf, eps, mask, block_start, block_end, param, commit
                                                     param, commit, n_commit)
 
 
-# The attention calls are made once a layer, on a few tokens at a time: their
-# checks look at each tensor once and pass plain numbers on.
-def _raw(t: torch.Tensor, dtype, shape, name: str) -> int:
-    """Address of a contiguous GPU tensor of this type and shape."""
-    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
-        return t.data_ptr()
-    _ptr(t, dtype, shape, name)
-    raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}")
+# The attention calls are made once a layer, on a few tokens at a time, where
+# checking and converting their arguments here would take longer than their
+# kernels: csrc/binding.cpp does that.
+def _native():
+    global _native_module
+    if _native_module is None:
+        load()
+        if not os.path.exists(BINDING_PATH):
+            raise FileNotFoundError(
+                f"{BINDING_PATH} is missing: build it first (python -m paper_2606_02955_amd.build)")
+        from . import _binding
+        _native_module = _binding
+    return _native_module
 
 
-def _opt(t: Optional[torch.Tensor], dtype, shape, name: str) -> int:
-    return 0 if t is None else _raw(t, dtype, shape, name)
-
-
-def _heads(t: torch.Tensor, shape, dtype, name: str):
-    """Address and token stride of [T, heads, D] whose tokens may lie apart."""
-    s = t.stride()
-    if (t.dtype is dtype and t.is_cuda and t.shape == shape and (s[1] == shape[2] or shape[1] == 1)
-            and (s[2] == 1 or shape[2] == 1)):
-        return t.data_ptr(), s[0] if shape[0] > 1 else shape[1] * shape[2]
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor")
-    if t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    raise ValueError(f"{name}: the heads of a token must lie side by side")
-
-
-def _three(t: torch.Tensor, name: str):
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be [tokens, heads, head size], got {tuple(t.shape)}")
-    return t.shape
+def _attention_status(status, where: str):
+    """A workspace (or None) as it is; a status raises."""
+    if type(status) is int and status != OK:
+        _check(status, where)
+    return status
 
 
 # The current stream's handle; torch.cuda.current_stream builds an object first,
@@ -491,21 +481,11 @@ _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _stream_of(t: torch.Tensor) -> int:
+    if not t.is_cuda:
+        return 0          # (the call refuses it)
     if _current_stream is not None:
         return _current_stream(t.get_device())
     return torch.cuda.current_stream(t.device).cuda_stream
-
-
-def _scratch(workspace: Optional[torch.Tensor], need: int, device):
-    """(workspace, its address, its bytes): the caller's, or a new one of the bytes needed."""
-    if workspace is None:
-        if need == 0:
-            return None, 0, 0
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        return workspace, workspace.data_ptr(), need
-    if not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous GPU tensor")
-    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 @functools.lru_cache(maxsize=None)
@@ -522,53 +502,17 @@ def new_cache(n_pages: int, kv_heads: int, head_dim: int, device=None) -> torch.
                        device=device if device is not None else "cuda")
 
 
-def _cache(cache: torch.Tensor, kv_heads: int, head_dim: int):
-    n_pages = cache.shape[0]
-    return _raw(cache, torch.uint8, (n_pages, kv_heads, fdllm_cache_tile_bytes(head_dim)), "cache"), n_pages
-
-
 def fdllm_qk_norm_rope(q, k, v, positions, cos_sin, q_out, k_out=None, q_weight=None, k_weight=None,
                        eps: float = 1e-6, interleaved: bool = False, cache=None, slots=None):
     """Head norm and rotation of q and k, keys and values into the cache, in one
     pass (see fdllm.h).  cos_sin None: no rotation; v is only read for a cache."""
-    T, H, D = _three(q, "q")
-    Hk, dt = _three(k, "k")[1], q.dtype
-    code = _dtype_code(q)
-    qp, qs = _heads(q, (T, H, D), dt, "q")
-    kp, ks = _heads(k, (T, Hk, D), dt, "k")
-    vp, vs, cp, n_pages, sp = 0, 0, 0, 0, 0
-    if cache is not None:
-        if v is None or slots is None:
-            raise ValueError("v and slots must be given with a cache")
-        vp, vs = _heads(v, (T, Hk, D), dt, "v")
-        cp, n_pages = _cache(cache, Hk, D)
-        sp = _raw(slots, torch.int32, (T,), "slots")
-    n_pos, rot, tp = 0, 0, 0
-    if cos_sin is not None:
-        n_pos, rot = cos_sin.shape
-        tp = _raw(cos_sin, torch.float32, (n_pos, rot), "cos_sin")
-    st = load().fdllm_qk_norm_rope(
-        qp, qs, kp, ks, vp, vs, code, T, H, Hk, D, _opt(q_weight, torch.float32, (D,), "q_weight"),
-        _opt(k_weight, torch.float32, (D,), "k_weight"), eps, _raw(positions, torch.int32, (T,), "positions"),
-        tp, n_pos, rot, 1 if interleaved else 0, _raw(q_out, dt, (T, H, D), "q_out"),
-        _opt(k_out, dt, (T, Hk, D), "k_out"), cp, n_pages, sp, _stream_of(q))
-    _check(st, "fdllm_qk_norm_rope")
+    _attention_status(_native().qk_norm_rope(q, k, v, positions, cos_sin, q_out, k_out, q_weight, k_weight, eps,
+                                             interleaved, cache, slots, _stream_of(q)), "fdllm_qk_norm_rope")
 
 
 def fdllm_cache_read(cache, slots, k_out=None, v_out=None):
     """What the cache holds for the given slots, as bfloat16 or float8_e5m2 (see fdllm.h)."""
-    like = k_out if k_out is not None else v_out
-    if like is None:
-        raise ValueError("k_out or v_out must be given")
-    T, Hk, D = _three(like, "k_out")
-    dt = like.dtype
-    if dt is not torch.bfloat16 and dt is not torch.float8_e5m2:
-        raise ValueError(f"the cache is read as bfloat16 or float8_e5m2, got {dt}")
-    cp, n_pages = _cache(cache, Hk, D)
-    st = load().fdllm_cache_read(
-        cp, n_pages, Hk, D, _raw(slots, torch.int32, (T,), "slots"), T, OUT_BF16 if dt is torch.bfloat16 else OUT_E5M2,
-        _opt(k_out, dt, (T, Hk, D), "k_out"), _opt(v_out, dt, (T, Hk, D), "v_out"), _stream_of(cache))
-    _check(st, "fdllm_cache_read")
+    _attention_status(_native().cache_read(cache, slots, k_out, v_out, _stream_of(cache)), "fdllm_cache_read")
 
 
 @functools.lru_cache(maxsize=4096)
@@ -584,21 +528,8 @@ def fdllm_cache_attention(q, cache, page_table, kv_len, cu_q, out, max_q: int, l
     """Attention of q's tokens over the 4-bit cache (see fdllm.h).  scale
     defaults to 1 / sqrt(head size); returns the workspace for reuse (None where
     the call needs none)."""
-    T, H, D = _three(q, "q")
-    Hk, i32 = cache.shape[1], torch.int32
-    B, width = page_table.shape
-    qp, qs = _heads(q, (T, H, D), torch.bfloat16, "q")
-    cp, n_pages = _cache(cache, Hk, D)
-    workspace, wp, wb = _scratch(
-        workspace, 0 if workspace is not None else fdllm_cache_attention_workspace_size(B, H, Hk, D, max_q, width),
-        q.device)
-    st = load().fdllm_cache_attention(
-        qp, qs, T, _raw(cu_q, i32, (B + 1,), "cu_q"), B, max_q, H, Hk, D, cp, n_pages,
-        _raw(page_table, i32, (B, width), "page_table"), width, _raw(kv_len, i32, (B,), "kv_len"),
-        _opt(q_start, i32, (B,), "q_start"), D ** -0.5 if scale is None else scale, blk,
-        _raw(out, torch.bfloat16, (T, H, D), "out"), _opt(lse, torch.float32, (T, H), "lse"), wp, wb, _stream_of(q))
-    _check(st, "fdllm_cache_attention")
-    return workspace
+    return _attention_status(_native().cache_attention(q, cache, page_table, kv_len, cu_q, out, max_q, lse, scale, blk,
+                                                       q_start, workspace, _stream_of(q)), "fdllm_cache_attention")
 
 
 @functools.lru_cache(maxsize=4096)
@@ -614,22 +545,8 @@ def fdllm_prompt_attention(q, k, v, cu_q, cu_k, out, max_q: int, lse=None, scale
                            blk: int = 0, workspace=None):
     """Attention of packed sequences (see fdllm.h); scale defaults to 1 / sqrt(head
     size); returns the workspace for reuse (None where the call needs none)."""
-    T, H, D = _three(q, "q")
-    Tk, Hk, _ = _three(k, "k")
-    bf16 = torch.bfloat16
-    qp, qs = _heads(q, (T, H, D), bf16, "q")
-    kp, ks = _heads(k, (Tk, Hk, D), bf16, "k")
-    vp, vs = _heads(v, (Tk, Hk, D), bf16, "v")
-    B = cu_q.shape[0] - 1
-    workspace, wp, wb = _scratch(
-        workspace, 0 if workspace is not None else fdllm_prompt_attention_workspace_size(B, T, Tk, H, Hk, D, max_q, blk),
-        q.device)
-    st = load().fdllm_prompt_attention(
-        qp, qs, kp, ks, vp, vs, T, Tk, _raw(cu_q, torch.int32, (B + 1,), "cu_q"),
-        _raw(cu_k, torch.int32, (B + 1,), "cu_k"), B, max_q, H, Hk, D, D ** -0.5 if scale is None else scale, blk,
-        _raw(out, bf16, (T, H, D), "out"), _opt(lse, torch.float32, (T, H), "lse"), wp, wb, _stream_of(q))
-    _check(st, "fdllm_prompt_attention")
-    return workspace
+    return _attention_status(_native().prompt_attention(q, k, v, cu_q, cu_k, out, max_q, lse, scale, blk, workspace,
+                                                        _stream_of(q)), "fdllm_prompt_attention")
 
 
 def load_bench(path: Optional[str] = None) -> ctypes.CDLL:

@@ -2,7 +2,8 @@
 
 libfdllm.so is the commit selector (include/fdllm.h); libfdllm_bench.so is
 the read-only HBM stream used as the bandwidth reference in reports
-(include/fdllm_bench.h).
+(include/fdllm_bench.h); _binding.so takes torch tensors to the attention calls
+(host code, the C++ compiler).
 """
 from __future__ import annotations
 
@@ -10,6 +11,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -24,6 +26,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libfdllm.so")
 BENCH_SRC = os.path.join(PKG, "csrc", "stream_read.hip")
 BENCH_LIB = os.path.join(PKG, "libfdllm_bench.so")
+BINDING_SRC = os.path.join(PKG, "csrc", "binding.cpp")
+BINDING = os.path.join(PKG, "_binding.so")
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [
@@ -53,21 +57,40 @@ def hipcc() -> str:
 
 def _compile(srcs, lib: str, verbose: bool, extra=()) -> str:
     tmp = lib + ".tmp"
-    cmd = [hipcc(), *HIPCC_FLAGS, *extra, "-I", INCLUDE, *srcs, "-o", tmp]
+    return _run([hipcc(), *HIPCC_FLAGS, *extra, "-I", INCLUDE, *srcs, "-o", tmp], tmp, lib, verbose)
+
+
+def _compile_binding(verbose: bool) -> str:
+    """_binding.so against the installed torch and the libfdllm.so beside it."""
+    import torch
+    from torch.utils import cpp_extension
+    tmp = BINDING + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", INCLUDE]
+    for path in (*cpp_extension.include_paths(), sysconfig.get_paths()["include"]):
+        cmd += ["-isystem", path]
+    cmd += [BINDING_SRC, "-o", tmp, "-L", PKG, "-lfdllm", "-L", os.path.join(os.path.dirname(torch.__file__), "lib"),
+            "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
+    return _run(cmd, tmp, BINDING, verbose)
+
+
+def _run(cmd, tmp: str, lib: str, verbose: bool) -> str:
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError(f"hipcc failed with status {res.returncode} on {srcs}")
+        raise RuntimeError(f"{cmd[0]} failed with status {res.returncode} on {lib}")
     os.replace(tmp, lib)
     return lib
 
 
 def build(verbose: bool = False, extra=()) -> str:
-    """Compile libfdllm.so and libfdllm_bench.so (always recompiles both)."""
+    """Compile libfdllm.so, libfdllm_bench.so and _binding.so (always all of them)."""
     _compile([BENCH_SRC], BENCH_LIB, verbose)
-    return _compile([SRC, LMHEAD_SRC, LOOP_SRC, STATIC_SRC, ROPE_SRC, CACHE_SRC, PROMPT_SRC], LIB, verbose, extra)
+    _compile([SRC, LMHEAD_SRC, LOOP_SRC, STATIC_SRC, ROPE_SRC, CACHE_SRC, PROMPT_SRC], LIB, verbose, extra)
+    _compile_binding(verbose)
+    return LIB
 
 
 if __name__ == "__main__":

@@ -15,7 +15,7 @@ HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))
 
 @pytest.fixture(scope="module")
 def lib():
-    if not os.path.exists(fd.LIB_PATH):
+    if not os.path.exists(fd.LIB_PATH) or not os.path.exists(fd.BINDING_PATH):
         from paper_2606_02955_amd import build
         build.build()
     return fd.load()
@@ -137,3 +137,21 @@ def test_binding_refuses(lib):
         fd.fdllm_prompt_attention(q, q, q[:, :, :32], cu, cu, q, 4)
     with pytest.raises(ValueError):
         fd.fdllm_cache_read(torch.zeros(2, 2, 100, dtype=torch.uint8), None)
+
+
+@pytest.mark.parametrize("call", ["rope", "read", "cache", "prompt"])
+def test_binding_refuses_what_is_no_tensor_or_has_no_heads(lib, call):
+    q, cu = torch.zeros(4, 4, 64, dtype=torch.bfloat16), torch.tensor([0, 4], dtype=torch.int32)
+    n = fd._native()
+    for bad in (None, 3, torch.zeros(4, 64, dtype=torch.bfloat16)):
+        with pytest.raises(ValueError):
+            if call == "rope":
+                n.qk_norm_rope(bad, q, q, cu, None, q, q, None, None, 1e-6, False, None, None, 0)
+            elif call == "read":
+                n.cache_read(bad, cu, q, None, 0)
+            elif call == "cache":
+                n.cache_attention(bad, q, cu, cu, cu, q, 4, None, None, 0, None, None, 0)
+            else:
+                n.prompt_attention(bad, q, q, cu, cu, q, 4, None, None, 0, None, 0)
+    with pytest.raises(TypeError):
+        n.cache_read(q, cu)
