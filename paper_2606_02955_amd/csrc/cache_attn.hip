@@ -450,6 +450,7 @@ k_cache_attn(const CacheAttnArgs a) {
         const i16x4 v1 = read_transposed(at + (MT == 32 ? 8 * S::RowBytes + (v_at[t] ^ 16) : 16 * S::RowBytes + v_at[t]));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
       };
+      __builtin_amdgcn_s_setprio(1);
       bf16x8 vf[3];
       vf[0] = value_operand(0);
       vf[1] = value_operand(1);
@@ -471,6 +472,7 @@ k_cache_attn(const CacheAttnArgs a) {
         }
         CA_FENCE();
       }
+      __builtin_amdgcn_s_setprio(0);
     }
     l = sum_row<MT>(l + l2);
 
