@@ -41,6 +41,7 @@ struct PromptArgs {
   float* lse;
   int tiles, splits;   // row tiles of max_q tokens; most parts that the keys of one are divided into
   int share;           // tiles of keys that a part is to have
+  int by_sequence;     // order of the workgroups (pa_by_sequence)
   float* part_ml;      // [row tile, h, split, wave][32][2]: reference and sum of a row's partial result
   float* part;         // [row tile, h, split, wave] tiles of partial sums (attn_common.h)
 };
@@ -126,8 +127,9 @@ k_prompt_attn(const PromptArgs a) {
 
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int col = lane % 32, part = lane / 32;
-  const int b = blockIdx.x / a.Hk, h = blockIdx.x % a.Hk;
-  const int tile = a.tiles - 1 - blockIdx.y;   // the rows that see most keys first
+  const int outer = blockIdx.x / a.Hk, h = blockIdx.x % a.Hk;
+  const int b = a.by_sequence ? blockIdx.y : outer;
+  const int tile = a.tiles - 1 - (a.by_sequence ? outer : blockIdx.y);   // the rows that see most keys first
   const PaTile pt = pa_tile(a, b, tile);
   if (tile * kPaRows >= pt.rows || (int)blockIdx.z >= pt.parts) return;
   const int nt = (pt.far + kPaKeys - 1) / kPaKeys;
@@ -490,6 +492,23 @@ static PaPlan pa_plan(int B, int T, int Tk, int H, int Hk, int D, int max_q, int
   return p;
 }
 
+// Workgroups run the longest row tiles of all sequences first, so that none is
+// left over in the end; but one sequence after another
+// - where many of those would be tiles that a shorter sequence does not have:
+//   workgroups are handed out in turn, and empty ones between the others leave
+//   the work to some of the CUs (four prompts of 1 to 4096 tokens 382 us by tile,
+//   230 by sequence; eight of 1 to 1024 53 and 45; six of 100 to 900 37 and 38);
+// - where the keys and values that an XCD's workgroups then have in use (a
+//   head's; from eight heads on it works on every eighth) exceed its cache (128
+//   prompts of 128 tokens, 8 heads, 8.4 MB: 107 us by tile, 98 by sequence).
+// Four of 500 to 777 tokens behind 2000, 2.7 MB: 40.4 us by tile, 42.8 by sequence.
+constexpr long long kPaCacheBytes = 4 << 20;
+
+static bool pa_by_sequence(int B, int T, int Tk, int Hk, int D, int max_q) {
+  if (B < 2 || B > 65535) return false;
+  return 4ll * T < 3ll * B * max_q || 4ll * Tk * D * ((Hk + 7) / 8) > kPaCacheBytes;
+}
+
 // The kernel's LDS is above the default limit; the limit is raised once per
 // device and kernel, before the first launch there.
 constexpr int kPaMaxDevices = 64;
@@ -507,8 +526,9 @@ static hipError_t pa_launch(const PromptArgs& a, hipStream_t st) {
     if (dev >= 0 && dev < kPaMaxDevices) allowed[dev].store(true, std::memory_order_release);
   }
   const unsigned bh = (unsigned)(a.B * a.Hk);
-  hipLaunchKernelGGL(k_prompt_attn<NG>, dim3(bh, (unsigned)a.tiles, (unsigned)a.splits), dim3(kPaThreads), S::LdsBytes,
-                     st, a);
+  const dim3 grid = a.by_sequence ? dim3((unsigned)(a.tiles * a.Hk), (unsigned)a.B, (unsigned)a.splits)
+                                  : dim3(bh, (unsigned)a.tiles, (unsigned)a.splits);
+  hipLaunchKernelGGL(k_prompt_attn<NG>, grid, dim3(kPaThreads), S::LdsBytes, st, a);
   if (a.splits > 1)
     hipLaunchKernelGGL(k_prompt_join<NG>, dim3(bh, (unsigned)(a.tiles * kPaWaves)), dim3(kPaThreads), 0, st, a);
   return hipGetLastError();
@@ -548,7 +568,7 @@ fdllm_status fdllm_prompt_attention(const void* q, int64_t q_stride, const void*
   char* ws = (char*)workspace;
   const PromptArgs a{(const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, q_stride, k_stride, v_stride, T, Tk,
                      cu_q, cu_k, B, H, Hk, H / Hk, max_q, blk, scale * kLog2e, (uint16_t*)out, lse, p.tiles, p.splits, p.share,
-                     (float*)ws, (float*)(ws + p.at_part)};
+                     pa_by_sequence(B, T, Tk, Hk, D, max_q), (float*)ws, (float*)(ws + p.at_part)};
   hipStream_t st = (hipStream_t)stream;
   const hipError_t e = D == 64 ? pa_launch<2>(a, st) : D == 96 ? pa_launch<3>(a, st) : pa_launch<4>(a, st);
   return e == hipSuccess ? FDLLM_OK : FDLLM_ERR_HIP;

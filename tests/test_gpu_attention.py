@@ -408,6 +408,9 @@ PROMPT_CASES = [
     (64, 2, 2, 0, [(40, 3000), (1, 1), (2, 1025)]),
     (96, 3, 1, 32, [(10, 2500)]),
     (128, 40, 8, 1, [(9, 9)] * 20),
+    (64, 4, 2, 32, [(1, 1), (150, 150), (9, 9), (40, 40), (0, 0)]),       # ragged: one sequence after another
+    (96, 2, 1, 1, [(1, 1), (3, 2600), (170, 170)]),                       # and with divided keys
+    (128, 1, 1, 0, [(20, 3000)] * 3),                                     # more keys than an XCD's cache holds
 ]
 
 
