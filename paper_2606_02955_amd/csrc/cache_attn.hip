@@ -16,6 +16,14 @@
 // Each workgroup takes an equal share of all units, whatever the sequences'
 // lengths; an item that lies in several shares is joined afterwards, in the
 // order of its pages.
+//
+// Tiles of 16 rows are bound by the read: two tokens over 99001 to 131072 keys
+// (8 heads of keys of 128) 43 us for 250 MB, 5.8 TB/s.  Tiles of 32 by the
+// instructions: 64 blocks of 32 tokens, four heads a key head, over 6000 to 8192
+// keys 250 us, 0.80 PFLOP/s, the matrix cores busy half of the time and the
+// vector units 58%, since a wave's scores, softmax and outputs follow one
+// another; to form the next page's scores beside this page's softmax takes more
+// registers than a wave has (measured with spills in the starts and ends: 300).
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>
@@ -680,6 +688,13 @@ k_cache_join(const CacheAttnArgs a, int wgs) {
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
+// Pages of an item up to which a set of waves takes them alone, where there is
+// one sequence: without parts there is no join, which costs as much as two or
+// three pages.  (32 heads, one token: 12.6 us divided and 9.3 whole at 1024 keys,
+// two pages a set; 13.3 and 12.7 at 2048, four; 15.6 and 20.3 at 4096, eight.
+// A block of 32: 14.6 and 12.3, 16.0 and 16.5, 22.0 and 24.9.)
+constexpr int kCaWholePages = 4;
+
 struct CaPlan {
   int mt, wr;        // variant
   int wgs;           // workgroups
@@ -713,6 +728,7 @@ static CaPlan ca_plan(int B, int H, int Hk, int D, int max_q, int table_w) {
   const long long items = (long long)B * p.items, most = items * ((table_w + wk - 1) / wk);
   const int fill = 256 * 8 / waves;
   p.wgs = (int)(most < fill ? (most < 1 ? 1 : most) : fill);
+  if (B == 1 && groups == 1 && items <= fill && table_w <= kCaWholePages * wk) p.wgs = (int)items;
   // None is split where there is one share, where an item has no more than a
   // page, or where one sequence of one group of rows has an item a share.  (With
   // more groups it may have fewer items than max_q stands for, and shares that

@@ -5,7 +5,13 @@
 //
 // The query tokens of a sequence times the query heads that share a key head
 // are the rows of one product; a workgroup takes 128 of them, a wave 32, over
-// tiles of 64 keys staged in LDS.
+// tiles of 64 keys staged in LDS: 32 rows a wave read each key's operand once for
+// 32 columns, and 64 KiB of LDS and 256 registers let two workgroups share a CU.
+//
+// Bound by the matrix cores: one causal prompt of 16384 tokens, 16 heads of 128
+// over 4, 962 to 1000 us, 1.10 to 1.14 PFLOP/s (a 16384^3 library product reaches
+// 1.37).  Short prompts by the starts and ends of the workgroups: 16384 tokens in
+// prompts of equal length take 88 us and 14 more for every 64 keys.
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>

@@ -114,6 +114,9 @@ __device__ __forceinline__ void write_octet(uint8_t* tile, int D, bool value, in
   if (o % 4 == 0) tile[(value ? v_scales_at(D) : k_scales_at(D)) + token * scale_stride(D) + g] = (uint8_t)byte;
 }
 
+// Bound by HBM: 14088 tokens of 32 + 8 + 8 heads of 128 in bfloat16, keys out and
+// into the cache, 76 us for 333 MB, 4.4 TB/s (a copy reaches 4.76).
+//
 // A workgroup takes 256 / lanes tokens of a few heads; `lanes` (8 up to D =
 // 128, 16 beyond) share a row.  A lane holds two octets of its row that rotate
 // against each other, with the cosines and sines and the norm's weights, which
@@ -258,7 +261,8 @@ k_rope(const RopeArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// what the cache holds: a thread per sixteen elements of a token's head
+// what the cache holds: a thread per sixteen elements of a token's head (14088
+// tokens of 8 heads 13.7 us for 44 MB)
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void store_held(__bf16* p, const bf16x2* x, bool nan) {
 #pragma unroll

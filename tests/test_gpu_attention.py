@@ -248,6 +248,10 @@ CACHE_CASES = [
     (96, 7, 1, 48, [(50, 100), (64, 64)]),
     (128, 5, 1, 0, [(70, 65), (2, 130), (70, 1)]),
     (64, 4, 1, 0, [(1, 20000)]),
+    (128, 4, 4, 1, [(1, 2048)]),                                         # one sequence: items whole up to four pages a set
+    (128, 4, 4, 1, [(1, 2049)]),
+    (96, 8, 2, 32, [(8, 1500)]),
+    (64, 7, 1, 0, [(8, 500)]),
     (64, 40, 8, 0, [(32, 20)] * 33),                                     # more items of one page than workgroups
     (64, 1, 1, 1, [(1, 1 + 7 * i) for i in range(300)]),                 # more sequences than threads
 ]
