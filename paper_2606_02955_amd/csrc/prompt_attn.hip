@@ -510,8 +510,9 @@ static PaPlan pa_plan(int B, int T, int Tk, int H, int Hk, int D, int max_q, int
 // Four of 500 to 777 tokens behind 2000, 2.7 MB: 40.4 us by tile, 42.8 by sequence.
 constexpr long long kPaCacheBytes = 4 << 20;
 
-static bool pa_by_sequence(int B, int T, int Tk, int Hk, int D, int max_q) {
-  if (B < 2 || B > 65535) return false;
+static bool pa_by_sequence(int B, int T, int Tk, int Hk, int D, int max_q, int tiles) {
+  // (what the grid has room for: 2^32 threads along the tiles, 65535 sequences)
+  if (B < 2 || B > 65535 || (long long)tiles * Hk > (1ll << 32) / kPaThreads - 1) return false;
   return 4ll * T < 3ll * B * max_q || 4ll * Tk * D * ((Hk + 7) / 8) > kPaCacheBytes;
 }
 
@@ -574,7 +575,7 @@ fdllm_status fdllm_prompt_attention(const void* q, int64_t q_stride, const void*
   char* ws = (char*)workspace;
   const PromptArgs a{(const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, q_stride, k_stride, v_stride, T, Tk,
                      cu_q, cu_k, B, H, Hk, H / Hk, max_q, blk, scale * kLog2e, (uint16_t*)out, lse, p.tiles, p.splits, p.share,
-                     pa_by_sequence(B, T, Tk, Hk, D, max_q), (float*)ws, (float*)(ws + p.at_part)};
+                     pa_by_sequence(B, T, Tk, Hk, D, max_q, p.tiles), (float*)ws, (float*)(ws + p.at_part)};
   hipStream_t st = (hipStream_t)stream;
   const hipError_t e = D == 64 ? pa_launch<2>(a, st) : D == 96 ? pa_launch<3>(a, st) : pa_launch<4>(a, st);
   return e == hipSuccess ? FDLLM_OK : FDLLM_ERR_HIP;
