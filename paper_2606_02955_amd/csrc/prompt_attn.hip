@@ -111,10 +111,12 @@ __device__ __forceinline__ i32x4 pa_rows(const uint16_t* p, int rows, long long 
 
 // 16 bytes a lane from rsrc + voff to LDS byte lds + 16 lane.  As inline
 // assembly, since the compiler would wait for it before every later LDS read;
-// pa_arrive is what waits.
+// pa_arrive is what waits.  The wait states are the ones that the compiler does
+// not put in here: one after the write of m0, five (with the two moves) after a
+// vector instruction that wrote a word of rsrc.
 __device__ __forceinline__ void pa_dma(i32x4 rsrc, uint32_t lds, uint32_t voff) {
   uint32_t keep;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
                "s_mov_b32 m0, %0"
                : "=&s"(keep) : "s"(lds), "v"(voff), "s"(rsrc) : "memory");
 }
