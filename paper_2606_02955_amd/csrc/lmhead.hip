@@ -277,18 +277,21 @@ __device__ __forceinline__ i32x4 lm_rsrc(const void* base, uint32_t bytes) {
 // one wave-wide 16-byte-per-lane load into LDS: lane i's vector lands at
 // byte lds + 16 i.  Issued as inline assembly: the compiler cannot tell which
 // buffer such a load writes and would drain every load in flight before the
-// next LDS read; the explicit vmcnt waits of lm_sync are the ones needed.
+// next LDS read; the explicit vmcnt waits of lm_sync are the ones needed.  The
+// wait states are the ones that it does not put in here: one after the write of
+// m0, five (with the two moves) after a vector instruction that wrote a word of
+// rsrc or soff.
 // NT: data that no other workgroup reads (nontemporal).
 template <bool NT>
 __device__ __forceinline__ void lm_dma(i32x4 rsrc, uint32_t lds, uint32_t voff, int soff) {
   int keep;   // m0 is the compiler's register: saved and restored around the load
   if constexpr (NT)
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\tbuffer_load_dwordx4 %2, %3, %4 offen nt lds\n\t"
-                 "s_mov_b32 m0, %0"
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\t"
+                 "buffer_load_dwordx4 %2, %3, %4 offen nt lds\n\ts_mov_b32 m0, %0"
                  : "=&s"(keep) : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
   else
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds\n\t"
-                 "s_mov_b32 m0, %0"
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\t"
+                 "buffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
                  : "=&s"(keep) : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
 }
 

@@ -10,7 +10,7 @@ import pytest
 
 from paper_2606_02955_amd import build
 
-SOURCES = ["prompt_attn.hip"]
+SOURCES = ["prompt_attn.hip", "lmhead.hip"]
 LOAD = re.compile(r"buffer_load_\w+ (?:v\d+|off), s\[(\d+):(\d+)\], (\S+) .*\blds\b")
 
 
