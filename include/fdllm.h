@@ -446,7 +446,8 @@ fdllm_status fdllm_workspace_size(int B, int L, int V, fdllm_dtype dtype, size_t
  * Packed sequences.  cu_q [B + 1] int32: sequence b has the rows
  *   [cu_q[b], cu_q[b + 1]) of the T.  A sequence whose two counts are not
  *   0 <= cu_q[b] <= cu_q[b + 1] <= T, or that has more than max_q rows, is
- *   left out: its rows of the outputs are not written.
+ *   left out: its rows of the outputs are not written.  Sequences may lie in
+ *   any order; a row that is in several gets the result of one of them.
  * Masks.  A query at position p of its sequence sees the keys
  *   j < min(len, (floor(p / blk) + 1) * blk): blk = 1 is the causal mask, blk
  *   = 32 that of decoding in blocks of 32, blk = 0 stands for no mask.  The

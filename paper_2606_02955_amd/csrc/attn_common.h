@@ -9,6 +9,7 @@
 
 #include <stdint.h>
 
+#include "attn_work.h"
 #include "fdllm.h"
 #include "pass_common.h"
 
@@ -52,14 +53,6 @@ __device__ __forceinline__ int visible_end(int p, int blk, int len) {
   if (p < 0) return 0;
   const long long e = ((long long)(p / blk) + 1) * blk;
   return e < len ? (int)e : len;
-}
-
-// Rows [s, e) of a packed tensor of T rows, as two cumulated counts give them;
-// anything else (or more than `most` rows) counts as a sequence without rows.
-__device__ __forceinline__ int packed_rows(const int32_t* cu, int b, int T, int most, int* first) {
-  const int s = cu[b], e = cu[b + 1];
-  *first = s;
-  return (s >= 0 && s <= e && e <= T && e - s <= most) ? e - s : 0;
 }
 
 // ---------------------------------------------------------------------------

@@ -26,7 +26,7 @@ namespace fdllm {
 
 constexpr int kPaThreads = 256;
 constexpr int kPaWaves = kPaThreads / kWave;
-constexpr int kPaRows = kPaWaves * 32;
+static_assert(kPaRows == kPaWaves * 32, "a wave 32 rows");
 constexpr int kPaKeys = 64;
 constexpr int kPaSplitTiles = 4;   // tiles of keys that a part of a split row tile has at least
 constexpr int kPaWholeTiles = 8;   // and those up to which none is split: joining costs a launch and 4 us
@@ -47,9 +47,10 @@ struct PromptArgs {
   float* lse;
   int tiles, splits;   // row tiles of max_q tokens; most parts that the keys of one are divided into
   int share;           // tiles of keys that a part is to have
+  int places;          // row tiles that there is room for, where keys are divided
   int by_sequence;     // order of the workgroups (pa_by_sequence)
-  float* part_ml;      // [row tile, h, split, wave][32][2]: reference and sum of a row's partial result
-  float* part;         // [row tile, h, split, wave] tiles of partial sums (attn_common.h)
+  float* part_ml;      // [place, h, split, wave][32][2]: reference and sum of a row's partial result
+  float* part;         // [place, h, split, wave] tiles of partial sums (attn_common.h)
 };
 
 // A tile of rows: 128 of a sequence's query tokens times the heads of a key head.
@@ -57,7 +58,7 @@ struct PaTile {
   int first, firstk, n, len, rows;
   int far;      // the most keys that any row sees
   int parts;    // into which its keys are divided
-  int place;    // among the row tiles of all sequences (with gaps)
+  int place;    // among the row tiles of all sequences, where parts > 1
 };
 
 __device__ __forceinline__ PaTile pa_tile(const PromptArgs& a, int b, int tile) {
@@ -73,7 +74,13 @@ __device__ __forceinline__ PaTile pa_tile(const PromptArgs& a, int b, int tile) 
   t.far = visible_end(t.len - t.n + last / a.R, a.blk, t.len);
   const int nt = (t.far + kPaKeys - 1) / kPaKeys;
   t.parts = nt <= max(kPaWholeTiles, 2 * a.share) ? 1 : min(a.splits, (nt + a.share - 1) / a.share);
-  t.place = (int)((long long)t.first * a.R / kPaRows) + b + tile;
+  if (t.parts > 1) {   // (a lane counts the tiles of every 64th sequence)
+    int before = pa_tiles_before(a.cu_q, b, a.T, a.max_q, a.R, threadIdx.x % kWave, kWave);
+#pragma unroll
+    for (int x = 1; x < kWave; x <<= 1) before += __shfl_xor(before, x);
+    t.place = __builtin_amdgcn_readfirstlane(before) + tile;
+    if (t.place >= a.places) t.parts = 1;   // tokens in several sequences: more row tiles than room
+  }
   return t;
 }
 
@@ -455,7 +462,7 @@ k_prompt_join(const PromptArgs a) {
 // host side
 // ---------------------------------------------------------------------------
 struct PaPlan {
-  int tiles, splits, share;
+  int tiles, splits, share, places;
   size_t at_part, bytes;
 };
 
@@ -480,7 +487,7 @@ static PaPlan pa_plan(int B, int T, int Tk, int H, int Hk, int D, int max_q, int
   p.splits = 1;
   p.share = kPaSplitTiles;
   if (B < 1 || p.tiles < 1) return p;
-  const long long places = (long long)T * R / kPaRows + B + 1;
+  const long long places = pa_places(B, T, R);
   const long long past = Tk > T ? (Tk - T) / B : 0;
   const long long keys = Tk / B - (blk && T < Tk + B ? T / B / 2 : 0);   // of a row, in the middle
   const long long units = ((long long)T * R + kPaRows - 1) / kPaRows * Hk * (keys / kPaKeys + 1);
@@ -494,6 +501,7 @@ static PaPlan pa_plan(int B, int T, int Tk, int H, int Hk, int D, int max_q, int
     p.splits = 1;
     return p;
   }
+  p.places = (int)places;
   const size_t rows = (size_t)places * Hk * p.splits * kPaRows;
   p.at_part = align256(rows * 8);
   p.bytes = p.at_part + rows * D * sizeof(float);
@@ -576,8 +584,9 @@ fdllm_status fdllm_prompt_attention(const void* q, int64_t q_stride, const void*
   if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return FDLLM_ERR_WORKSPACE;
   char* ws = (char*)workspace;
   const PromptArgs a{(const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, q_stride, k_stride, v_stride, T, Tk,
-                     cu_q, cu_k, B, H, Hk, H / Hk, max_q, blk, scale * kLog2e, (uint16_t*)out, lse, p.tiles, p.splits, p.share,
-                     pa_by_sequence(B, T, Tk, Hk, D, max_q, p.tiles), (float*)ws, (float*)(ws + p.at_part)};
+                     cu_q, cu_k, B, H, Hk, H / Hk, max_q, blk, scale * kLog2e, (uint16_t*)out, lse, p.tiles, p.splits,
+                     p.share, p.places, pa_by_sequence(B, T, Tk, Hk, D, max_q, p.tiles), (float*)ws,
+                     (float*)(ws + p.at_part)};
   hipStream_t st = (hipStream_t)stream;
   const hipError_t e = D == 64 ? pa_launch<2>(a, st) : D == 96 ? pa_launch<3>(a, st) : pa_launch<4>(a, st);
   return e == hipSuccess ? FDLLM_OK : FDLLM_ERR_HIP;
