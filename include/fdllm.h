@@ -456,7 +456,8 @@ fdllm_status fdllm_workspace_size(int B, int L, int V, fdllm_dtype dtype, size_t
  *   than keys).  A query that sees no key gets out = 0 and lse = -inf.
  * Values.  q, k, v of the rows of a sequence must be finite; whatever lies
  *   between sequences or behind one's end (in a page, or past kv_len) is never
- *   part of a result.
+ *   part of a result.  A query that has a NaN or sees a key with one gets NaN for
+ *   out and lse; a NaN among the values may reach queries that do not see it.
  *
  * The 4-bit cache: [n_pages, Hk, fdllm_cache_tile_bytes(D)] bytes, 16-byte
  * aligned.  A page holds FDLLM_CACHE_PAGE = 64 tokens; slot s is token s % 64

@@ -127,6 +127,14 @@ struct OutRows {
 
 constexpr float kLn2 = 0.69314718055994530942f;
 
+// The reciprocal and the logarithm of a row's sum l of weights 2^(x - ref): 0 and
+// -inf where no key was seen.  Told by the bits, since the build leaves NaN out of
+// comparisons' account: a row with a NaN gets NaN, not what stands for no keys.
+__device__ __forceinline__ float inverse_sum(float l) { return __float_as_uint(l) ? 1.0f / l : 0.0f; }
+__device__ __forceinline__ float log_sum(float ref, float l) {
+  return __float_as_uint(l) ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+}
+
 }  // namespace fdllm
 
 #endif  // FDLLM_ATTN_COMMON_H

@@ -525,10 +525,10 @@ k_cache_attn(const CacheAttnArgs a) {
           if (rr >= seq.n * a.R) break;
           const f32x4 v = joined(row / MT, row % MT, d);
           const float2 ml = joined_ml(row / MT, row % MT);
-          const float inv = ml.y > 0.0f ? 1.0f / ml.y : 0.0f;
+          const float inv = inverse_sum(ml.y);
           const size_t to_row = (size_t)(seq.first + rr / a.R) * a.H + h * a.R + rr % a.R;
           *(u32x2*)(a.out + to_row * D + d) = u32x2{pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
-          if (a.lse && d == 0) a.lse[to_row] = ml.y > 0.0f ? (ml.x + __builtin_amdgcn_logf(ml.y)) * kLn2 : kNegInf;
+          if (a.lse && d == 0) a.lse[to_row] = log_sum(ml.x, ml.y);
         }
       } else {
         for (int x = wave; x < WR * Quads; x += S::Waves) {
@@ -541,7 +541,7 @@ k_cache_attn(const CacheAttnArgs a) {
     } else if (whole) {
       // through LDS, so that a row leaves in one piece
       __syncthreads();
-      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+      const float inv = inverse_sum(l);
       uint8_t* lds = s_mem + wave * MT * OutRows<NG>::RowBytes;
 #pragma unroll
       for (int q = 0; q < Quads; ++q) {
@@ -551,7 +551,7 @@ k_cache_attn(const CacheAttnArgs a) {
       }
       __builtin_amdgcn_wave_barrier();
       const size_t at = (size_t)(seq.first + tok) * a.H + head;
-      if (row_ok && a.lse && part == 0) a.lse[at] = l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+      if (row_ok && a.lse && part == 0) a.lse[at] = log_sum(ref, l);
       for (int x = lane; x < MT * (D / 8); x += kWave) {
         const int row = x / (D / 8), d = 8 * (x % (D / 8)), rr = (group * WR + wr) * MT + row;
         if (rr >= seq.n * a.R) break;
@@ -662,7 +662,7 @@ k_cache_join(const CacheAttnArgs a, int wgs) {
     ref = to;
   }
   // out through LDS, so that a row leaves in one piece
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const float inv = inverse_sum(l);
   if (sp == 0) {
 #pragma unroll
     for (int i = 0; i < QPer; ++i) {
@@ -674,7 +674,7 @@ k_cache_join(const CacheAttnArgs a, int wgs) {
     const int r = r0 + col;
     if (set == 0 && part == 0 && a.lse && r < seq.n * a.R)
       a.lse[(size_t)(seq.first + r / a.R) * a.H + h * a.R + r % a.R] =
-          l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+          log_sum(ref, l);
   }
   __syncthreads();
   for (int x = threadIdx.x; x < MT * (D / 8); x += kCaJoinWaves * kWave) {

@@ -363,7 +363,7 @@ k_prompt_attn(const PromptArgs a) {
   if (pt.parts == 1) {
     // through LDS (where the keys were: nobody reads them any more), so that a
     // row leaves in one piece
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const float inv = inverse_sum(l);
     uint8_t* lds = s_mem + wave * 32 * OutRows<NG>::RowBytes;
 #pragma unroll
     for (int q = 0; q < Quads; ++q) {
@@ -373,7 +373,7 @@ k_prompt_attn(const PromptArgs a) {
     }
     __builtin_amdgcn_wave_barrier();
     if (row_ok && a.lse && part == 0)
-      a.lse[(size_t)(pt.first + tok) * a.H + head] = l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+      a.lse[(size_t)(pt.first + tok) * a.H + head] = log_sum(ref, l);
 #pragma unroll
     for (int j = 0; j < 32 * (D / 8) / kWave; ++j) {
       const int x = j * kWave + lane, row = x / (D / 8), d = 8 * (x % (D / 8)), rr = tile * kPaRows + wave * 32 + row;
@@ -441,14 +441,14 @@ k_prompt_join(const PromptArgs a) {
       for (int i = 0; i < QPer; ++i) acc[i] += v[k][i] * f;
     }
   }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const float inv = inverse_sum(l);
 #pragma unroll
   for (int i = 0; i < QPer; ++i)
     *(u32x2*)(s_out + OutRows<NG>::at(col, quad_element<32>(wave * QPer + i, part))) =
         u32x2{pack_bf16(acc[i][0] * inv, acc[i][1] * inv), pack_bf16(acc[i][2] * inv, acc[i][3] * inv)};
   if (wave == 0 && part == 0 && a.lse && r0 + col < pt.rows)
     a.lse[(size_t)(pt.first + (r0 + col) / a.R) * a.H + h * a.R + (r0 + col) % a.R] =
-        l > 0.0f ? (ref + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+        log_sum(ref, l);
   __syncthreads();
   for (int x = threadIdx.x; x < 32 * (D / 8); x += kPaThreads) {
     const int row = x / (D / 8), d = 8 * (x % (D / 8)), r = r0 + row;

@@ -43,3 +43,64 @@ def test_tokens_in_several_sequences_with_divided_keys(gpu):
     out, lse, ws = _prompt(gpu, q, k, v, [0, 64, 0, 64, 0, 64, 0, 64], [0, L, 0, L, 0, L, 0, L], 64)
     assert ws is not None
     _check(out, lse, oa.attend(_np(q.float()), _np(k.float()), _np(v.float()), D ** -0.5, 0, 0), D)
+
+
+def _cache_of(gpu, k, v):
+    """A cache of one sequence's keys and values, [T, Hk, D] float32, and its page table."""
+    T, Hk, D = k.shape
+    cache = gpu.new_cache(-(-T // 64), Hk, D)
+    gpu.fdllm_qk_norm_rope(k, k, v, _i32(np.zeros(T)), None, torch.empty_like(k), cache=cache, slots=_i32(range(T)))
+    return cache, torch.arange(cache.shape[0], dtype=torch.int32, device=DEV).view(1, -1)
+
+
+@pytest.mark.parametrize("D,H,Hk,n,T", [
+    (64, 4, 1, 1, 300), (128, 1, 1, 32, 300), (128, 2, 1, 30, 300),        # whole items: 16 rows, 32 rows, two waves by two
+    (96, 4, 1, 32, 100), (128, 4, 1, 32, 3000), (64, 2, 2, 1, 9000)])      # four waves of rows; divided items
+def test_nan_over_the_cache_is_not_an_empty_row(gpu, D, H, Hk, n, T):
+    k, v = (_normal((T, Hk, D), i) for i in range(2))
+    q = _normal((n, H, D), 3, torch.bfloat16)
+
+    def run(q, k, blk):
+        cache, table = _cache_of(gpu, k, v)
+        out, lse = torch.empty_like(q), torch.empty((n, H), device=DEV)
+        gpu.fdllm_cache_attention(q, cache, table, _i32([T]), _i32([0, n]), out, n, lse=lse, blk=blk)
+        torch.cuda.synchronize()
+        return out, lse
+
+    clean, clean_lse = run(q, k, 1)
+    bad_q = q.clone()
+    bad_q[n // 2, H - 1, 7] = float("nan")
+    out, lse = run(bad_q, k, 1)
+    hit = torch.zeros((n, H), dtype=torch.bool, device=DEV)
+    hit[n // 2, H - 1] = True
+    assert out[hit].isnan().all() and lse[hit].isnan().all()
+    assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit])
+    # a key that the later half of the tokens sees
+    bad_k = k.clone()
+    bad_k[T - 1 - (n - 1) // 2, 0, 9] = float("nan")
+    out, lse = run(q, bad_k, 1)
+    hit = torch.zeros((n, H), dtype=torch.bool, device=DEV)
+    hit[n - 1 - (n - 1) // 2:, :H // Hk] = True
+    assert out[hit].isnan().all() and lse[hit].isnan().all()
+    assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit])
+
+
+@pytest.mark.parametrize("D,H,n,T", [(128, 2, 100, 100), (64, 3, 5, 3000), (96, 1, 70, 2000)])
+def test_nan_in_a_prompt_is_not_an_empty_row(gpu, D, H, n, T):
+    q = _normal((n, H, D), 1, torch.bfloat16)
+    k, v = (_normal((T, 1, D), 2 + i, torch.bfloat16) for i in range(2))
+    clean, clean_lse, _ = _prompt(gpu, q, k, v, [0, n], [0, T], n, 1)
+    bad_q = q.clone()
+    bad_q[n // 2, H - 1, 7] = float("nan")
+    out, lse, _ = _prompt(gpu, bad_q, k, v, [0, n], [0, T], n, 1)
+    hit = torch.zeros((n, H), dtype=torch.bool, device=DEV)
+    hit[n // 2, H - 1] = True
+    assert out[hit].isnan().all() and lse[hit].isnan().all()
+    assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit])
+    bad_k = k.clone()
+    bad_k[T - 1 - (n - 1) // 2, 0, 9] = float("nan")
+    out, lse, _ = _prompt(gpu, q, bad_k, v, [0, n], [0, T], n, 1)
+    hit = torch.zeros((n, H), dtype=torch.bool, device=DEV)
+    hit[n - 1 - (n - 1) // 2:] = True
+    assert out[hit].isnan().all() and lse[hit].isnan().all()
+    assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit])
