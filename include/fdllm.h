@@ -527,7 +527,8 @@ fdllm_status fdllm_cache_read(const uint8_t* cache, int n_pages, int Hk, int D, 
  *   kv_len [B] int32: tokens in the cache (negative counts as 0, more than 64 *
  *   table_width as that);
  *   q_start [B] int32: position of a sequence's first query (NULL: kv_len less
- *   its number of queries); only blk > 0 looks at it;
+ *   its number of queries; the others follow, none beyond 2^31 - 1); only blk
+ *   > 0 looks at it;
  *   scale: > 0, usually 1 / sqrt(D);
  *   out [T, H, D] bf16; lse [T, H] float: log of the sum of exp(scale q.k) (may
  *   be NULL);

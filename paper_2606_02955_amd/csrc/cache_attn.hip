@@ -313,7 +313,8 @@ k_cache_attn(const CacheAttnArgs a) {
     const bool row_ok = r < seq.n * a.R;
     const int tok = row_ok ? r / a.R : 0, head = h * a.R + (row_ok ? r % a.R : 0);
     const int start = a.q_start ? a.q_start[b] : seq.len - seq.n;
-    const int end = row_ok ? visible_end(start + tok, a.blk, seq.len) : 0;
+    const int pos = start > INT32_MAX - tok ? INT32_MAX : start + tok;
+    const int end = row_ok ? visible_end(pos, a.blk, seq.len) : 0;
     int all_see = row_ok ? end : INT32_MAX;                 // keys that every row of the wave sees
 #pragma unroll
     for (int x = 1; x < MT; x <<= 1) all_see = min(all_see, __shfl_xor(all_see, x));

@@ -104,3 +104,22 @@ def test_nan_in_a_prompt_is_not_an_empty_row(gpu, D, H, n, T):
     hit[n - 1 - (n - 1) // 2:] = True
     assert out[hit].isnan().all() and lse[hit].isnan().all()
     assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit])
+
+
+@pytest.mark.parametrize("blk", [1, 32, 1 << 30])
+def test_query_positions_at_the_end_of_their_type(gpu, blk):
+    # positions past every key see all of them, also where counting on would leave 32 bits
+    D, H, n, T = 64, 2, 8, 150
+    k, v = (_normal((T, 1, D), i) for i in range(2))
+    cache, table = _cache_of(gpu, k, v)
+    q = _normal((2 * n, H, D), 2, torch.bfloat16)
+    out, lse = torch.empty_like(q), torch.empty((2 * n, H), device=DEV)
+    held = [torch.empty((T, 1, D), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    gpu.fdllm_cache_read(cache, _i32(range(T)), *held)
+    for start in ((2 ** 31 - 1, 2 ** 31 - 5), (-2 ** 31, 2 ** 31 - 8)):
+        gpu.fdllm_cache_attention(q, cache, table.expand(2, -1).contiguous(), _i32([T, T]), _i32([0, n, 2 * n]), out, n,
+                                  lse=lse, blk=blk, q_start=_i32(start))
+        torch.cuda.synchronize()
+        for rows, s in zip((slice(0, n), slice(n, 2 * n)), start):
+            want = oa.attend(_np(q[rows].float()), _np(held[0].float()), _np(held[1].float()), D ** -0.5, blk, s)
+            _check(out[rows], lse[rows], want, D)
