@@ -534,7 +534,11 @@ fdllm_status fdllm_cache_read(const uint8_t* cache, int n_pages, int Hk, int D, 
  *   be NULL);
  *   workspace: fdllm_cache_attention_workspace_size() bytes, 16-byte aligned
  *   (NULL where that is 0), scratch between calls.
- *   D: 64, 96 or 128.  bf16 rounding of the weights exp(s - max) and of out;
+ *   Sizes (FDLLM_ERR_SIZE beyond): D 64, 96 or 128; B at most 65535, H 2^15,
+ *   max_q * H / Hk 2^24; table_width and n_pages at most (2^31 - 1) / 64; with
+ *   G = ceil(max_q * H / Hk / 16), B * (table_width + 5) * G * Hk below 2e9;
+ *   max_q * H below about 2^28 where a table has more than one page.
+ *   bf16 rounding of the weights exp(s - max) and of out;
  *   scores, sums and maxima in float32.  For fixed sizes, lengths and tables a
  *   call is bitwise reproducible.
  */

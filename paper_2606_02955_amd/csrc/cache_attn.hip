@@ -744,6 +744,12 @@ static CaPlan ca_plan(int B, int H, int Hk, int D, int max_q, int table_w) {
   return p;
 }
 
+// The join's workgroups, one a wave's rows of an item, in what a launch has room
+// for: 2^32 threads.
+static bool ca_join_ok(const CaPlan& p) {
+  return !p.join || (long long)p.items * p.wr < (1ll << 32) / (kCaJoinWaves * kWave);
+}
+
 // The attention kernels' LDS is above the default limit; the limit is raised
 // once per device and kernel, before the first launch there.
 constexpr int kCaMaxDevices = 64;
@@ -786,7 +792,9 @@ fdllm_status fdllm_cache_attention_workspace_size(int B, int H, int Hk, int D, i
                                                   size_t* bytes) {
   if (!bytes || B < 0 || H < 1 || Hk < 1 || max_q < 0 || table_width < 0) return FDLLM_ERR_INVALID_ARG;
   if (!ca_sizes_ok(B, H, Hk, D, max_q, table_width, 0)) return FDLLM_ERR_SIZE;
-  *bytes = ca_plan(B, H, Hk, D, max_q, table_width).bytes;
+  const CaPlan p = ca_plan(B, H, Hk, D, max_q, table_width);
+  if (!ca_join_ok(p)) return FDLLM_ERR_SIZE;
+  *bytes = p.bytes;
   return FDLLM_OK;
 }
 
@@ -805,6 +813,7 @@ fdllm_status fdllm_cache_attention(const void* q, int64_t q_stride, int T, const
   for (const void* p : {q, (const void*)cache, (const void*)out, (const void*)workspace})
     if ((uintptr_t)p & 15) return FDLLM_ERR_INVALID_ARG;
   const CaPlan p = ca_plan(B, H, Hk, D, max_q, table_width);
+  if (!ca_join_ok(p)) return FDLLM_ERR_SIZE;
   if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return FDLLM_ERR_WORKSPACE;
   char* ws = (char*)workspace;
   const CacheAttnArgs a{(const uint16_t*)q, q_stride, T, cache, n_pages, page_table, table_width, kv_len, cu_q,

@@ -1,0 +1,38 @@
+"""What the attention calls refuse for its size: a launch that would not fit is
+refused before anything is enqueued, and nothing smaller is."""
+import ctypes
+import os
+
+import pytest
+
+import paper_2606_02955_amd as fd
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(fd.LIB_PATH):
+        from paper_2606_02955_amd import build
+        build.build()
+    return fd.load()
+
+
+P = ctypes.c_void_p(0x1000)      # never dereferenced: checks fail first
+
+
+def _cache_status(lib, B, H, Hk, max_q, width, call):
+    if not call:
+        n = ctypes.c_size_t(0)
+        return lib.fdllm_cache_attention_workspace_size(B, H, Hk, 64, max_q, width, ctypes.byref(n))
+    return lib.fdllm_cache_attention(P, H * 64, 6, P, B, max_q, H, Hk, 64, P, 3, P, width, P, None, 0.1, 0, P, None, P,
+                                     1 << 60, None)
+
+
+@pytest.mark.parametrize("B,H,Hk,max_q,width,ok", [
+    (1, 32, 32, 1 << 23, 2, False),        # the join's 2^23 workgroups of 512
+    (1, 32, 32, (1 << 23) - 128, 2, True),
+    (1, 32, 32, 1 << 23, 1, True),         # tables of one page: no join
+])
+def test_cache_attention_join_has_room(lib, B, H, Hk, max_q, width, ok):
+    assert _cache_status(lib, B, H, Hk, max_q, width, False) == (fd.OK if ok else fd.ERR_SIZE)
+    if not ok:
+        assert _cache_status(lib, B, H, Hk, max_q, width, True) == fd.ERR_SIZE
