@@ -538,9 +538,9 @@ fdllm_status fdllm_cache_read(const uint8_t* cache, int n_pages, int Hk, int D, 
  *   max_q * H / Hk 2^24; table_width and n_pages at most (2^31 - 1) / 64; with
  *   G = ceil(max_q * H / Hk / 16), B * (table_width + 5) * G * Hk below 2e9;
  *   max_q * H below about 2^28 where a table has more than one page.
- *   bf16 rounding of the weights exp(s - max) and of out;
- *   scores, sums and maxima in float32.  For fixed sizes, lengths and tables a
- *   call is bitwise reproducible.
+ *   bf16 rounding of the weights exp(s - max) and of out; scores, sums and
+ *   maxima in float32.  For fixed sizes, lengths and tables a call is bitwise
+ *   reproducible.
  */
 fdllm_status fdllm_cache_attention_workspace_size(int B, int H, int Hk, int D, int max_q, int table_width,
                                                   size_t* bytes);
@@ -557,6 +557,8 @@ fdllm_status fdllm_cache_attention(const void* q, int64_t q_stride, int T, const
  * queries where its first tokens are done).  workspace:
  * fdllm_prompt_attention_workspace_size() bytes, 16-byte aligned (NULL where
  * that is 0).  Other arguments as above.
+ *   Sizes (FDLLM_ERR_SIZE beyond): D 64, 96 or 128; H at most 2^15; B * Hk below
+ *   2^24; max_q * H / Hk at most 2097024; k_stride and v_stride at most 16776959.
  */
 fdllm_status fdllm_prompt_attention_workspace_size(int B, int T, int Tk, int H, int Hk, int D, int max_q, int blk,
                                                    size_t* bytes);

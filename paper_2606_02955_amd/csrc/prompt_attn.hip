@@ -471,7 +471,8 @@ constexpr int64_t kPaMaxStride = INT32_MAX / (2 * kPaKeys) - 256;
 
 static bool pa_sizes_ok(int B, int H, int Hk, int D, int max_q) {
   if ((D != 64 && D != 96 && D != 128) || H % Hk || H > (1 << 15)) return false;
-  return (long long)B * Hk <= INT32_MAX && (long long)max_q * (H / Hk) <= 65535ll / kPaWaves * kPaRows;
+  if ((long long)B * Hk >= (1ll << 32) / kPaThreads) return false;   // threads along a launch's first axis
+  return (long long)max_q * (H / Hk) <= 65535ll / kPaWaves * kPaRows;
 }
 
 // A row tile's keys are divided where the longest tile would run on while the

@@ -36,3 +36,28 @@ def test_cache_attention_join_has_room(lib, B, H, Hk, max_q, width, ok):
     assert _cache_status(lib, B, H, Hk, max_q, width, False) == (fd.OK if ok else fd.ERR_SIZE)
     if not ok:
         assert _cache_status(lib, B, H, Hk, max_q, width, True) == fd.ERR_SIZE
+
+
+def _prompt_status(lib, B, T, H, Hk, max_q, call, k_stride=None):
+    if not call:
+        n = ctypes.c_size_t(0)
+        return lib.fdllm_prompt_attention_workspace_size(B, T, T, H, Hk, 64, max_q, 1, ctypes.byref(n))
+    stride = k_stride or Hk * 64
+    return lib.fdllm_prompt_attention(P, H * 64, P, stride, P, stride, T, T, P, P, B, max_q, H, Hk, 64, 0.1, 1, P, None, P,
+                                      1 << 60, None)
+
+
+@pytest.mark.parametrize("B,H,Hk,ok", [
+    (1 << 19, 32, 32, False),              # a workgroup of 256 for every sequence and key head: 2^32 threads
+    ((1 << 19) - 1, 32, 32, True),
+    (1 << 24, 1, 1, False),
+    ((1 << 24) - 1, 1, 1, True),
+])
+def test_prompt_attention_has_room(lib, B, H, Hk, ok):
+    assert _prompt_status(lib, B, 1 << 20, H, Hk, 4, False) == (fd.OK if ok else fd.ERR_SIZE)
+    if not ok:
+        assert _prompt_status(lib, B, 1 << 20, H, Hk, 4, True) == fd.ERR_SIZE
+
+
+def test_prompt_attention_strides(lib):
+    assert _prompt_status(lib, 1, 64, 4, 4, 64, True, k_stride=16776960) == fd.ERR_SIZE
