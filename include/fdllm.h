@@ -558,7 +558,7 @@ fdllm_status fdllm_cache_attention(const void* q, int64_t q_stride, int T, const
  * fdllm_prompt_attention_workspace_size() bytes, 16-byte aligned (NULL where
  * that is 0).  Other arguments as above.
  *   Sizes (FDLLM_ERR_SIZE beyond): D 64, 96 or 128; H at most 2^15; B * Hk below
- *   2^24; max_q * H / Hk at most 2097024; k_stride and v_stride at most 16776959.
+ *   2^24; min(max_q, T) * H / Hk at most 8388480; k_stride and v_stride at most 16776959.
  */
 fdllm_status fdllm_prompt_attention_workspace_size(int B, int T, int Tk, int H, int Hk, int D, int max_q, int blk,
                                                    size_t* bytes);

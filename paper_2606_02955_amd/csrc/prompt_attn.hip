@@ -45,7 +45,7 @@ struct PromptArgs {
   float c;
   uint16_t* out;
   float* lse;
-  int tiles, splits;   // row tiles of max_q tokens; most parts that the keys of one are divided into
+  int tiles, splits;   // row tiles of the longest sequence; most parts that the keys of one are divided into
   int share;           // tiles of keys that a part is to have
   int places;          // row tiles that there is room for, where keys are divided
   int by_sequence;     // order of the workgroups (pa_by_sequence)
@@ -469,10 +469,15 @@ struct PaPlan {
 // a tile's rows are addressed by 32-bit byte offsets
 constexpr int64_t kPaMaxStride = INT32_MAX / (2 * kPaKeys) - 256;
 
-static bool pa_sizes_ok(int B, int H, int Hk, int D, int max_q) {
+// Row tiles of a sequence of n query tokens.
+static long long pa_tiles(int n, int R) { return ((long long)n * R + kPaRows - 1) / kPaRows; }
+
+static bool pa_sizes_ok(int B, int T, int H, int Hk, int D, int max_q) {
   if ((D != 64 && D != 96 && D != 128) || H % Hk || H > (1 << 15)) return false;
   if ((long long)B * Hk >= (1ll << 32) / kPaThreads) return false;   // threads along a launch's first axis
-  return (long long)max_q * (H / Hk) <= 65535ll / kPaWaves * kPaRows;
+  // workgroups along its second; the join has kPaWaves times as many, but keys are
+  // divided only where there are few row tiles (kPaMaxParts)
+  return pa_tiles(max_q < T ? max_q : T, H / Hk) <= 65535;
 }
 
 // A row tile's keys are divided where the longest tile would run on while the
@@ -484,7 +489,8 @@ static bool pa_sizes_ok(int B, int H, int Hk, int D, int max_q) {
 static PaPlan pa_plan(int B, int T, int Tk, int H, int Hk, int D, int max_q, int blk) {
   PaPlan p{};
   const int R = H / Hk;
-  p.tiles = (int)(((long long)max_q * R + kPaRows - 1) / kPaRows);
+  if (max_q > T) max_q = T;   // no sequence is longer than all of them
+  p.tiles = (int)pa_tiles(max_q, R);
   p.splits = 1;
   p.share = kPaSplitTiles;
   if (B < 1 || p.tiles < 1) return p;
@@ -561,7 +567,7 @@ extern "C" {
 fdllm_status fdllm_prompt_attention_workspace_size(int B, int T, int Tk, int H, int Hk, int D, int max_q, int blk,
                                                    size_t* bytes) {
   if (!bytes || B < 0 || T < 0 || Tk < 0 || blk < 0 || H < 1 || Hk < 1 || max_q < 0) return FDLLM_ERR_INVALID_ARG;
-  if (!pa_sizes_ok(B, H, Hk, D, max_q)) return FDLLM_ERR_SIZE;
+  if (!pa_sizes_ok(B, T, H, Hk, D, max_q)) return FDLLM_ERR_SIZE;
   *bytes = pa_plan(B, T, Tk, H, Hk, D, max_q, blk).bytes;
   return FDLLM_OK;
 }
@@ -572,7 +578,7 @@ fdllm_status fdllm_prompt_attention(const void* q, int64_t q_stride, const void*
                                     void* workspace, size_t workspace_bytes, fdllm_stream stream) {
   if (T < 0 || Tk < 0 || B < 0 || max_q < 0 || H < 1 || Hk < 1 || blk < 0) return FDLLM_ERR_INVALID_ARG;
   if (!(scale > 0.0f) || scale > 3.0e38f) return FDLLM_ERR_INVALID_ARG;
-  if (!pa_sizes_ok(B, H, Hk, D, max_q)) return FDLLM_ERR_SIZE;
+  if (!pa_sizes_ok(B, T, H, Hk, D, max_q)) return FDLLM_ERR_SIZE;
   if (T == 0 || B == 0 || max_q == 0) return FDLLM_OK;
   if (!q || !cu_q || !cu_k || !out || (Tk > 0 && (!k || !v))) return FDLLM_ERR_INVALID_ARG;
   if (q_stride < (int64_t)H * D || k_stride < (int64_t)Hk * D || v_stride < (int64_t)Hk * D || q_stride % 8 ||

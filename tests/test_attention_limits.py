@@ -61,3 +61,21 @@ def test_prompt_attention_has_room(lib, B, H, Hk, ok):
 
 def test_prompt_attention_strides(lib):
     assert _prompt_status(lib, 1, 64, 4, 4, 64, True, k_stride=16776960) == fd.ERR_SIZE
+
+
+@pytest.mark.parametrize("T,H,Hk,max_q,ok", [
+    (65536, 32, 1, 65536, True),           # 16384 row tiles
+    (262140, 32, 1, 262140, True),         # 65535
+    (262141, 32, 1, 262141, False),
+    (100, 32, 1, 1 << 30, True),           # no sequence is longer than all tokens
+])
+def test_prompt_attention_row_tiles(lib, T, H, Hk, max_q, ok):
+    assert _prompt_status(lib, 1, T, H, Hk, max_q, False) == (fd.OK if ok else fd.ERR_SIZE)
+    if not ok:
+        assert _prompt_status(lib, 1, T, H, Hk, max_q, True) == fd.ERR_SIZE
+
+
+def test_room_for_more_queries_than_there_are_costs_no_workspace(lib):
+    size = fd.fdllm_prompt_attention_workspace_size
+    for B, T, Tk, H, Hk, blk in ((3, 700, 700, 5, 1, 1), (1, 40, 6000, 8, 2, 0), (4, 2000, 2000, 32, 8, 1)):
+        assert size(B, T, Tk, H, Hk, 128, 1 << 30, blk) == size(B, T, Tk, H, Hk, 128, T, blk)

@@ -123,3 +123,24 @@ def test_query_positions_at_the_end_of_their_type(gpu, blk):
         for rows, s in zip((slice(0, n), slice(n, 2 * n)), start):
             want = oa.attend(_np(q[rows].float()), _np(held[0].float()), _np(held[1].float()), D ** -0.5, blk, s)
             _check(out[rows], lse[rows], want, D)
+
+
+def test_prompt_with_many_row_tiles(gpu):
+    # 65536 tokens of 32 heads on one key head: 16384 row tiles; some of the rows
+    D, H, T = 64, 32, 65536
+    q = _normal((T, H, D), 1, torch.bfloat16)
+    k, v = (_normal((T, 1, D), 2 + i, torch.bfloat16) for i in range(2))
+    out, lse, _ = _prompt(gpu, q, k, v, [0, T], [0, T], T, 1)
+    assert not out.isnan().any() and not lse.isnan().any()
+    kn, vn = _np(k.float()), _np(v.float())
+    for t in (0, 1, 127, 40000, 65532, 65535):
+        _check(out[t:t + 1], lse[t:t + 1], oa.attend(_np(q[t:t + 1].float()), kn, vn, D ** -0.5, 1, t), D)
+
+
+def test_prompt_with_room_for_more_queries_than_there_are(gpu):
+    D, H = 64, 4
+    q = _normal((133, H, D), 1, torch.bfloat16)
+    k, v = (_normal((133, 2, D), 2 + i, torch.bfloat16) for i in range(2))
+    out, lse, _ = _prompt(gpu, q, k, v, [0, 100, 133], [0, 100, 133], 100, 1)
+    more, more_lse, _ = _prompt(gpu, q, k, v, [0, 100, 133], [0, 100, 133], 1 << 30, 1)
+    assert torch.equal(out, more) and torch.equal(lse, more_lse)
