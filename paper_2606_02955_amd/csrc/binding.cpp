@@ -95,6 +95,14 @@ float real(PyObject* o, const char* name) {
   }
   return (float)v;
 }
+bool truth(PyObject* o, const char* name) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) {
+    PyErr_Clear();
+    throw std::invalid_argument(std::string(name) + " must be true or false");
+  }
+  return v != 0;
+}
 fdllm_stream stream_of(PyObject* o) { return (fdllm_stream)PyLong_AsVoidPtr(o); }
 
 uint8_t* cache_of(PyObject* o, int64_t Hk, int64_t D, int* n_pages) {
@@ -192,7 +200,7 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* q_out = at_of(a[5], type, {T, H, D}, "q_out");
     void* k_out = at_or_null(a[6], type, {T, Hk, D}, "k_out");
     const float eps = real(a[9], "eps");
-    const int inter = PyObject_IsTrue(a[10]) == 1, t32 = whole(T, "tokens"), h32 = whole(H, "heads"),
+    const int inter = truth(a[10], "interleaved"), t32 = whole(T, "tokens"), h32 = whole(H, "heads"),
               hk32 = whole(Hk, "heads"), d32 = whole(D, "head size");
     const fdllm_stream st = stream_of(a[13]);
     return PyLong_FromLong(unlocked([&] {
