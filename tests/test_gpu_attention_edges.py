@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from oracle import attention as oa
-from test_gpu_attention import _check, _i32, _normal, _np
+from test_gpu_attention import _check, _i32, _normal, _np, _run_cache, _want
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -144,3 +144,30 @@ def test_prompt_with_room_for_more_queries_than_there_are(gpu):
     out, lse, _ = _prompt(gpu, q, k, v, [0, 100, 133], [0, 100, 133], 100, 1)
     more, more_lse, _ = _prompt(gpu, q, k, v, [0, 100, 133], [0, 100, 133], 1 << 30, 1)
     assert torch.equal(out, more) and torch.equal(lse, more_lse)
+
+
+def _ragged(B, n, longest, seed):
+    """B sequences of at most n queries and `longest` cached tokens, some without either."""
+    g = np.random.default_rng(seed)
+    seqs = [(int(g.integers(1, n + 1)), int(g.integers(1, longest + 1))) for _ in range(B)]
+    for i in range(0, B, 17):
+        seqs[i] = (0, seqs[i][1])
+    for i in range(5, B, 23):
+        seqs[i] = (seqs[i][0], 0)
+    seqs[1] = (n, longest)
+    return seqs
+
+
+@pytest.mark.parametrize("D,H,Hk,blk,B,n,longest", [
+    (64, 1, 1, 1, 1100, 1, 200),         # 8 waves, 512 threads: up to three sequences a thread
+    (64, 2, 2, 0, 600, 1, 400),
+    (64, 4, 4, 32, 520, 20, 130),        # tiles of 32 rows
+    (64, 8, 1, 1, 300, 8, 500),          # two waves of rows: 256 threads, up to two sequences a thread
+    (64, 8, 1, 0, 300, 16, 500),         # four waves of rows
+    (96, 6, 1, 32, 100, 8, 700),         # more sequences than a wave has lanes, one a thread
+    (128, 8, 1, 0, 65, 16, 300),
+    (64, 5, 1, 1, 256, 40, 200)])        # several groups of rows, a sequence a thread
+def test_cache_attention_of_many_sequences(gpu, D, H, Hk, blk, B, n, longest):
+    q, kv, cu, out, lse, _, _ = _run_cache(gpu, D, H, Hk, blk, _ragged(B, n, longest, B + n), B)
+    torch.cuda.synchronize()
+    _check(out, lse, _want(q, kv, cu, blk, D), D)
