@@ -277,22 +277,23 @@ __device__ __forceinline__ i32x4 lm_rsrc(const void* base, uint32_t bytes) {
 // one wave-wide 16-byte-per-lane load into LDS: lane i's vector lands at
 // byte lds + 16 i.  Issued as inline assembly: the compiler cannot tell which
 // buffer such a load writes and would drain every load in flight before the
-// next LDS read; the explicit vmcnt waits of lm_sync are the ones needed.  The
-// wait states are the ones that it does not put in here: one after the write of
-// m0, five (with the two moves) after a vector instruction that wrote a word of
-// rsrc or soff.
+// next LDS read; the explicit vmcnt waits of lm_sync are the ones needed.  It
+// puts no wait states in here either: one is needed after the write of m0, and
+// five, the two moves among them, after a vector instruction that writes a word
+// of rsrc or soff (tests/test_lds_loads.py counts them in the assembly); Nops of
+// those on top where a soff may come from one right before.
 // NT: data that no other workgroup reads (nontemporal).
-template <bool NT>
+template <bool NT, int Nops>
 __device__ __forceinline__ void lm_dma(i32x4 rsrc, uint32_t lds, uint32_t voff, int soff) {
   int keep;   // m0 is the compiler's register: saved and restored around the load
   if constexpr (NT)
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\t"
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop %5\n\t"
                  "buffer_load_dwordx4 %2, %3, %4 offen nt lds\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep) : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
+                 : "=&s"(keep) : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff), "n"(Nops) : "memory");
   else
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\t"
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop %5\n\t"
                  "buffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep) : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
+                 : "=&s"(keep) : "s"(lds), "v"(voff), "s"(rsrc), "s"(soff), "n"(Nops) : "memory");
 }
 
 // waits until at most N of this wave's loads are outstanding and its LDS
@@ -343,6 +344,7 @@ struct LmProducer {
   int hks, hleft, hbuf;           // hidden stages
   i32x4 wr, hr;
   uint32_t w_voff[kLmWDma], h_voff[Sh::HDma];
+  int woff, hoff;                 // interleaved: byte offsets of the stages within a row
   uint32_t lds_w, lds_h;          // the wave's LDS offsets within a stage
 };
 
@@ -419,16 +421,38 @@ __device__ __forceinline__ void lm_segment(const LmArgs& a, const int32_t* rows,
   }
   lm_tile_setup(pr, a.weight, v_beg, v_end, d);
 
+  // Byte offsets of the stages to load within a row.  The interleaved schedule
+  // has them in scalar registers a stage ahead, so that its loads need no more
+  // wait states for them (4096 candidates, d = 4096, V = 126464: 3156 us with two
+  // more a load, 3053 so); the others form them load by load (128 candidates:
+  // 178 us, 181 a stage ahead).
+  auto offset_w = [&]() { return __builtin_amdgcn_readfirstlane((pr.ks ^ flip) * kLmRowBytes); };
+  auto offset_h = [&]() { return __builtin_amdgcn_readfirstlane((pr.hks ^ flip) * kLmRowBytes); };
+  auto place_w = [&]() {
+    if constexpr (kInterleaved) {
+      pr.woff = offset_w();
+      asm volatile("" : "+s"(pr.woff));   // there from here on
+    }
+  };
+  auto place_h = [&]() {
+    if constexpr (kInterleaved) {
+      pr.hoff = offset_h();
+      asm volatile("" : "+s"(pr.hoff));
+    }
+  };
+  place_w();
+  place_h();
+
   // the loads of the producers' stages: H j (j < HDma) of the hidden
   // producer, then W j - HDma of the weight producer
   auto dma = [&](int j) {
     if (j < Sh::HDma)
-      lm_dma<false>(pr.hr, pr.lds_h + (uint32_t)(pr.hbuf * Sh::HBytes + j * kWave * 16), pr.h_voff[j],
-                    __builtin_amdgcn_readfirstlane((pr.hks ^ flip) * kLmRowBytes));
+      lm_dma<false, kInterleaved ? 0 : 2>(
+          pr.hr, pr.lds_h + (uint32_t)(pr.hbuf * Sh::HBytes + j * kWave * 16), pr.h_voff[j],
+          kInterleaved ? pr.hoff : offset_h());
     else
-      lm_dma<NT>(pr.wr, pr.lds_w + (uint32_t)(pr.buf * kLmWBytes + (j - Sh::HDma) * kWave * 16),
-                 pr.w_voff[j - Sh::HDma],
-                 __builtin_amdgcn_readfirstlane((pr.ks ^ flip) * kLmRowBytes));
+      lm_dma<NT, 0>(pr.wr, pr.lds_w + (uint32_t)(pr.buf * kLmWBytes + (j - Sh::HDma) * kWave * 16),
+                    pr.w_voff[j - Sh::HDma], kInterleaved ? pr.woff : offset_w());
   };
   auto advance_w = [&]() {
     if (pr.left > 1) {
@@ -439,6 +463,7 @@ __device__ __forceinline__ void lm_segment(const LmArgs& a, const int32_t* rows,
         lm_tile_setup(pr, a.weight, v_beg + pr.tile * kLmVt, v_end, d);
       }
     }
+    place_w();
     pr.buf = pr.buf + 1 == Sh::WB ? 0 : pr.buf + 1;
   };
   auto advance_h = [&]() {
@@ -446,6 +471,7 @@ __device__ __forceinline__ void lm_segment(const LmArgs& a, const int32_t* rows,
       --pr.hleft;
       if (++pr.hks == nks) pr.hks = 0;
     }
+    place_h();
     pr.hbuf = pr.hbuf + 1 == Sh::HB ? 0 : pr.hbuf + 1;
   };
 
