@@ -458,6 +458,7 @@ fdllm_status fdllm_workspace_size(int B, int L, int V, fdllm_dtype dtype, size_t
  *   between sequences or behind one's end (in a page, or past kv_len) is never
  *   part of a result.  A query that has a NaN or sees a key with one gets NaN for
  *   out and lse; a NaN among the values may reach queries that do not see it.
+ *   scale q.k must stay below 2^30 in magnitude (the exponents' float32).
  *
  * The 4-bit cache: [n_pages, Hk, fdllm_cache_tile_bytes(D)] bytes, 16-byte
  * aligned.  A page holds FDLLM_CACHE_PAGE = 64 tokens; slot s is token s % 64
@@ -475,7 +476,8 @@ fdllm_status fdllm_workspace_size(int B, int L, int V, fdllm_dtype dtype, size_t
  */
 #define FDLLM_CACHE_PAGE 64
 
-/* Bytes of one page of one head; D a multiple of 32, 32 to 256. */
+/* Bytes of one page of one head; D a multiple of 32, 32 to 256 (of which the
+ * attention below takes 64, 96 and 128). */
 fdllm_status fdllm_cache_tile_bytes(int D, size_t* bytes);
 
 /*
@@ -554,7 +556,8 @@ fdllm_status fdllm_cache_attention(const void* q, int64_t q_stride, int T, const
  * Attention of whole packed sequences: queries q [T, H, D] over keys and
  * values k, v [Tk, Hk, D], bf16, sequence b's rows given by cu_q and cu_k
  * [B + 1] (the same array where a sequence attends to itself; more keys than
- * queries where its first tokens are done).  workspace:
+ * queries where its first tokens are done; counts of keys that run backwards or
+ * past Tk stand for no keys).  workspace:
  * fdllm_prompt_attention_workspace_size() bytes, 16-byte aligned (NULL where
  * that is 0).  Other arguments as above.
  *   Sizes (FDLLM_ERR_SIZE beyond): D 64, 96 or 128; H at most 2^15; B * Hk below

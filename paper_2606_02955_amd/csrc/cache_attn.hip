@@ -20,7 +20,7 @@
 // Tiles of 16 rows are bound by the read: two tokens over 99001 to 131072 keys
 // (8 heads of keys of 128) 43 us for 250 MB, 5.8 TB/s.  Tiles of 32 by the
 // instructions: 64 blocks of 32 tokens, four heads a key head, over 6000 to 8192
-// keys 250 us, 0.80 PFLOP/s, the matrix cores busy half of the time and the
+// keys 247 us, 0.81 PFLOP/s, the matrix cores busy half of the time and the
 // vector units 58%, since a wave's scores, softmax and outputs follow one
 // another; to form the next page's scores beside this page's softmax takes more
 // registers than a wave has (measured with spills in the starts and ends: 300).
@@ -441,7 +441,10 @@ k_cache_attn(const CacheAttnArgs a) {
       else __builtin_amdgcn_wave_barrier();
 
       // outputs: the weights of a step of 16 (32) keys are formed beside the
-      // products of the one before; to 8 bits, as the values they meet
+      // products of the one before.  Rounded to bfloat16, the type of the values
+      // that they meet in one product (the sums take them unrounded): over many
+      // keys an output is off by 0.0020 to 0.0022 relative, 0.0017 in 32 bits
+      // rounded once; in two pieces they would double this product.
       u32x4 p[2];
       const auto weigh = [&](int k, int i) {   // pair i of step k
         const int x = MT == 32 ? k / 2 : 2 * k + i / 2, at = MT == 32 ? 8 * (k % 2) + 2 * i : 2 * (i % 2);
@@ -689,9 +692,9 @@ k_cache_join(const CacheAttnArgs a, int wgs) {
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-// Pages of an item up to which a set of waves takes them alone, where there is
-// one sequence: without parts there is no join, which costs as much as two or
-// three pages.  (32 heads, one token: 12.6 us divided and 9.3 whole at 1024 keys,
+// Pages a set of waves up to which items stay whole, where there is one sequence:
+// without parts there is no join, which costs as much as two or three pages.
+// Counted by the width of the page table, all that the host knows of a length.  (32 heads, one token: 12.6 us divided and 9.3 whole at 1024 keys,
 // two pages a set; 13.3 and 12.7 at 2048, four; 15.6 and 20.3 at 4096, eight.
 // A block of 32: 14.6 and 12.3, 16.0 and 16.5, 22.0 and 24.9.)
 constexpr int kCaWholePages = 4;

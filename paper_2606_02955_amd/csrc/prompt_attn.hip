@@ -9,8 +9,8 @@
 // 32 columns, and 64 KiB of LDS and 256 registers let two workgroups share a CU.
 //
 // Bound by the matrix cores: one causal prompt of 16384 tokens, 16 heads of 128
-// over 4, 962 to 1000 us, 1.10 to 1.14 PFLOP/s (a 16384^3 library product reaches
-// 1.37).  Short prompts by the starts and ends of the workgroups: 16384 tokens in
+// over 4, 962 to 1000 us, 1.10 to 1.14 PFLOP/s (a 16384^3 library product of normal
+// values reaches 1.36 to 1.38 in the same runs).  Short prompts by the starts and ends of the workgroups: 16384 tokens in
 // prompts of equal length take 88 us and 14 more for every 64 keys.
 #include <hip/hip_runtime.h>
 
@@ -253,9 +253,11 @@ k_prompt_attn(const PromptArgs a) {
         for (int i = 0; i < 16; ++i) o[x][i] *= f;
     }
   };
-  // Pair i of a tile's 16 pairs of weights, rounded to 8 bits as the values
-  // they meet; four pairs make the operand of one product of outputs and NG - 1
-  // more.
+  // Pair i of a tile's 16 pairs of weights; four pairs make the operand of one
+  // product of outputs and NG - 1 more.  Rounded to bfloat16, the type of the values
+  // that they meet (the sums take them unrounded): an output is off by 0.0021 to
+  // 0.0022 relative, 0.0017 in 32 bits rounded once; in two pieces they would
+  // double the products of the outputs.
   u32x4 p[4];
   const auto weigh = [&](const f32x16* of, int i) {
     const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(of[i / 8][2 * (i % 8)], a.c, -ref));

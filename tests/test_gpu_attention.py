@@ -2,8 +2,8 @@
 
 Bounds.  A float32 sum of n products errs by at most n 2^-24 of the sum of
 magnitudes; a head's norm and rotation stay within 2e-6 of the row's largest
-element.  An attention output in bfloat16 is off by its own rounding (2^-9 of
-it), by that of the weights (2^-9 of the attention of |v|), and by the scores'
+element.  An attention output in bfloat16 is off by its own rounding (2^-8 of
+it), by that of the weights (2^-8 of the attention of |v|), and by the scores'
 float32 error d = D 2^-24 max_j sum_d |q_d k_jd| scale, which moves every
 weight by 2 d at most; the log-sum-exp by d and its own rounding.  4-bit codes
 are equal to the oracle's wherever the value is not within float32's error of
@@ -236,7 +236,7 @@ CACHE_CASES = [
     (128, 4, 1, 1, [(1, 63), (1, 64), (1, 65), (1, 0), (1, 700)]),      # up to 16 rows: single tokens
     (64, 16, 1, 0, [(1, 129), (1, 2000)]),                               # 16 rows exactly
     (96, 6, 2, 1, [(3, 200), (1, 2), (5, 131), (0, 50)]),
-    (64, 17, 1, 0, [(1, 300), (1, 5)]),                                  # 17 rows: 32-row tiles, pages dealt to four waves
+    (64, 17, 1, 0, [(1, 300), (1, 5)]),                                  # 17 rows: 32-row tiles, pages dealt to eight waves
     (128, 2, 2, 0, [(32, 1024), (7, 90), (32, 1)]),
     (128, 2, 2, 32, [(32, 97), (20, 40), (32, 33), (9, 9)]),
     (96, 3, 3, 1, [(30, 333), (32, 12)]),                                # more queries than keys: rows that see nothing
@@ -253,7 +253,7 @@ CACHE_CASES = [
     (96, 8, 2, 32, [(8, 1500)]),
     (64, 7, 1, 0, [(8, 500)]),
     (64, 40, 8, 0, [(32, 20)] * 33),                                     # more items of one page than workgroups
-    (64, 1, 1, 1, [(1, 1 + 7 * i) for i in range(300)]),                 # more sequences than threads
+    (64, 1, 1, 1, [(1, 1 + 7 * i) for i in range(300)]),                 # more sequences than a wave has lanes
 ]
 
 
