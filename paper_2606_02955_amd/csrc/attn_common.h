@@ -88,6 +88,16 @@ __device__ __forceinline__ float sum_row(float v) {
   else return sum_quarters(v);
 }
 
+// The sum over a wave, in a scalar register.
+__device__ __forceinline__ int wave_sum(int v) {
+  v += partner_i32<0>(v);
+  v += partner_i32<1>(v);
+  v += partner_i32<2>(v);
+  v += partner_i32<3>(v);
+  v += partner_i32<4>(v);
+  return __builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 32);
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   bf16x2 p;
   p[0] = (__bf16)a;

@@ -63,6 +63,11 @@ struct PaTile {
 
 __device__ __forceinline__ PaTile pa_tile(const PromptArgs& a, int b, int tile) {
   PaTile t;
+  // first of all, so that its loads are under way beside the others: a lane counts
+  // the row tiles of every 64th sequence before
+  int before = 0;
+  if (a.splits > 1 && b > 0)
+    before = wave_sum(pa_tiles_before(a.cu_q, b, a.T, a.max_q, a.R, threadIdx.x % kWave, kWave));
   t.n = packed_rows(a.cu_q, b, a.T, a.max_q, &t.first);
   t.len = packed_rows(a.cu_k, b, a.Tk, INT32_MAX, &t.firstk);
   t.rows = t.n * a.R;
@@ -74,11 +79,8 @@ __device__ __forceinline__ PaTile pa_tile(const PromptArgs& a, int b, int tile) 
   t.far = visible_end(t.len - t.n + last / a.R, a.blk, t.len);
   const int nt = (t.far + kPaKeys - 1) / kPaKeys;
   t.parts = nt <= max(kPaWholeTiles, 2 * a.share) ? 1 : min(a.splits, (nt + a.share - 1) / a.share);
-  if (t.parts > 1) {   // (a lane counts the tiles of every 64th sequence)
-    int before = pa_tiles_before(a.cu_q, b, a.T, a.max_q, a.R, threadIdx.x % kWave, kWave);
-#pragma unroll
-    for (int x = 1; x < kWave; x <<= 1) before += __shfl_xor(before, x);
-    t.place = __builtin_amdgcn_readfirstlane(before) + tile;
+  if (t.parts > 1) {
+    t.place = before + tile;
     if (t.place >= a.places) t.parts = 1;   // tokens in several sequences: more row tiles than room
   }
   return t;
@@ -485,9 +487,10 @@ static bool pa_sizes_ok(int B, int T, int H, int Hk, int D, int max_q) {
 // A row tile's keys are divided where the longest tile would run on while the
 // rest of the chip is done: where it has more than twice the keys that fall to
 // one of the workgroups that run at once, as far as the host knows them (it
-// knows the sums of the lengths, not the lengths).  Three sequences of 1, 1937
-// and 3873 tokens with 5 heads on one: 61 us whole, 47 divided; 13 of 570
-// tokens: 18 whole, 31 divided, so what is merely uneven stays whole.
+// knows the sums of the lengths, not the lengths).  Three causal sequences
+// of 1, 1937 and 3873 tokens with 5 heads on one: 61 us whole, 52 divided (67 and
+// 71 without a mask); three of 20 tokens behind 3000: 48 and 14; 13 of 570 tokens:
+// 18 whole, 31 divided, so what is merely uneven stays whole.
 static PaPlan pa_plan(int B, int T, int Tk, int H, int Hk, int D, int max_q, int blk) {
   PaPlan p{};
   const int R = H / Hk;
