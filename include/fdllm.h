@@ -570,6 +570,147 @@ fdllm_status fdllm_prompt_attention(const void* q, int64_t q_stride, const void*
                                     int max_q, int H, int Hk, int D, float scale, int blk, void* out, float* lse,
                                     void* workspace, size_t workspace_bytes, fdllm_stream stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Decoding with drafted tokens
+ * ---------------------------------------------------------------------------
+ * A drafter (a block decoder's per-position marginals, or a small model)
+ * proposes tokens, a chain or a tree of them; one call of the target model over
+ * all of them says which stand.  A step of a tree: fdllm_tree_layout, in every
+ * layer fdllm_qk_norm_rope and fdllm_tree_attention, fdllm_verify_tree on the
+ * logits, fdllm_cache_keep over all layers.  A chain needs no tree: blk = 1 of
+ * fdllm_cache_attention, then fdllm_verify_draft.
+ *
+ * Requests.  Packed as sequences are above: request b has the n rows
+ *   [cu_q[b], cu_q[b + 1]) of the T, one a node; node 0 is the token that the
+ *   last step ended with, the others are drafted.  kv_len[b] counts the tokens in
+ *   the cache with the n nodes, which are its last, in the nodes' order.  A
+ *   request whose counts are out of order, or that has more than max_q rows, is
+ *   one without rows.
+ * Trees.  parents [T] int32: the node of the same request that a node follows,
+ *   an earlier one; anything else stands for none (-1: it follows the context).
+ */
+
+/* Nodes of a tree, or rows of a chain, at most (max_q). */
+#define FDLLM_MAX_TREE 1024
+
+/*
+ * What a layer's calls need for the nodes of trees:
+ *   masks [T, mask_words] uint64 (out): bit j % 64 of word j / 64 of a node's row
+ *   is set where j is the node itself or one of its ancestors; mask_words at
+ *   least ceil(max_q / 64);
+ *   positions [T] int32 (out, may be NULL): kv_len - n plus the number of a
+ *   node's ancestors: the row of cos_sin for it;
+ *   page_table [B, table_width], slots [T] int32 (out; both may be NULL): the
+ *   cache slot of a node, -1 where the table has no page for it (or a negative one).
+ * Rows of no request are not written.  Sizes (FDLLM_ERR_SIZE beyond): max_q at most
+ * FDLLM_MAX_TREE, B 65535, mask_words 2^16.
+ */
+fdllm_status fdllm_tree_layout(const int32_t* parents, int T, const int32_t* cu_q, int B, int max_q,
+                               const int32_t* kv_len, const int32_t* page_table, int table_width, uint64_t* masks,
+                               int mask_words, int32_t* positions, int32_t* slots, fdllm_stream stream);
+
+/*
+ * Attention of trees over the cache: fdllm_cache_attention with another mask.
+ * Every node sees the first kv_len - n keys, and of its request's nodes those
+ * whose bits its row of masks has (any bits will do, not only ancestors'; bits
+ * from n on are not looked at).  A node that sees nothing gets out = 0 and lse =
+ * -inf.  masks [T, mask_words] uint64, mask_words at least ceil(max_q / 64); the other
+ * arguments, the values and the limits are those of fdllm_cache_attention, the
+ * workspace too (fdllm_cache_attention_workspace_size).
+ */
+fdllm_status fdllm_tree_attention(const void* q, int64_t q_stride, int T, const int32_t* cu_q, int B, int max_q,
+                                  int H, int Hk, int D, const uint8_t* cache, int n_pages,
+                                  const int32_t* page_table, int table_width, const int32_t* kv_len,
+                                  const uint64_t* masks, int mask_words, float scale, void* out, float* lse,
+                                  void* workspace, size_t workspace_bytes, fdllm_stream stream);
+
+/*
+ * Verification.  Row i of a request holds the target's logits for the token that
+ * follows its node i.
+ *   logits [T, V] bf16 or float per `dtype`, a row logits_stride elements after
+ *   the one before (any stride of at least V); finite, or -inf for a token that
+ *   cannot be (NaN and +inf: results are unspecified, no fault);
+ *   temperature [B] float (NULL: 1): p = softmax(logits / temperature); 0
+ *   (negative, NaN) puts all of p on the highest logit, the lowest index among
+ *   equals;
+ *   ids [T] int32: the tokens at the nodes (one outside [0, V) never stands).
+ * Draws.  A number u and weights w give the lowest v for which w_0 + ... + w_v >
+ *   u (w_0 + w_1 + ...); tokens less likely than 2^-1000 of the likeliest have
+ *   weight 0.  Numbers are floats in [0, 1): negative ones and NaN with a sign
+ *   count as 0, others outside as 1 - 2^-24.  Probabilities, sums and comparisons
+ *   are formed in 64 bits (a relative error below 1e-12), so that the token is the
+ *   definition's unless u lies that near a border.
+ * Results are packed as the rows are: of a request's rows the first n_tokens get
+ *   the tokens that follow (the drafted ones that stand, then the one drawn), the
+ *   others -1.  logp [T] float (may be NULL): the logarithms of their
+ *   probabilities p, 0 for the others.  Rows of no request are not written;
+ *   n_tokens of a request without rows is 0.  A row that cannot have any token
+ *   (all -inf) gets -1 for the token drawn, counted in n_tokens, and logp 0.
+ *   Rows in more than one request: each must have the same temperature in all.
+ * Sizes (FDLLM_ERR_SIZE beyond): V from 1 to 2^30, max_q at most FDLLM_MAX_TREE,
+ *   B at most 65535.  For the same arguments a call is bitwise reproducible, whatever
+ *   other requests are in it.
+ */
+
+/*
+ * A chain: row i judges the draft ids[i + 1].  It stands when all before it do
+ * and u_i q(draft) < p(draft), q = softmax(draft_logits / temperature) of the
+ * row.  When all n - 1 stand one more token is drawn from p of the last row, with
+ * the request's own number u_draw; when one falls, from max(p - q, 0) of its row.
+ *   draft_logits [T, V] of the same type (NULL: the drafter is sure of its token:
+ *   q is 1 there and 0 elsewhere), of which a request's last row is not read;
+ *   u [T] float, u_draw [B] float: the numbers; u of a request's last row is
+ *   not looked at.
+ * With temperature 0 a draft stands when it is the highest logit's, and the
+ * token drawn is that: neither the drafter's logits nor the numbers are looked
+ * at.  A draft whose row of draft_logits cannot have any token falls, and the
+ * token is drawn from p; so it is where p - q is positive nowhere.
+ *   workspace: fdllm_verify_draft_workspace_size() bytes, 16-byte aligned,
+ *   scratch between calls.
+ */
+fdllm_status fdllm_verify_draft_workspace_size(int T, int B, int V, int with_draft_logits, size_t* bytes);
+fdllm_status fdllm_verify_draft(const void* logits, int64_t logits_stride, const void* draft_logits,
+                                int64_t draft_stride, fdllm_dtype dtype, int T, int V, const int32_t* ids,
+                                const int32_t* cu_q, int B, int max_q, const float* temperature, const float* u,
+                                const float* u_draw, int32_t* tokens, int32_t* n_tokens, float* logp,
+                                void* workspace, size_t workspace_bytes, fdllm_stream stream);
+
+/*
+ * A tree: at every node a token y is drawn from the row's p with the node's own
+ * number u.  From node 0 on, y is the next token, and the next node the child that
+ * holds it, the lowest of several; where no child does, the walk ends.
+ *   path [T] int32 (out): of a request's rows the first n_tokens get the nodes of
+ *   the walk (0 first), the others -1; tokens has what follows each.
+ *   workspace: fdllm_verify_tree_workspace_size() bytes, 16-byte aligned.
+ */
+fdllm_status fdllm_verify_tree_workspace_size(int T, int B, int V, size_t* bytes);
+fdllm_status fdllm_verify_tree(const void* logits, int64_t logits_stride, fdllm_dtype dtype, int T, int V,
+                               const int32_t* ids, const int32_t* parents, const int32_t* cu_q, int B, int max_q,
+                               const float* temperature, const float* u, int32_t* path, int32_t* tokens,
+                               int32_t* n_tokens, float* logp, void* workspace, size_t workspace_bytes,
+                               fdllm_stream stream);
+
+/*
+ * What stands of a tree moves to its place in the cache: the entries of node
+ * path[i] of a request become those of its node i, for i < n_path[b], in all
+ * heads and layers, bit for bit, each as it was before the call.
+ *   cache [layers, n_pages, Hk, tile]: layers caches of the same pages, one behind
+ *   the other;
+ *   path [T], n_path [B] int32: as fdllm_verify_tree leaves them (path, n_tokens).
+ *   An entry path[i] that is not at least i and below n moves nothing, neither
+ *   does one whose page, or its place's, the table does not have; a request with
+ *   n_path outside [0, n] is left as it is;
+ *   kv_out [B] int32 (out, may be NULL; not kv_len itself): the new length, kv_len - n +
+ *   n_path (kv_len for a request that is left as it is).
+ * Requests must not share pages that they write.  Sizes (FDLLM_ERR_SIZE beyond):
+ * layers * Hk below 2^24, B at most 65535, max_q at most FDLLM_MAX_TREE; D a multiple of
+ * 32, 32 to 256.
+ */
+fdllm_status fdllm_cache_keep(uint8_t* cache, int layers, int n_pages, int Hk, int D, const int32_t* page_table,
+                              int table_width, const int32_t* kv_len, const int32_t* cu_q, int T, int B, int max_q,
+                              const int32_t* path, const int32_t* n_path, int32_t* kv_out, fdllm_stream stream);
+
 /* Static, human-readable text for a status code. */
 const char* fdllm_status_string(fdllm_status status);
 

@@ -1,7 +1,7 @@
 """Python binding of libfdllm.so, the gfx950 Fast-dLLM++ commit selector.
 
 Thin marshalling of the C ABI declared in include/fdllm.h (by ctypes; the
-attention calls' by csrc/binding.cpp): every function takes torch tensors that already live on the GPU, checks their
+attention calls' and those of drafted tokens by csrc/binding.cpp): every function takes torch tensors that already live on the GPU, checks their
 dtype/shape/contiguity, and passes raw device pointers plus the current HIP
 stream.  All arithmetic happens in the HIP kernels; there is no CPU fallback,
 and loading fails loudly when the library has not been built.
@@ -32,6 +32,7 @@ ERR_BOUNDS, ERR_BLOCK_TOO_LARGE, ERR_NONFINITE, ERR_SCRATCH = -6, -7, -8, -9
 MAX_ABS_LOGIT = 1.0e7
 CACHE_PAGE = 64
 OUT_BF16, OUT_E5M2 = 0, 1
+MAX_TREE = 1024
 STATIC_SCRATCH_BYTES = 8 << 20
 
 EXPORTS = ("fdllm_confidence", "fdllm_select_profile", "fdllm_select_factor",
@@ -42,7 +43,10 @@ EXPORTS = ("fdllm_confidence", "fdllm_select_profile", "fdllm_select_factor",
            "fdllm_lmhead_confidence", "fdllm_lmhead_decode_step", "fdllm_check_inputs",
            "fdllm_decode_step_static", "fdllm_cache_tile_bytes", "fdllm_qk_norm_rope",
            "fdllm_cache_read", "fdllm_cache_attention_workspace_size", "fdllm_cache_attention",
-           "fdllm_prompt_attention_workspace_size", "fdllm_prompt_attention")
+           "fdllm_prompt_attention_workspace_size", "fdllm_prompt_attention",
+           "fdllm_tree_layout", "fdllm_tree_attention", "fdllm_verify_draft_workspace_size",
+           "fdllm_verify_draft", "fdllm_verify_tree_workspace_size", "fdllm_verify_tree",
+           "fdllm_cache_keep")
 
 
 class GenerationDesc(ctypes.Structure):
@@ -118,7 +122,18 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.fdllm_prompt_attention.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, i32, i32, i32, i32, i32,
                                            f32, i32, vp, vp, vp, sz, vp]
     lib.fdllm_prompt_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
-    for name in ("fdllm_cache_tile_bytes", "fdllm_qk_norm_rope", "fdllm_cache_read",
+    lib.fdllm_tree_layout.argtypes = [vp, i32, vp, i32, i32, vp, vp, i32, vp, i32, vp, vp, vp]
+    lib.fdllm_tree_attention.argtypes = [vp, i64, i32, vp, i32, i32, i32, i32, i32, vp, i32, vp, i32, vp, vp, i32,
+                                         f32, vp, vp, vp, sz, vp]
+    lib.fdllm_verify_draft_workspace_size.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.fdllm_verify_draft.argtypes = [vp, i64, vp, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp,
+                                       vp, sz, vp]
+    lib.fdllm_verify_tree_workspace_size.argtypes = [i32, i32, i32, ctypes.POINTER(sz)]
+    lib.fdllm_verify_tree.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.fdllm_cache_keep.argtypes = [vp, i32, i32, i32, i32, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp]
+    for name in ("fdllm_tree_layout", "fdllm_tree_attention", "fdllm_verify_draft_workspace_size",
+                 "fdllm_verify_draft", "fdllm_verify_tree_workspace_size", "fdllm_verify_tree", "fdllm_cache_keep",
+                 "fdllm_cache_tile_bytes", "fdllm_qk_norm_rope", "fdllm_cache_read",
                  "fdllm_cache_attention_workspace_size", "fdllm_cache_attention",
                  "fdllm_prompt_attention_workspace_size", "fdllm_prompt_attention",
                  "fdllm_confidence", "fdllm_reveal", "fdllm_decode_step", "fdllm_workspace_size",
@@ -547,6 +562,62 @@ def fdllm_prompt_attention(q, k, v, cu_q, cu_k, out, max_q: int, lse=None, scale
     size); returns the workspace for reuse (None where the call needs none)."""
     return _attention_status(_native().prompt_attention(q, k, v, cu_q, cu_k, out, max_q, lse, scale, blk, workspace,
                                                         _stream_of(q)), "fdllm_prompt_attention")
+
+
+# ---- decoding with drafted tokens (see fdllm.h) ----
+def fdllm_tree_layout(parents, kv_len, cu_q, max_q: int, masks, positions=None, page_table=None, slots=None):
+    """Masks [T, words] int64 of the ancestors of every node of trees, the nodes'
+    positions and, with a page table, their cache slots (see fdllm.h)."""
+    _attention_status(_native().tree_layout(parents, kv_len, cu_q, max_q, masks, positions, page_table, slots,
+                                            _stream_of(parents)), "fdllm_tree_layout")
+
+
+def fdllm_tree_attention(q, cache, page_table, kv_len, cu_q, masks, out, max_q: int, lse=None,
+                         scale: Optional[float] = None, workspace=None):
+    """Attention of trees' nodes over the 4-bit cache: the context and what each
+    node's masks say (see fdllm.h).  scale defaults to 1 / sqrt(head size);
+    returns the workspace for reuse (None where the call needs none), of
+    fdllm_cache_attention_workspace_size() bytes."""
+    return _attention_status(_native().tree_attention(q, cache, page_table, kv_len, cu_q, masks, out, max_q, lse, scale,
+                                                      workspace, _stream_of(q)), "fdllm_tree_attention")
+
+
+def fdllm_verify_draft_workspace_size(T: int, B: int, V: int, with_draft: bool) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().fdllm_verify_draft_workspace_size(T, B, V, int(bool(with_draft)), ctypes.byref(n)),
+           "fdllm_verify_draft_workspace_size")
+    return int(n.value)
+
+
+def fdllm_verify_draft(logits, ids, cu_q, max_q: int, u, u_draw, tokens, n_tokens, draft=None, temperature=None,
+                       logp=None, workspace=None):
+    """Chains of drafted tokens against the target's probabilities (and the
+    drafter's, from its logits `draft`), with given numbers u [T], u_draw [B] (see
+    fdllm.h); returns the workspace for reuse."""
+    return _attention_status(_native().verify_draft(logits, ids, cu_q, max_q, u, u_draw, tokens, n_tokens, draft, temperature,
+                                                    logp, workspace, _stream_of(logits)), "fdllm_verify_draft")
+
+
+def fdllm_verify_tree_workspace_size(T: int, B: int, V: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().fdllm_verify_tree_workspace_size(T, B, V, ctypes.byref(n)), "fdllm_verify_tree_workspace_size")
+    return int(n.value)
+
+
+def fdllm_verify_tree(logits, ids, parents, cu_q, max_q: int, u, path, tokens, n_tokens, temperature=None, logp=None,
+                      workspace=None):
+    """Trees of drafted tokens against draws from the target at their nodes, with
+    given numbers u [T] (see fdllm.h); returns the workspace for reuse."""
+    return _attention_status(_native().verify_tree(logits, ids, parents, cu_q, max_q, u, path, tokens, n_tokens, temperature,
+                                                   logp, workspace, _stream_of(logits)), "fdllm_verify_tree")
+
+
+def fdllm_cache_keep(cache, page_table, kv_len, cu_q, path, n_path, max_q: int, kv_out=None):
+    """The cache entries of what stands of trees moved to their places, in a cache
+    [pages, kv heads, tile bytes] or [layers, ...] of them; kv_out: the new
+    lengths (see fdllm.h)."""
+    _attention_status(_native().cache_keep(cache, page_table, kv_len, cu_q, path, n_path, max_q, kv_out,
+                                           _stream_of(cache)), "fdllm_cache_keep")
 
 
 def load_bench(path: Optional[str] = None) -> ctypes.CDLL:

@@ -22,6 +22,8 @@ STATIC_SRC = os.path.join(PKG, "csrc", "decode_static.hip")
 ROPE_SRC = os.path.join(PKG, "csrc", "qk_rope.hip")
 CACHE_SRC = os.path.join(PKG, "csrc", "cache_attn.hip")
 PROMPT_SRC = os.path.join(PKG, "csrc", "prompt_attn.hip")
+TREE_SRC = os.path.join(PKG, "csrc", "tree.hip")
+VERIFY_SRC = os.path.join(PKG, "csrc", "verify.hip")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libfdllm.so")
 BENCH_SRC = os.path.join(PKG, "csrc", "stream_read.hip")
@@ -88,7 +90,8 @@ def _run(cmd, tmp: str, lib: str, verbose: bool) -> str:
 def build(verbose: bool = False, extra=()) -> str:
     """Compile libfdllm.so, libfdllm_bench.so and _binding.so (always all of them)."""
     _compile([BENCH_SRC], BENCH_LIB, verbose)
-    _compile([SRC, LMHEAD_SRC, LOOP_SRC, STATIC_SRC, ROPE_SRC, CACHE_SRC, PROMPT_SRC], LIB, verbose, extra)
+    _compile([SRC, LMHEAD_SRC, LOOP_SRC, STATIC_SRC, ROPE_SRC, CACHE_SRC, PROMPT_SRC, TREE_SRC,
+              VERIFY_SRC], LIB, verbose, extra)
     _compile_binding(verbose)
     return LIB
 

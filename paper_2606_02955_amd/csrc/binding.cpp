@@ -1,10 +1,12 @@
-// binding.cpp -- the attention calls on torch tensors: each checks its tensors,
-// takes their addresses and strides and calls libfdllm.so.  They are made once
-// a layer on a few tokens at a time, where a launch takes 2 to 3 us and checking
-// and converting two dozen arguments in Python took 6 more.
+// binding.cpp -- the attention calls and those of decoding with drafted tokens on
+// torch tensors: each checks its tensors, takes their addresses and strides and
+// calls libfdllm.so.  They are made once a layer, or a step, on a few tokens at a
+// time, where a launch takes 2 to 3 us and checking and converting two dozen
+// arguments in Python took 6 more.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 
 #include <cmath>
 #include <cstdint>
@@ -301,10 +303,219 @@ PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- decoding with drafted tokens ----
+// The tensors of a call lie on one device, which is the current one while it is made.
+void together(std::initializer_list<PyObject*> list, const at::Tensor& with, const char* what) {
+  for (PyObject* o : list)
+    if (o != Py_None && THPVariable_Check(o) && THPVariable_Unpack(o).device() != with.device())
+      throw std::invalid_argument(std::string("all tensors must be on the device of ") + what);
+}
+
+// [rows, columns] of 64-bit masks, or of logits whose rows may lie apart.
+const at::Tensor& masks_of(PyObject* o, int64_t T, const char* name, int* words) {
+  const at::Tensor& t = dims(o, 2, name, "[tokens, words of 64 bits]");
+  *words = whole(t.size(1), "mask words");
+  at_of(o, at::kLong, {T, t.size(1)}, name);
+  return t;
+}
+Heads rows_of(PyObject* o, at::ScalarType type, int64_t T, int64_t V, const char* name) {
+  const at::Tensor& t = tensor(o, name);
+  expect(t, type, {T, V}, name);
+  if (t.stride(1) != 1 && V != 1) throw std::invalid_argument(std::string(name) + ": a row's logits must lie side by side");
+  return {t.data_ptr(), T > 1 ? t.stride(0) : V};
+}
+
+PyObject* tree_layout(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const at::Tensor& parents = dims(a[0], 1, "parents", "[tokens]");
+    const int64_t T = parents.size(0);
+    const int32_t* pp = (const int32_t*)at_of(a[0], at::kInt, {T}, "parents");
+    const int64_t B = dims(a[1], 1, "kv_len", "[sequences]").size(0);
+    const int32_t* kv = (const int32_t*)at_of(a[1], at::kInt, {B}, "kv_len");
+    const int32_t* cu = (const int32_t*)at_of(a[2], at::kInt, {B + 1}, "cu_q");
+    const int max_q = whole(a[3], "max_q");
+    int words = 0;
+    uint64_t* masks = (uint64_t*)masks_of(a[4], T, "masks", &words).data_ptr();
+    int32_t* positions = (int32_t*)at_or_null(a[5], at::kInt, {T}, "positions");
+    int64_t width = 0;
+    const int32_t* table = nullptr;
+    if (a[6] != Py_None) {
+      width = dims(a[6], 2, "page_table", "[sequences, pages]").size(1);
+      table = (const int32_t*)at_of(a[6], at::kInt, {B, width}, "page_table");
+    } else if (a[7] != Py_None) {
+      throw std::invalid_argument("page_table must be given with slots");
+    }
+    int32_t* slots = (int32_t*)at_or_null(a[7], at::kInt, {T}, "slots");
+    together({a[1], a[2], a[4], a[5], a[6], a[7]}, parents, "parents");
+    const int t32 = whole(T, "tokens"), b32 = whole(B, "sequences"), w32 = whole(width, "page_table columns");
+    const fdllm_stream stream = stream_of(a[8]);
+    const c10::DeviceGuard guard(parents.device());
+    return PyLong_FromLong(unlocked([&] {
+      return fdllm_tree_layout(pp, t32, cu, b32, max_q, kv, table, w32, masks, words, positions, slots, stream);
+    }));
+  });
+}
+
+PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 12, [&]() -> PyObject* {
+    const at::Tensor& q = rows(a[0], "q");
+    const int64_t T = q.size(0), H = q.size(1), D = q.size(2);
+    const Heads hq = heads_of(a[0], at::kBFloat16, T, H, D, "q");
+    const int64_t Hk = dims(a[1], 3, "cache", "[pages, key heads, tile bytes]").size(1);
+    int n_pages = 0;
+    const uint8_t* cache = cache_of(a[1], Hk, D, &n_pages);
+    const at::Tensor& table = dims(a[2], 2, "page_table", "[sequences, pages]");
+    const int64_t B = table.size(0), width = table.size(1);
+    const int32_t* tp = (const int32_t*)at_of(a[2], at::kInt, {B, width}, "page_table");
+    const int32_t* kv = (const int32_t*)at_of(a[3], at::kInt, {B}, "kv_len");
+    const int32_t* cu = (const int32_t*)at_of(a[4], at::kInt, {B + 1}, "cu_q");
+    int words = 0;
+    const uint64_t* masks = (const uint64_t*)masks_of(a[5], T, "masks", &words).data_ptr();
+    void* out = at_of(a[6], at::kBFloat16, {T, H, D}, "out");
+    const int max_q = whole(a[7], "max_q");
+    float* lse = (float*)at_or_null(a[8], at::kFloat, {T, H}, "lse");
+    const float scale = scale_of(a[9], D);
+    together({a[1], a[2], a[3], a[4], a[5], a[6], a[8], a[10]}, q, "q");
+    const int t32 = whole(T, "tokens"), b32 = whole(B, "sequences"), h32 = whole(H, "heads"), hk32 = whole(Hk, "heads"),
+              d32 = whole(D, "head size"), w32 = whole(width, "page_table columns");
+    size_t need = 0;
+    if (a[10] == Py_None) {
+      const fdllm_status st = fdllm_cache_attention_workspace_size(b32, h32, hk32, d32, max_q, w32, &need);
+      if (st != FDLLM_OK) return PyLong_FromLong(st);
+    }
+    const c10::DeviceGuard guard(q.device());
+    const Scratch ws = scratch(a[10], need, q);
+    const fdllm_stream stream = stream_of(a[11]);
+    return result(unlocked([&] {
+      return fdllm_tree_attention(hq.p, hq.stride, t32, cu, b32, max_q, h32, hk32, d32, cache, n_pages, tp, w32, kv, masks,
+                                  words, scale, out, lse, ws.p, ws.bytes, stream);
+    }), a[10], ws);
+  });
+}
+
+// What both verifications take of the target.
+struct Target {
+  at::ScalarType type;
+  fdllm_dtype code;
+  int64_t T, V, B;
+  Heads logits;
+  const int32_t *ids, *cu;
+  const float *temperature, *u;
+  int32_t *tokens, *n_tokens;
+  float* logp;
+  int t32, v32, b32, max_q;
+};
+Target target_of(PyObject* logits, PyObject* ids, PyObject* cu, PyObject* max_q, PyObject* u, PyObject* tokens,
+                 PyObject* n_tokens, PyObject* temperature, PyObject* logp) {
+  Target x;
+  const at::Tensor& t = dims(logits, 2, "logits", "[tokens, vocabulary]");
+  x.type = t.scalar_type();
+  if (x.type != at::kBFloat16 && x.type != at::kFloat) throw std::invalid_argument("logits must be bfloat16 or float32");
+  x.code = x.type == at::kFloat ? FDLLM_F32 : FDLLM_BF16;
+  x.T = t.size(0), x.V = t.size(1);
+  x.logits = rows_of(logits, x.type, x.T, x.V, "logits");
+  x.B = dims(n_tokens, 1, "n_tokens", "[requests]").size(0);
+  x.n_tokens = (int32_t*)at_of(n_tokens, at::kInt, {x.B}, "n_tokens");
+  x.ids = (const int32_t*)at_of(ids, at::kInt, {x.T}, "ids");
+  x.cu = (const int32_t*)at_of(cu, at::kInt, {x.B + 1}, "cu_q");
+  x.u = (const float*)at_of(u, at::kFloat, {x.T}, "u");
+  x.tokens = (int32_t*)at_of(tokens, at::kInt, {x.T}, "tokens");
+  x.temperature = (const float*)at_or_null(temperature, at::kFloat, {x.B}, "temperature");
+  x.logp = (float*)at_or_null(logp, at::kFloat, {x.T}, "logp");
+  x.t32 = whole(x.T, "tokens"), x.v32 = whole(x.V, "vocabulary"), x.b32 = whole(x.B, "requests");
+  x.max_q = whole(max_q, "max_q");
+  return x;
+}
+
+PyObject* verify_draft(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 13, [&]() -> PyObject* {
+    const Target x = target_of(a[0], a[1], a[2], a[3], a[4], a[6], a[7], a[9], a[10]);
+    const at::Tensor& like = THPVariable_Unpack(a[0]);
+    const float* u_draw = (const float*)at_of(a[5], at::kFloat, {x.B}, "u_draw");
+    Heads draft;
+    if (a[8] != Py_None) draft = rows_of(a[8], x.type, x.T, x.V, "draft");
+    together({a[1], a[2], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11]}, like, "logits");
+    size_t need = 0;
+    if (a[11] == Py_None) {
+      const fdllm_status st = fdllm_verify_draft_workspace_size(x.t32, x.b32, x.v32, a[8] != Py_None, &need);
+      if (st != FDLLM_OK) return PyLong_FromLong(st);
+    }
+    const c10::DeviceGuard guard(like.device());
+    const Scratch ws = scratch(a[11], need, like);
+    const fdllm_stream stream = stream_of(a[12]);
+    return result(unlocked([&] {
+      return fdllm_verify_draft(x.logits.p, x.logits.stride, draft.p, draft.stride, x.code, x.t32, x.v32, x.ids, x.cu, x.b32,
+                                x.max_q, x.temperature, x.u, u_draw, x.tokens, x.n_tokens, x.logp, ws.p, ws.bytes, stream);
+    }), a[11], ws);
+  });
+}
+
+PyObject* verify_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 13, [&]() -> PyObject* {
+    const Target x = target_of(a[0], a[1], a[3], a[4], a[5], a[7], a[8], a[9], a[10]);
+    const at::Tensor& like = THPVariable_Unpack(a[0]);
+    const int32_t* parents = (const int32_t*)at_of(a[2], at::kInt, {x.T}, "parents");
+    int32_t* path = (int32_t*)at_of(a[6], at::kInt, {x.T}, "path");
+    PyObject* given = a[11];
+    together({a[1], a[2], a[3], a[5], a[6], a[7], a[8], a[9], a[10], given}, like, "logits");
+    size_t need = 0;
+    if (given == Py_None) {
+      const fdllm_status st = fdllm_verify_tree_workspace_size(x.t32, x.b32, x.v32, &need);
+      if (st != FDLLM_OK) return PyLong_FromLong(st);
+    }
+    const c10::DeviceGuard guard(like.device());
+    const Scratch ws = scratch(given, need, like);
+    const fdllm_stream stream = stream_of(a[12]);
+    return result(unlocked([&] {
+      return fdllm_verify_tree(x.logits.p, x.logits.stride, x.code, x.t32, x.v32, x.ids, parents, x.cu, x.b32, x.max_q,
+                               x.temperature, x.u, path, x.tokens, x.n_tokens, x.logp, ws.p, ws.bytes, stream);
+    }), given, ws);
+  });
+}
+
+// The head size whose tiles have this many bytes.
+int head_size_of(int64_t bytes) {
+  size_t tile = 0;
+  for (int D = 32; fdllm_cache_tile_bytes(D, &tile) == FDLLM_OK; D += 32)
+    if ((int64_t)tile == bytes) return D;
+  throw std::invalid_argument("no cache has tiles of " + std::to_string(bytes) + " bytes");
+}
+
+PyObject* cache_keep(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const at::Tensor& t = tensor(a[0], "cache");
+    if (t.dim() != 3 && t.dim() != 4)
+      throw std::invalid_argument("cache must be [pages, key heads, tile bytes], or [layers, ...] of them");
+    const int64_t layers = t.dim() == 4 ? t.size(0) : 1, pages = t.size(-3), Hk = t.size(-2), tile = t.size(-1);
+    const int D = head_size_of(tile);
+    uint8_t* cache = (uint8_t*)(t.dim() == 4 ? at_of(a[0], at::kByte, {layers, pages, Hk, tile}, "cache")
+                                             : at_of(a[0], at::kByte, {pages, Hk, tile}, "cache"));
+    const at::Tensor& table = dims(a[1], 2, "page_table", "[sequences, pages]");
+    const int64_t B = table.size(0), width = table.size(1);
+    const int32_t* tp = (const int32_t*)at_of(a[1], at::kInt, {B, width}, "page_table");
+    const int32_t* kv = (const int32_t*)at_of(a[2], at::kInt, {B}, "kv_len");
+    const int32_t* cu = (const int32_t*)at_of(a[3], at::kInt, {B + 1}, "cu_q");
+    const int64_t T = dims(a[4], 1, "path", "[tokens]").size(0);
+    const int32_t* path = (const int32_t*)at_of(a[4], at::kInt, {T}, "path");
+    const int32_t* n_path = (const int32_t*)at_of(a[5], at::kInt, {B}, "n_path");
+    const int max_q = whole(a[6], "max_q");
+    int32_t* kv_out = (int32_t*)at_or_null(a[7], at::kInt, {B}, "kv_out");
+    together({a[1], a[2], a[3], a[4], a[5], a[7]}, t, "cache");
+    const int l32 = whole(layers, "layers"), p32 = whole(pages, "cache pages"), hk32 = whole(Hk, "heads"),
+              w32 = whole(width, "page_table columns"), t32 = whole(T, "tokens"), b32 = whole(B, "sequences");
+    const fdllm_stream stream = stream_of(a[8]);
+    const c10::DeviceGuard guard(t.device());
+    return PyLong_FromLong(unlocked([&] {
+      return fdllm_cache_keep(cache, l32, p32, hk32, D, tp, w32, kv, cu, t32, b32, max_q, path, n_path, kv_out, stream);
+    }));
+  });
+}
+
 #define FDLLM_METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FDLLM_METHOD(qk_norm_rope), FDLLM_METHOD(cache_read), FDLLM_METHOD(cache_attention),
-                         FDLLM_METHOD(prompt_attention), {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "The attention calls on torch tensors.", -1, methods,
+                         FDLLM_METHOD(prompt_attention), FDLLM_METHOD(tree_layout), FDLLM_METHOD(tree_attention),
+                         FDLLM_METHOD(verify_draft), FDLLM_METHOD(verify_tree), FDLLM_METHOD(cache_keep), {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "The attention calls and those of drafted tokens on torch tensors.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -66,6 +66,8 @@ struct CacheAttnArgs {
   int32_t* plan;              // units of all sequences, then those before each (null: no item is split)
   float* part_ml;             // [workgroups][2][WR][MT][2]: reference and sum of a row's partial result
   float* part;                // [workgroups][2][WR] tiles of partial sums (attn_common.h)
+  const unsigned long long* masks;   // of a tree: [T][mask_w]
+  int mask_w;
 };
 
 // A sequence as the plan sees it: its query rows, pages and groups of rows.
@@ -83,6 +85,25 @@ __device__ __forceinline__ Seq sequence(const CacheAttnArgs& a, int b) {
   s.groups = (s.n * a.R + Rows - 1) / Rows;
   s.pages = max(1, (s.len + kPage - 1) / kPage);   // one at least: a row without keys gets its zeros
   return s;
+}
+
+// Which of the 64 keys from `base` on a node of a tree sees, a bit each: those
+// before the nodes, which begin at key `context`, and of the n nodes those in its
+// words of the mask.  (base and context meet in 32 bits: context is negative only
+// where there are fewer keys than nodes.)
+__device__ __forceinline__ unsigned long long tree_window(const unsigned long long* words, int n_words, int n, int base,
+                                                          int context) {
+  const int f = base - context;   // the node at the first of them
+  const auto word = [&](int w) { return w < n_words && w * 64 < n ? words[w] : 0ull; };
+  unsigned long long seen;
+  if (f < 0) {
+    seen = f <= -64 ? ~0ull : word(0) << -f | ((1ull << -f) - 1);
+  } else {
+    seen = word(f / 64) >> (f % 64);
+    if (f % 64) seen |= word(f / 64 + 1) << (64 - f % 64);
+  }
+  const int left = n - f;         // nodes from the first key on
+  return left <= 0 ? 0ull : left < 64 ? seen & ((1ull << left) - 1) : seen;
 }
 
 // The units are shared out evenly: share g begins at unit g * q + min(g, r), q
@@ -216,7 +237,8 @@ __device__ __forceinline__ u32x4 unpack8(uint32_t c, float s) {
   return y;
 }
 
-template <int NG, int MT, int WR>
+// Tree: what a row sees is told by its words of the mask (fdllm_tree_attention).
+template <int NG, int MT, int WR, bool Tree>
 __global__ void __launch_bounds__((CaShape<NG, MT, WR>::Threads), 2)
 k_cache_attn(const CacheAttnArgs a) {
   typedef CaShape<NG, MT, WR> S;
@@ -312,13 +334,18 @@ k_cache_attn(const CacheAttnArgs a) {
     const int r = (group * WR + wr) * MT + col;             // row of this lane
     const bool row_ok = r < seq.n * a.R;
     const int tok = row_ok ? r / a.R : 0, head = h * a.R + (row_ok ? r % a.R : 0);
-    const int start = a.q_start ? a.q_start[b] : seq.len - seq.n;
-    const int pos = start > INT32_MAX - tok ? INT32_MAX : start + tok;
-    const int end = row_ok ? visible_end(pos, a.blk, seq.len) : 0;
-    int all_see = row_ok ? end : INT32_MAX;                 // keys that every row of the wave sees
+    int end = 0, all_see;                                   // keys that every row of the wave sees
+    if constexpr (Tree) {
+      all_see = seq.len - seq.n;
+    } else {
+      const int start = a.q_start ? a.q_start[b] : seq.len - seq.n;
+      const int pos = start > INT32_MAX - tok ? INT32_MAX : start + tok;
+      end = row_ok ? visible_end(pos, a.blk, seq.len) : 0;
+      all_see = row_ok ? end : INT32_MAX;
 #pragma unroll
-    for (int x = 1; x < MT; x <<= 1) all_see = min(all_see, __shfl_xor(all_see, x));
-    all_see = __builtin_amdgcn_readfirstlane(all_see);
+      for (int x = 1; x < MT; x <<= 1) all_see = min(all_see, __shfl_xor(all_see, x));
+      all_see = __builtin_amdgcn_readfirstlane(all_see);
+    }
     Acc o[S::DT];
 #pragma unroll
     for (int t = 0; t < S::DT; ++t) o[t] = Acc{};
@@ -408,14 +435,27 @@ k_cache_attn(const CacheAttnArgs a) {
 
       // keys that a row does not see
       if (!there || base + kPage > all_see) {
-        const int seen = there ? end - base : 0;
+        if constexpr (Tree) {
+          unsigned long long seen = 0;
+          if (there && row_ok)
+            seen = tree_window(a.masks + (size_t)(seq.first + tok) * a.mask_w, a.mask_w, seq.n, base, seq.len - seq.n) >> (4 * part);
 #pragma unroll
-        for (int x = 0; x < SPT; ++x)
+          for (int x = 0; x < SPT; ++x)
 #pragma unroll
-          for (int i = 0; i < S::OR; ++i) {
-            const int key = x * MT + (MT == 32 ? i % 4 + 8 * (i / 4) + 4 * part : 4 * part + i);
-            sc[x][i] = key < seen ? sc[x][i] : kNegInf;
-          }
+            for (int i = 0; i < S::OR; ++i) {
+              const int key = x * MT + (MT == 32 ? i % 4 + 8 * (i / 4) : i);   // less the lane's part, shifted out
+              sc[x][i] = (uint32_t)(seen >> (key & 32)) >> (key & 31) & 1u ? sc[x][i] : kNegInf;
+            }
+        } else {
+          const int seen = there ? end - base : 0;
+#pragma unroll
+          for (int x = 0; x < SPT; ++x)
+#pragma unroll
+            for (int i = 0; i < S::OR; ++i) {
+              const int key = x * MT + (MT == 32 ? i % 4 + 8 * (i / 4) + 4 * part : 4 * part + i);
+              sc[x][i] = key < seen ? sc[x][i] : kNegInf;
+            }
+        }
       }
       // The running reference follows the maximum only where that has grown by
       // more than 2^8: weights up to 256 lose nothing in floating point, and
@@ -757,7 +797,7 @@ static bool ca_join_ok(const CaPlan& p) {
 // once per device and kernel, before the first launch there.
 constexpr int kCaMaxDevices = 64;
 
-template <int NG, int MT, int WR>
+template <int NG, int MT, int WR, bool Tree>
 static hipError_t ca_launch_one(const CacheAttnArgs& a, const CaPlan& p, hipStream_t st) {
   typedef CaShape<NG, MT, WR> S;
   static std::atomic<bool> allowed[kCaMaxDevices];
@@ -765,24 +805,53 @@ static hipError_t ca_launch_one(const CacheAttnArgs& a, const CaPlan& p, hipStre
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
   if (dev < 0 || dev >= kCaMaxDevices || !allowed[dev].load(std::memory_order_acquire)) {
-    e = hipFuncSetAttribute((const void*)k_cache_attn<NG, MT, WR>, hipFuncAttributeMaxDynamicSharedMemorySize,
+    e = hipFuncSetAttribute((const void*)k_cache_attn<NG, MT, WR, Tree>, hipFuncAttributeMaxDynamicSharedMemorySize,
                             S::LdsBytes);
     if (e != hipSuccess) return e;
     if (dev >= 0 && dev < kCaMaxDevices) allowed[dev].store(true, std::memory_order_release);
   }
-  hipLaunchKernelGGL((k_cache_attn<NG, MT, WR>), dim3((unsigned)p.wgs), dim3(S::Threads), S::LdsBytes, st, a);
+  hipLaunchKernelGGL((k_cache_attn<NG, MT, WR, Tree>), dim3((unsigned)p.wgs), dim3(S::Threads), S::LdsBytes, st, a);
   const dim3 join((unsigned)(p.items * WR), (unsigned)a.B), threads(kCaJoinWaves * kWave);
   if (p.join && p.split) hipLaunchKernelGGL((k_cache_join<NG, MT, WR, 4>), join, threads, 0, st, a, p.wgs);
   else if (p.join) hipLaunchKernelGGL((k_cache_join<NG, MT, WR, 1>), join, threads, 0, st, a, p.wgs);
   return hipGetLastError();
 }
 
-template <int NG>
+template <int NG, bool Tree>
 static hipError_t ca_launch(const CacheAttnArgs& a, const CaPlan& p, hipStream_t st) {
-  if (p.mt == 16) return ca_launch_one<NG, 16, 1>(a, p, st);
-  if (p.wr == 1) return ca_launch_one<NG, 32, 1>(a, p, st);
-  if (p.wr == 2) return ca_launch_one<NG, 32, 2>(a, p, st);
-  return ca_launch_one<NG, 32, 4>(a, p, st);
+  if (p.mt == 16) return ca_launch_one<NG, 16, 1, Tree>(a, p, st);
+  if (p.wr == 1) return ca_launch_one<NG, 32, 1, Tree>(a, p, st);
+  if (p.wr == 2) return ca_launch_one<NG, 32, 2, Tree>(a, p, st);
+  return ca_launch_one<NG, 32, 4, Tree>(a, p, st);
+}
+
+// Both calls: of a (masks, q_start, blk) either the masks or the others count.
+template <bool Tree>
+static fdllm_status ca_call(CacheAttnArgs a, int D, float scale, void* workspace, size_t workspace_bytes, fdllm_stream stream) {
+  if (a.T < 0 || a.B < 0 || a.max_q < 0 || a.H < 1 || a.Hk < 1 || a.n_pages < 0 || a.table_w < 0 || a.blk < 0 || a.mask_w < 0)
+    return FDLLM_ERR_INVALID_ARG;
+  if (!(scale > 0.0f) || scale > 3.0e38f) return FDLLM_ERR_INVALID_ARG;
+  if (!ca_sizes_ok(a.B, a.H, a.Hk, D, a.max_q, a.table_w, a.n_pages)) return FDLLM_ERR_SIZE;
+  if (Tree && a.mask_w < (a.max_q + 63) / 64) return FDLLM_ERR_INVALID_ARG;
+  if (a.T == 0 || a.B == 0 || a.max_q == 0) return FDLLM_OK;
+  if (!a.q || !a.cu_q || !a.kv_len || !a.out || (a.table_w > 0 && !a.table) || !a.cache || a.n_pages < 1)
+    return FDLLM_ERR_INVALID_ARG;
+  if (Tree && (!a.masks || (uintptr_t)a.masks & 7)) return FDLLM_ERR_INVALID_ARG;
+  if (a.q_stride < (int64_t)a.H * D || a.q_stride % 8) return FDLLM_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)a.q, (const void*)a.cache, (const void*)a.out, (const void*)workspace})
+    if ((uintptr_t)p & 15) return FDLLM_ERR_INVALID_ARG;
+  const CaPlan p = ca_plan(a.B, a.H, a.Hk, D, a.max_q, a.table_w);
+  if (!ca_join_ok(p)) return FDLLM_ERR_SIZE;
+  if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return FDLLM_ERR_WORKSPACE;
+  char* ws = (char*)workspace;
+  a.R = a.H / a.Hk;
+  a.c = scale * kLog2e;
+  a.plan = p.join ? (int32_t*)ws : nullptr;
+  a.part_ml = (float*)(ws + p.at_ml);
+  a.part = (float*)(ws + p.at_part);
+  hipStream_t st = (hipStream_t)stream;
+  const hipError_t e = D == 64 ? ca_launch<2, Tree>(a, p, st) : D == 96 ? ca_launch<3, Tree>(a, p, st) : ca_launch<4, Tree>(a, p, st);
+  return e == hipSuccess ? FDLLM_OK : FDLLM_ERR_HIP;
 }
 
 }  // namespace fdllm
@@ -806,25 +875,23 @@ fdllm_status fdllm_cache_attention(const void* q, int64_t q_stride, int T, const
                                    const int32_t* page_table, int table_width, const int32_t* kv_len,
                                    const int32_t* q_start, float scale, int blk, void* out, float* lse,
                                    void* workspace, size_t workspace_bytes, fdllm_stream stream) {
-  if (T < 0 || B < 0 || max_q < 0 || H < 1 || Hk < 1 || n_pages < 0 || table_width < 0 || blk < 0)
-    return FDLLM_ERR_INVALID_ARG;
-  if (!(scale > 0.0f) || scale > 3.0e38f) return FDLLM_ERR_INVALID_ARG;
-  if (!ca_sizes_ok(B, H, Hk, D, max_q, table_width, n_pages)) return FDLLM_ERR_SIZE;
-  if (T == 0 || B == 0 || max_q == 0) return FDLLM_OK;
-  if (!q || !cu_q || !kv_len || !out || (table_width > 0 && !page_table) || !cache || n_pages < 1) return FDLLM_ERR_INVALID_ARG;
-  if (q_stride < (int64_t)H * D || q_stride % 8) return FDLLM_ERR_INVALID_ARG;
-  for (const void* p : {q, (const void*)cache, (const void*)out, (const void*)workspace})
-    if ((uintptr_t)p & 15) return FDLLM_ERR_INVALID_ARG;
-  const CaPlan p = ca_plan(B, H, Hk, D, max_q, table_width);
-  if (!ca_join_ok(p)) return FDLLM_ERR_SIZE;
-  if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return FDLLM_ERR_WORKSPACE;
-  char* ws = (char*)workspace;
-  const CacheAttnArgs a{(const uint16_t*)q, q_stride, T, cache, n_pages, page_table, table_width, kv_len, cu_q,
-                        q_start, B, H, Hk, H / Hk, max_q, blk, scale * kLog2e, (uint16_t*)out, lse,
-                        p.join ? (int32_t*)ws : nullptr, (float*)(ws + p.at_ml), (float*)(ws + p.at_part)};
-  hipStream_t st = (hipStream_t)stream;
-  const hipError_t e = D == 64 ? ca_launch<2>(a, p, st) : D == 96 ? ca_launch<3>(a, p, st) : ca_launch<4>(a, p, st);
-  return e == hipSuccess ? FDLLM_OK : FDLLM_ERR_HIP;
+  CacheAttnArgs a{};
+  a.q = (const uint16_t*)q, a.q_stride = q_stride, a.T = T, a.cache = cache, a.n_pages = n_pages, a.table = page_table;
+  a.table_w = table_width, a.kv_len = kv_len, a.cu_q = cu_q, a.q_start = q_start, a.B = B, a.H = H, a.Hk = Hk;
+  a.max_q = max_q, a.blk = blk, a.out = (uint16_t*)out, a.lse = lse;
+  return ca_call<false>(a, D, scale, workspace, workspace_bytes, stream);
+}
+
+fdllm_status fdllm_tree_attention(const void* q, int64_t q_stride, int T, const int32_t* cu_q, int B, int max_q,
+                                  int H, int Hk, int D, const uint8_t* cache, int n_pages,
+                                  const int32_t* page_table, int table_width, const int32_t* kv_len,
+                                  const uint64_t* masks, int mask_words, float scale, void* out, float* lse,
+                                  void* workspace, size_t workspace_bytes, fdllm_stream stream) {
+  CacheAttnArgs a{};
+  a.q = (const uint16_t*)q, a.q_stride = q_stride, a.T = T, a.cache = cache, a.n_pages = n_pages, a.table = page_table;
+  a.table_w = table_width, a.kv_len = kv_len, a.cu_q = cu_q, a.B = B, a.H = H, a.Hk = Hk, a.max_q = max_q;
+  a.masks = (const unsigned long long*)masks, a.mask_w = mask_words, a.out = (uint16_t*)out, a.lse = lse;
+  return ca_call<true>(a, D, scale, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"
