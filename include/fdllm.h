@@ -636,11 +636,12 @@ fdllm_status fdllm_tree_attention(const void* q, int64_t q_stride, int T, const 
  *   equals;
  *   ids [T] int32: the tokens at the nodes (one outside [0, V) never stands).
  * Draws.  A number u and weights w give the lowest v for which w_0 + ... + w_v >
- *   u (w_0 + w_1 + ...); tokens less likely than 2^-1000 of the likeliest have
+ *   u (w_0 + w_1 + ...); tokens less likely than 2^-500 of the likeliest may have
  *   weight 0.  Numbers are floats in [0, 1): negative ones and NaN with a sign
  *   count as 0, others outside as 1 - 2^-24.  Probabilities, sums and comparisons
  *   are formed in 64 bits (a relative error below 1e-12), so that the token is the
- *   definition's unless u lies that near a border.
+ *   definition's unless u lies that near a border; equal float logits have borders
+ *   exactly where the definition has them.
  * Results are packed as the rows are: of a request's rows the first n_tokens get
  *   the tokens that follow (the drafted ones that stand, then the one drawn), the
  *   others -1.  logp [T] float (may be NULL): the logarithms of their
@@ -649,8 +650,8 @@ fdllm_status fdllm_tree_attention(const void* q, int64_t q_stride, int T, const 
  *   (all -inf) gets -1 for the token drawn, counted in n_tokens, and logp 0.
  *   Rows in more than one request: each must have the same temperature in all.
  * Sizes (FDLLM_ERR_SIZE beyond): V from 1 to 2^30, max_q at most FDLLM_MAX_TREE,
- *   B at most 65535.  For the same arguments a call is bitwise reproducible, whatever
- *   other requests are in it.
+ *   B at most 65535, T * V and B * min(max_q, T) * V at most about 2^41.  For the same
+ *   arguments a call is bitwise reproducible.
  */
 
 /*

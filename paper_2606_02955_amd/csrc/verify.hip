@@ -11,10 +11,11 @@
 // are formed in 64 bits.  Sums are kept by chunk of a row; a draw finds its chunk
 // in them and looks at that chunk alone again.
 //
-// One pass over all rows (k_vf_sums), then a chain's decision with the sums of
-// max(p - q, 0) of the one row that needs them (k_vd_decide) and its draw
-// (k_vd_draw), or the draws at a tree's nodes (k_vt_draw) and its walk
-// (k_vt_walk).
+// One pass over all rows (k_vf_sums); then a chain's decision, with the draw where
+// there are no drafter's logits (k_vd_decide), otherwise with the sums of max(p - q,
+// 0) of the row that needs them (apart for many requests: k_vd_rest) and the draw
+// behind it (k_vd_draw); or the draws at a tree's nodes and its walk (k_vt_draw,
+// k_vt_walk).
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>
@@ -29,6 +30,7 @@ typedef u32x4 u32x4_a2 __attribute__((aligned(2)));   // rows may begin at any e
 typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
 
 constexpr int kVfThreads = 256, kVfWaves = kVfThreads / kWave;
+constexpr int kVtThreads = 512;               // of the pass with a table
 constexpr int kVfLane = 32;                   // logits of a lane
 constexpr int kVfChunk = kVfLane * kWave;     // and of a chunk
 
@@ -51,6 +53,7 @@ struct VfArgs {
   struct VfPart* part;       // [sides][T][chunks]
   double* rest;              // [B][chunks]: sums of max(p - q, 0)
   struct VfChoice* choice;   // [B]
+  bool together;             // the decision forms rest as well
   int32_t* drawn;            // [T]: a tree's tokens
   float* drawn_lp;           // [T]
 };
@@ -96,11 +99,10 @@ __device__ __forceinline__ void fill_table(double* table) {
 __device__ __forceinline__ double exp2_steps(double d, double c, const double* table) {
   const double k = __builtin_fma(d, c, kVfRound);
   const double f = __builtin_fma(d, c, -(k - kVfRound));
-  const int lo = (int)(uint32_t)__double_as_longlong(k);
+  const int lo = __double2loint(k);
   const double t = *(const double*)((const char*)table + ((lo << 3) & (kVfSteps - 1) * 8));
-  const long long bits = __double_as_longlong(t);
-  const int hi = (int)(bits >> 32) + ((lo & ~(kVfSteps - 1)) << 13);   // the whole powers of two
-  const double scale = __longlong_as_double(((long long)hi << 32) | (uint32_t)bits);
+  const int hi = __double2hiint(t) + ((lo & ~(kVfSteps - 1)) << 13);   // the whole powers of two
+  const double scale = __hiloint2double(hi, __double2loint(t));
   double p = __builtin_fma(f, 0x1.c6b08d704a0bfp-26, 0x1.ebfbf049a8568p-17);
   p = __builtin_fma(f, p, 0x1.62e42fefa39efp-8);
   p = __builtin_fma(f, p, 1.0);
@@ -127,6 +129,29 @@ __device__ __forceinline__ double number_of(float u) {
 }
 
 // ---------------------------------------------------------------------------
+// Bfloat16 logits are few: between 2^-18 and 64 there are 6144, both signs taken
+// together.  Where a workgroup has many of one temperature it looks 2^(x c) up
+// (four instructions a logit for sixteen), without a reference: for 64 c <= 480 all
+// terms and sums are numbers of 64 bits.  Entries lie by the bits of a logit with its
+// sign moved to the end, so that two are told from one word at a time.
+// ---------------------------------------------------------------------------
+constexpr int kVtLow = 109 << 8, kVtHigh = 133 << 8, kVtEntries = kVtHigh - kVtLow;   // exponents -18 to 5
+constexpr double kVtMost = 480.0 / 64.0 * kVfSteps;   // c in steps, at most
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ void fill_lookup(double* lookup, double c, const double* table, int threads) {
+  for (int i = threadIdx.x; i < kVtEntries; i += threads) {
+    const uint32_t turned = i + kVtLow;
+    lookup[i] = exp2_steps((double)__uint_as_float((turned >> 1 | (turned & 1) << 15) << 16), c, table);
+  }
+}
+// Two logits' places in the table; beyond its end where they are not in it.
+__device__ __forceinline__ u16x2 places_of(uint32_t word) {
+  const u16x2 w = __builtin_bit_cast(u16x2, word);
+  return w * (unsigned short)2 + ((w >> 15) - (unsigned short)kVtLow);
+}
+
+// ---------------------------------------------------------------------------
 // a lane's logits of a chunk: vectors of 16 bytes, a wave's side by side
 // ---------------------------------------------------------------------------
 template <bool F32>
@@ -144,7 +169,7 @@ struct VfRow {
     if ((chunk + 1) * kVfChunk <= V) {
       const char* p = row + (size_t)chunk * kVfChunk * Bytes;
 #pragma unroll
-      for (int j = 0; j < Vecs; ++j) v[j] = *(const Vec*)(p + (uint32_t)(j * kWave + lane) * 16u);
+      for (int j = 0; j < Vecs; ++j) v[j] = __builtin_nontemporal_load((const Vec*)(p + (uint32_t)(j * kWave + lane) * 16u));
       return;
     }
 #pragma unroll
@@ -177,82 +202,200 @@ __device__ __forceinline__ float logit_at(const char* row, int v) {
 }
 
 // ---------------------------------------------------------------------------
-// the pass over all rows.  A wave takes every so-and-so-many-th chunk of one.
+// the pass over all rows.  The units of work are chunks: of a request those of
+// its rows, then those of its drafter's.  Every workgroup takes an equal share,
+// whatever the requests' lengths, its waves one chunk after another in turn, the
+// next one's loads under way.
 // ---------------------------------------------------------------------------
-template <bool F32>
-__global__ void __launch_bounds__(kVfThreads)
-k_vf_sums(const VfArgs a, int sides) {
+struct VfRequest {
+  int first, n, rows;   // rows: of both sides
+  bool warm;
+  double c;
+};
+__device__ __forceinline__ VfRequest request_of(const VfArgs& a, int b) {
+  VfRequest r;
+  r.n = packed_rows(a.cu_q, b, a.T, a.max_q, &r.first);
+  r.c = 0.0;
+  r.warm = scale_for(a, b, &r.c);
+  r.rows = r.n + (a.draft && r.warm ? max(r.n - 1, 0) : 0);   // (the drafter's last row is not read)
+  return r;
+}
+
+// Lookup: terms of bfloat16 logits out of a table.
+template <bool F32, bool Lookup>
+__global__ void __launch_bounds__(Lookup ? kVtThreads : kVfThreads, Lookup ? 4 : 1)
+k_vf_sums(const VfArgs a) {
   typedef VfRow<F32> Row;
+  constexpr int Threads = Lookup ? kVtThreads : kVfThreads, Waves = Threads / kWave;
   __shared__ double s_table[kVfSteps];
-  const int b = blockIdx.z, i = blockIdx.y / sides, side = blockIdx.y % sides;
-  int first;
-  const int n = packed_rows(a.cu_q, b, a.T, a.max_q, &first);
-  if (i >= n - side) return;   // (the drafter's last row is not read)
-  double c = 0.0;
-  const bool warm = scale_for(a, b, &c);
-  if (!warm && side) return;
+  __shared__ double s_lookup[Lookup ? kVtEntries : 1];
+  __shared__ int s_sum[Waves], s_at[2];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+
+  // all units, this workgroup's, and the request of its first (a lane, from 65
+  // requests on a thread, counts a few neighbouring requests; a scan adds up)
+  const bool apart = a.B <= kWave;
+  const int who = apart ? lane : tid, per = apart ? 1 : (a.B + Threads - 1) / Threads;
+  const int b0 = min(who * per, a.B), b1 = min(b0 + per, a.B);
+  int mine = 0;
+  for (int i = b0; i < b1; ++i) mine += request_of(a, i).rows * a.chunks;
+  int incl = mine;
+#pragma unroll
+  for (int x = 1; x < kWave; x <<= 1) {
+    const int y = __shfl_up(incl, x);
+    if (lane >= x) incl += y;
+  }
+  int units = __builtin_amdgcn_readlane(incl, kWave - 1);
   fill_table(s_table);
+  if (lane == kWave - 1) s_sum[wave] = incl;
   __syncthreads();
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const char* row = side ? a.draft + (size_t)(first + i) * a.draft_stride : a.logits + (size_t)(first + i) * a.stride;
-  VfPart* part = a.part + ((size_t)side * a.T + first + i) * a.chunks;
-  const int step = gridDim.x * kVfWaves;
-  int ch = blockIdx.x * kVfWaves + wave;
-  if (ch >= a.chunks) return;
-  const double lowest = kVfCut / c;
-  Row next;
-  next.load(row, a.V, ch, lane);
-  for (; ch < a.chunks; ch += step) {
-    const Row x = next;
-    if (ch + step < a.chunks) next.load(row, a.V, ch + step, lane);
-    float m = kNegInf;
+  if (!apart) {
+    units = 0;
 #pragma unroll
-    for (int j = 0; j < Row::Vecs; ++j)
+    for (int w = 0; w < Waves; ++w) {
+      if (w == wave) incl += units;
+      units += s_sum[w];
+    }
+  }
+  const int q = units / gridDim.x, r = units % gridDim.x, g = blockIdx.x;
+  int u = g * q + min(g, r);
+  const int u_end = u + q + (g < r ? 1 : 0);
+  if (u >= u_end) return;
+  int b, before;
+  const bool here = u >= incl - mine && u < incl;
+  if (apart) {
+    b = __ffsll((unsigned long long)__ballot(here)) - 1;
+    before = __builtin_amdgcn_readlane(incl - mine, b);
+  } else {
+    if (here) {
+      int i = b0, n = incl - mine;
+      for (;; ++i) {
+        const int k = request_of(a, i).rows * a.chunks;
+        if (u < n + k) break;
+        n += k;
+      }
+      s_at[0] = i;
+      s_at[1] = n;
+    }
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(s_at[0]);
+    before = __builtin_amdgcn_readfirstlane(s_at[1]);
+  }
+
+  double filled = 0.0;   // the lookup's c
+  for (; u < u_end; ++b) {
+    const VfRequest rq = request_of(a, b);
+    const bool looks_up = Lookup && rq.warm && rq.c <= kVtMost;
+    const int behind = before + rq.rows * a.chunks, upto = min(u_end, behind);
+    const double lowest = kVfCut / rq.c;
+    const auto row_of = [&](int v, int* ch, size_t* place) {
+      const int at = v - before, i = at / a.chunks;
+      *ch = at - i * a.chunks;
+      const bool drafter = i >= rq.n;
+      const int t = rq.first + (drafter ? i - rq.n : i);
+      *place = ((size_t)(drafter ? a.T : 0) + t) * a.chunks + *ch;
+      return drafter ? a.draft + (size_t)t * a.draft_stride : a.logits + (size_t)t * a.stride;
+    };
+    int v = u + wave, ch_next = 0;
+    size_t place_next = 0;
+    Row next;
+    if (v < upto) {
+      const char* row = row_of(v, &ch_next, &place_next);
+      next.load(row, a.V, ch_next, lane);
+    }
+    if (looks_up && rq.rows > 0 && rq.c != filled) {
+      __syncthreads();
+      fill_lookup(s_lookup, rq.c, s_table, Threads);
+      filled = rq.c;
+      __syncthreads();
+    }
+    for (; v < upto; v += Waves) {
+      const Row x = next;
+      const int ch = ch_next;
+      const size_t place = place_next;
+      if (v + Waves < upto) {
+        const char* row = row_of(v + Waves, &ch_next, &place_next);
+        next.load(row, a.V, ch_next, lane);
+      }
+      if constexpr (Lookup) {
+        if (looks_up) {
+          u16x2 at[Row::Vecs][4], most = 0;
 #pragma unroll
-      for (int e = 0; e < Row::Per; ++e) m = fmaxf(m, x.at(j, e));
-    m = wave_max(m);
-    double s = 0.0;
-    int at = 0;
-    if (!warm) {
-      at = INT32_MAX;
+          for (int j = 0; j < Row::Vecs; ++j)
 #pragma unroll
-      for (int j = Row::Vecs - 1; j >= 0; --j)
+            for (int e = 0; e < 4; ++e) {
+              at[j][e] = places_of(x.v[j][e]);
+              most = __builtin_elementwise_max(most, at[j][e]);
+            }
+          if (!__any(max(most[0], most[1]) >= kVtEntries)) {
+            double s = 0.0, s1 = 0.0;
 #pragma unroll
-        for (int e = Row::Per - 1; e >= 0; --e)
-          if (x.at(j, e) == m) at = Row::index(ch, j, lane) + e;
-      at = wave_min(at);
-    } else if (m > kNegInf) {
-      const double M = m;
-      double s1 = 0.0;
+            for (int j = 0; j < Row::Vecs; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t two = __builtin_bit_cast(uint32_t, at[j][e]);
+                s += s_lookup[two & 0xffffu];
+                s1 += s_lookup[two >> 16];
+              }
+            s = wave_sum_f64(s + s1);
+            if (lane == 0) a.part[place] = VfPart{s, 0.0f, 0};
+            continue;
+          }
+        }
+      }
+      float m = kNegInf;
 #pragma unroll
       for (int j = 0; j < Row::Vecs; ++j)
 #pragma unroll
-        for (int e = 0; e < Row::Per; e += 2) {
-          s += exp2_steps(fmax((double)x.at(j, e) - M, lowest), c, s_table);
-          s1 += exp2_steps(fmax((double)x.at(j, e + 1) - M, lowest), c, s_table);
-        }
-      s = wave_sum_f64(s + s1);
+        for (int e = 0; e < Row::Per; ++e) m = fmaxf(m, x.at(j, e));
+      m = wave_max(m);
+      double s = 0.0;
+      int at = 0;
+      if (!rq.warm) {
+        at = INT32_MAX;
+#pragma unroll
+        for (int j = Row::Vecs - 1; j >= 0; --j)
+#pragma unroll
+          for (int e = Row::Per - 1; e >= 0; --e)
+            if (x.at(j, e) == m) at = Row::index(ch, j, lane) + e;
+        at = wave_min(at);
+      } else if (m > kNegInf) {
+        const double M = m;
+        double s1 = 0.0;
+#pragma unroll
+        for (int j = 0; j < Row::Vecs; ++j)
+#pragma unroll
+          for (int e = 0; e < Row::Per; e += 2) {
+            s += exp2_steps(fmax((double)x.at(j, e) - M, lowest), rq.c, s_table);
+            s1 += exp2_steps(fmax((double)x.at(j, e + 1) - M, lowest), rq.c, s_table);
+          }
+        s = wave_sum_f64(s + s1);
+      }
+      if (lane == 0) a.part[place] = VfPart{s, m, at};
     }
-    if (lane == 0) part[ch] = VfPart{s, m, at};
+    u = upto;
+    before = behind;
   }
 }
 
 // ---------------------------------------------------------------------------
-// wave-level pieces of what follows
+// pieces of what follows
 // ---------------------------------------------------------------------------
-// A chunk's sum brought to the row's maximum M.
-__device__ __forceinline__ double part_weight(const VfPart& p, float M, double c) {
+// A chunk's sum brought to the row's reference M.
+__device__ __forceinline__ double part_weight(const VfPart& p, float M, double c, const double* table) {
   const double d = (double)p.m - (double)M;
-  return d * c > kVfCut ? p.s * exp2(d * c * (1.0 / kVfSteps)) : 0.0;   // (-inf: 0)
+  return d * c > kVfCut ? p.s * exp2_steps(d, c, table) : 0.0;   // (-inf: 0)
 }
 
-__device__ __forceinline__ VfStats row_stats(const VfPart* part, int chunks, bool warm, double c, int lane) {
+// By a wave.
+__device__ __forceinline__ VfStats row_stats(const VfPart* part, int chunks, bool warm, double c, int lane,
+                                             const double* table) {
   VfStats r{0.0, kNegInf, 0};
   for (int ch = lane; ch < chunks; ch += kWave) r.M = fmaxf(r.M, part[ch].m);
   r.M = wave_max(r.M);
   if (!(r.M > kNegInf)) return r;
   if (warm) {
-    for (int ch = lane; ch < chunks; ch += kWave) r.Z += part_weight(part[ch], r.M, c);
+    for (int ch = lane; ch < chunks; ch += kWave) r.Z += part_weight(part[ch], r.M, c, table);
     r.Z = wave_sum_f64(r.Z);
   } else {
     int at = INT32_MAX;
@@ -265,17 +408,42 @@ __device__ __forceinline__ VfStats row_stats(const VfPart* part, int chunks, boo
   return r;
 }
 
-// p of one token.
-template <bool F32>
-__device__ __forceinline__ double probability(const char* row, int v, const VfStats& r, double c) {
-  const double d = ((double)logit_at<F32>(row, v) - (double)r.M) * c;
-  return d > kVfCut ? exp2(d * (1.0 / kVfSteps)) / r.Z : 0.0;
+// p of one token, and its logarithm.
+__device__ __forceinline__ double probability(float x, const VfStats& r, double c, const double* table) {
+  const double d = (double)x - (double)r.M;
+  return d * c > kVfCut ? exp2_steps(d, c, table) / r.Z : 0.0;
 }
-template <bool F32>
-__device__ __forceinline__ float log_probability(const char* row, int v, const VfStats& r, double c) {
-  const double d = ((double)logit_at<F32>(row, v) - (double)r.M) * c;
-  return (float)(d * (0.69314718055994530942 / kVfSteps) - log(r.Z));
+__device__ __forceinline__ float log_probability(float x, const VfStats& r, double c) {
+  return (float)(((double)x - (double)r.M) * c * (0.69314718055994530942 / kVfSteps) - log(r.Z));
 }
+
+// Eight logits from an element on, a thread's of a piece that is looked at again.
+constexpr int kVfEight = 8;
+template <bool F32>
+struct VfEight {
+  u32x4 v[F32 ? 2 : 1];
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (F32) return __uint_as_float(v[e / 4][e % 4]);
+    else return __uint_as_float(e % 2 ? v[0][e / 2] & 0xffff0000u : v[0][e / 2] << 16);
+  }
+  __device__ __forceinline__ void load(const char* row, int V, int at) {
+    if (at + kVfEight <= V) {
+      if constexpr (F32) {
+        v[0] = *(const u32x4_a4*)(row + (size_t)at * 4);
+        v[1] = *(const u32x4_a4*)(row + (size_t)at * 4 + 16);
+      } else {
+        v[0] = *(const u32x4_a2*)(row + (size_t)at * 2);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVfEight; ++e) {
+        const uint32_t x = __float_as_uint(at + e < V ? logit_at<F32>(row, at + e) : kNegInf);
+        if constexpr (F32) v[e / 4][e % 4] = x;
+        else v[0][e / 2] = e % 2 ? v[0][e / 2] | x : x >> 16;
+      }
+    }
+  }
+};
 
 // The weights that a token is drawn from: 2^((x - M) c) of a row, without the
 // token `without`, or, where there is a row q, max(p - q, 0).
@@ -288,40 +456,27 @@ struct VfWeights {
   int without;
 
   __device__ VfWeights(const char* p_, const VfStats& sp_, const char* q_, const VfStats& sq_, double c_, int without_)
-      : p(p_), q(q_), sp(sp_), sq(sq_), c(c_), ip(1.0 / sp_.Z), iq(q_ ? 1.0 / sq_.Z : 0.0), lowest(kVfCut / c_),
+      : p(p_), q(q_), sp(sp_), sq(sq_), c(c_), ip(q_ ? 1.0 / sp_.Z : 1.0), iq(q_ ? 1.0 / sq_.Z : 0.0), lowest(kVfCut / c_),
         without(without_) {}
 
-  __device__ __forceinline__ void of_chunk(int V, int ch, int lane, const double* table, double (&w)[kVfLane]) const {
-    typedef VfRow<F32> Row;
-    Row x, y;
-    x.load(p, V, ch, lane);
-    if (q) y.load(q, V, ch, lane);
+  __device__ __forceinline__ void load(int V, int at, VfEight<F32>& x, VfEight<F32>& y) const {
+    x.load(p, V, at);
+    if (q) y.load(q, V, at);
+  }
+  // of eight tokens from their logits in both rows
+  __device__ __forceinline__ void of(int at, const VfEight<F32>& x, const VfEight<F32>& y, const double* table,
+                                     double (&w)[kVfEight]) const {
 #pragma unroll
-    for (int j = 0; j < Row::Vecs; ++j)
-#pragma unroll
-      for (int e = 0; e < Row::Per; ++e) w[j * Row::Per + e] = weight_of(x.at(j, e), sp.M, c, lowest, table);
+    for (int e = 0; e < kVfEight; ++e) w[e] = weight_of(x.at(e), sp.M, c, lowest, table);
     if (q) {
 #pragma unroll
-      for (int j = 0; j < Row::Vecs; ++j)
-#pragma unroll
-        for (int e = 0; e < Row::Per; ++e) {
-          double& v = w[j * Row::Per + e];
-          v = fmax(v * ip - weight_of(y.at(j, e), sq.M, c, lowest, table) * iq, 0.0);
-        }
-    } else if (without >= 0) {
-#pragma unroll
-      for (int j = 0; j < Row::Vecs; ++j)
-#pragma unroll
-        for (int e = 0; e < Row::Per; ++e)
-          if (Row::index(ch, j, lane) + e == without) w[j * Row::Per + e] = 0.0;
+      for (int e = 0; e < kVfEight; ++e) w[e] = fmax(w[e] * ip - weight_of(y.at(e), sq.M, c, lowest, table) * iq, 0.0);
     }
-  }
-  __device__ double sum_of_chunk(int V, int ch, int lane, const double* table) const {
-    double w[kVfLane], s = 0.0;
-    of_chunk(V, ch, lane, table, w);
+    if (without >= 0) {
 #pragma unroll
-    for (int i = 0; i < kVfLane; ++i) s += w[i];
-    return wave_sum_f64(s);
+      for (int e = 0; e < kVfEight; ++e)
+        if (at + e == without) w[e] = 0.0;
+    }
   }
 };
 
@@ -335,137 +490,272 @@ __device__ __forceinline__ double wave_scan_f64(double v, int lane) {
   return v;
 }
 
-// The token drawn with number u, -1 where all weights are 0; sum_of(chunk): a
-// chunk's sum, the same in every lane that asks for it.
-template <bool F32, typename F>
-__device__ int draw_token(const VfWeights<F32>& weights, int V, int chunks, const double* table, double u, int lane,
-                          F&& sum_of) {
-  typedef VfRow<F32> Row;
-  const int per = (chunks + kWave - 1) / kWave, c0 = lane * per, c1 = min(c0 + per, chunks);
-  double mine = 0.0;
-  for (int ch = c0; ch < c1; ++ch) mine += sum_of(ch);
+struct VfDrawn {
+  int token;   // -1: all weights are 0
+  float x;     // its logit
+};
+template <int Waves>
+struct VfDrawScratch {
+  double total[Waves];
+  int best[Waves], last[Waves];
+  VfDrawn drawn;
+};
+
+// The token drawn with number u, by a workgroup; all threads get it.  A row is
+// `pieces` pieces of `each` tokens (at most eight a thread), sum_of(piece) the sum
+// of one's weights, the same for every lane that asks.
+constexpr int kVfOwn = 4;   // sums that a lane keeps
+template <bool F32, int Waves, typename F>
+__device__ VfDrawn draw_token(const VfWeights<F32>& weights, int V, int pieces, int each, const double* table, double u,
+                              VfDrawScratch<Waves>* s, F&& sum_of) {
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  // the piece, by every wave for itself: a lane adds up neighbouring pieces
+  const int per = (pieces + kWave - 1) / kWave, c0 = min(lane * per, pieces), c1 = min(c0 + per, pieces);
+  double mine = 0.0, own[kVfOwn];
+#pragma unroll
+  for (int i = 0; i < kVfOwn; ++i) {
+    own[i] = c0 + i < c1 ? sum_of(c0 + i) : 0.0;
+    mine += own[i];
+  }
+  for (int k = c0 + kVfOwn; k < c1; ++k) mine += sum_of(k);
   const double incl = wave_scan_f64(mine, lane);
   const double total = readlane_f64(incl, kWave - 1);
-  if (!(total > 0.0)) return -1;
   const double target = u * total;
   const unsigned long long some = __ballot(mine > 0.0), over = __ballot(incl > target) & some;
-  if (!some) return -1;
+  if (!some) return VfDrawn{-1, 0.0f};
   const int L = over ? __ffsll(over) - 1 : 63 - __clzll(some);
-  double before = readlane_f64(incl - mine, L);
-  int ch = -1;
-  for (int k = L * per; k < min((L + 1) * per, chunks); ++k) {   // of the lane's chunks the first beyond, or its last
-    const double s = sum_of(k);
-    if (!(s > 0.0)) continue;
-    ch = k;
-    if (before + s > target) break;
-    if (k + 1 < min((L + 1) * per, chunks)) before += s;
-  }
-  ch = __builtin_amdgcn_readfirstlane(ch);
-  if (ch < 0) return -1;
-  double w[kVfLane], from[Row::Vecs];
-  weights.of_chunk(V, ch, lane, table, w);
-  // sums before each vector of the lane
+  // of the lane's pieces the first beyond, or the last with any
+  double before = readlane_f64(incl - mine, L), held = 0.0;
+  int piece = -1;
+  bool found = false;
+  const auto look = [&](int k, double w) {
+    if (found || !(w > 0.0)) return;
+    before += held;
+    held = w;
+    piece = k;
+    found = before + w > target;
+  };
 #pragma unroll
-  for (int j = 0; j < Row::Vecs; ++j) {
-    double s = 0.0;
+  for (int i = 0; i < kVfOwn; ++i) look(L * per + i, readlane_f64(own[i], L));
+  for (int k = L * per + kVfOwn; k < min((L + 1) * per, pieces) && !found; ++k) look(k, sum_of(k));
+  piece = __builtin_amdgcn_readfirstlane(piece);
+  if (piece < 0 || piece >= pieces) return VfDrawn{-1, 0.0f};
+
+  // its tokens
+  const int at = piece * each + tid * kVfEight;
+  VfEight<F32> x, y;
+  double w[kVfEight], sum = 0.0;
 #pragma unroll
-    for (int e = 0; e < Row::Per; ++e) s += w[j * Row::Per + e];
-    const double in = wave_scan_f64(s, lane);
-    from[j] = before + (in - s);
-    before += readlane_f64(in, kWave - 1);
+  for (int e = 0; e < kVfEight; ++e) w[e] = 0.0;
+  if (tid * kVfEight < each) {
+    weights.load(V, at, x, y);
+    weights.of(at, x, y, table, w);
+#pragma unroll
+    for (int e = 0; e < kVfEight; ++e) sum += w[e];
   }
+  const double in = wave_scan_f64(sum, lane);
+  if (lane == kWave - 1) s->total[wave] = in;
+  __syncthreads();
+  double from = before + (in - sum);
+#pragma unroll
+  for (int k = 0; k < Waves; ++k)
+    if (k < wave) from += s->total[k];
   int best = INT32_MAX, last = -1;
 #pragma unroll
-  for (int j = 0; j < Row::Vecs; ++j) {
-    double s = from[j];
-#pragma unroll
-    for (int e = 0; e < Row::Per; ++e) {
-      const double x = w[j * Row::Per + e];
-      const int at = Row::index(ch, j, lane) + e;
-      s += x;
-      if (x > 0.0 && at < V) {
-        last = at;
-        if (s > target) best = min(best, at);
-      }
+  for (int e = 0; e < kVfEight; ++e) {
+    from += w[e];
+    if (w[e] > 0.0 && at + e < V) {
+      last = at + e;
+      if (from > target) best = min(best, at + e);
     }
   }
-  best = wave_min(best);
-  // the chunk's sum was formed in another order: past its end by a rounding, its last
-  return best != INT32_MAX ? best : -wave_min(-last);
+  const int wave_best = wave_min(best), wave_last = -wave_min(-last);
+  if (lane == 0) s->best[wave] = wave_best, s->last[wave] = wave_last;
+  __syncthreads();
+  int token = INT32_MAX, end = -1;
+#pragma unroll
+  for (int k = 0; k < Waves; ++k) {
+    token = min(token, s->best[k]);
+    end = max(end, s->last[k]);
+  }
+  // the piece's sum was formed in another order: past its end by a rounding, its last
+  if (token == INT32_MAX) token = end;
+  if (token < 0) return VfDrawn{-1, 0.0f};
+#pragma unroll
+  for (int e = 0; e < kVfEight; ++e)
+    if (tid * kVfEight < each && at + e == token) s->drawn = VfDrawn{token, x.at(e)};
+  __syncthreads();
+  return s->drawn;
 }
 
 // ---------------------------------------------------------------------------
-// a chain: which drafts stand, and the sums of max(p - q, 0) where one fell.
-// Every workgroup of a request decides by itself; the first writes it down.
+// a chain: which drafts stand, the sums of max(p - q, 0) by piece where one fell,
+// and the draw.  Every workgroup of a request decides by itself, a wave a draft;
+// the first writes it down.  (One launch, the last workgroup of a request to be
+// done drawing, took longer than two: to tell it that the others' sums are written
+// is to write an XCD's cache back, 48 chains 66 -> 114 to 165 us.)
 // ---------------------------------------------------------------------------
+constexpr int kVdThreads = 1024, kVdWaves = kVdThreads / kWave;
+constexpr int kVdPiece = kWave * kVfEight, kVdPieces = kVfChunk / kVdPiece;   // pieces of a chunk
+
+// A wave's pieces of a row: k0, k0 + step, ...
 template <bool F32>
-__global__ void __launch_bounds__(kVfThreads)
+__device__ __forceinline__ void rest_sums(const VfWeights<F32>& weights, int V, int k0, int end, int step, double* rest,
+                                          const double* table, int lane) {
+  constexpr int Ahead = 2;   // pieces under way
+  for (; k0 < end; k0 += Ahead * step) {
+    VfEight<F32> x[Ahead], y[Ahead];
+#pragma unroll
+    for (int i = 0; i < Ahead; ++i)
+      if (k0 + i * step < end) weights.load(V, (k0 + i * step) * kVdPiece + lane * kVfEight, x[i], y[i]);
+#pragma unroll
+    for (int i = 0; i < Ahead; ++i) {
+      const int k = k0 + i * step;
+      if (k >= end) break;
+      double w[kVfEight], s = 0.0;
+      weights.of(k * kVdPiece + lane * kVfEight, x[i], y[i], table, w);
+#pragma unroll
+      for (int e = 0; e < kVfEight; ++e) s += w[e];
+      s = wave_sum_f64(s);
+      if (lane == 0) rest[k] = s;
+    }
+  }
+}
+
+// The token after the drafts that stand, by a workgroup.
+template <bool F32, int Waves>
+__device__ void draw_next(const VfArgs& a, int b, const VfChoice& r, bool warm, double c, const double* table,
+                          VfDrawScratch<Waves>* scratch) {
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const char* row = a.logits + (size_t)r.row * a.stride;
+  const VfPart* part = a.part + (size_t)r.row * a.chunks;
+  VfDrawn y{-1, 0.0f};
+  if (!(r.p.Z > 0.0)) {
+    // no token can be
+  } else if (!warm) {
+    y.token = r.p.first;
+  } else {
+    const double u = number_of(a.u_draw[b]);
+    if (r.rest && a.draft) {
+      const VfWeights<F32> w(row, r.p, a.draft + (size_t)r.row * a.draft_stride, r.q, c, -1);
+      const int pieces = a.chunks * kVdPieces;
+      const double* rest = a.rest + (size_t)b * pieces;
+      y = draw_token(w, a.V, pieces, kVdPiece, table, u, scratch, [&](int k) { return rest[k]; });
+    } else if (r.rest) {
+      // all but the draft: its chunk's sum without it
+      const int x = a.ids[r.row + 1];
+      const VfWeights<F32> w(row, r.p, nullptr, r.q, c, x >= 0 && x < a.V ? x : -1);
+      const int its = w.without >= 0 ? x / kVfChunk : -1;
+      double other = 0.0;
+      if (its >= 0) {
+        if (tid * kVfEight < kVfChunk) {
+          VfEight<F32> l;
+          double v[kVfEight];
+          w.load(a.V, its * kVfChunk + tid * kVfEight, l, l);
+          w.of(its * kVfChunk + tid * kVfEight, l, l, table, v);
+#pragma unroll
+          for (int e = 0; e < kVfEight; ++e) other += v[e];
+        }
+        other = wave_sum_f64(other);
+        if (lane == 0) scratch->total[wave] = other;
+        __syncthreads();
+        other = 0.0;
+#pragma unroll
+        for (int k = 0; k < Waves; ++k) other += scratch->total[k];
+        __syncthreads();
+      }
+      y = draw_token(w, a.V, a.chunks, kVfChunk, table, u, scratch,
+                     [&](int ch) { return ch == its ? other : part_weight(part[ch], r.p.M, c, table); });
+    }
+    if (y.token < 0) {
+      const VfWeights<F32> w(row, r.p, nullptr, r.q, c, -1);
+      __syncthreads();
+      y = draw_token(w, a.V, a.chunks, kVfChunk, table, u, scratch,
+                     [&](int ch) { return part_weight(part[ch], r.p.M, c, table); });
+    }
+  }
+  if (tid == 0) {
+    a.tokens[r.row] = y.token;
+    if (a.logp) a.logp[r.row] = warm && y.token >= 0 ? log_probability(y.x, r.p, c) : 0.0f;
+  }
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(kVdThreads)
 k_vd_decide(const VfArgs a) {
   __shared__ double s_table[kVfSteps];
-  __shared__ VfChoice s_choice;
-  __shared__ int s_fell[kVfWaves];
+  __shared__ VfChoice s_choice[kVdWaves];
+  __shared__ VfDrawScratch<kVdWaves> s_draw;
   const int b = blockIdx.y;
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const bool writes = blockIdx.x == 0;
-  int first;
-  const int n = packed_rows(a.cu_q, b, a.T, a.max_q, &first);
+  const VfRequest rq = request_of(a, b);
+  const int first = rq.first, n = rq.n;
   if (n == 0) {
     if (writes && tid == 0) {
       a.n_tokens[b] = 0;
-      if (a.choice) a.choice[b].row = -1;
+      a.choice[b].row = -1;
     }
     return;
   }
   fill_table(s_table);
-  double c = 0.0;
-  const bool warm = scale_for(a, b, &c);
-  const bool with_q = warm && a.draft;
+  __syncthreads();
+  const bool warm = rq.warm, with_q = warm && a.draft;
+  const double c = rq.c;
   const VfPart* p_part = a.part + (size_t)first * a.chunks;
   const VfPart* q_part = a.part + ((size_t)a.T + first) * a.chunks;
 
-  // a wave a draft, those after one that fell for nothing
-  int fell = n - 1;
-  for (int i = wave; i < fell; i += kVfWaves) {
-    const VfStats sp = row_stats(p_part + (size_t)i * a.chunks, a.chunks, warm, c, lane);
-    VfStats sq{1.0, 0.0, 0};
-    if (with_q) sq = row_stats(q_part + (size_t)i * a.chunks, a.chunks, warm, c, lane);
-    const int x = a.ids[first + i + 1];
-    const char* row = a.logits + (size_t)(first + i) * a.stride;
-    bool stands = x >= 0 && x < a.V && sp.Z > 0.0 && sq.Z > 0.0;
-    if (stands && warm) {
-      const double p = probability<F32>(row, x, sp, c);
-      double q = 1.0;
-      if (with_q) q = probability<F32>(a.draft + (size_t)(first + i) * a.draft_stride, x, sq, c);
-      stands = number_of(a.u[first + i]) * q < p;
-    } else if (stands) {
-      stands = x == sp.first;
+  // each wave goes on to the first of its drafts that falls, or to the last row
+  VfChoice r{};
+  int fell = n;
+  for (int i = wave; i < n; i += kVdWaves) {
+    bool stands = i < n - 1;
+    const int x = stands ? a.ids[first + i + 1] : -1;
+    const bool real = x >= 0 && x < a.V;
+    float lx = 0.0f, lq = 0.0f, u = 0.0f;   // (loaded before the sums are waited for)
+    if (real && warm) {
+      lx = logit_at<F32>(a.logits + (size_t)(first + i) * a.stride, x);
+      if (with_q) lq = logit_at<F32>(a.draft + (size_t)(first + i) * a.draft_stride, x);
+      u = a.u[first + i];
     }
-    if (!stands) fell = i;
-    else if (writes && a.logp && lane == 0) a.logp[first + i] = warm ? log_probability<F32>(row, x, sp, c) : 0.0f;
-  }
-  if (lane == 0) s_fell[wave] = fell;
-  __syncthreads();
-  int m = n - 1;
-#pragma unroll
-  for (int w = 0; w < kVfWaves; ++w) m = min(m, s_fell[w]);
-  if (wave == 0) {
-    VfChoice r{};
-    r.p = row_stats(p_part + (size_t)m * a.chunks, a.chunks, warm, c, lane);
-    r.q = VfStats{0.0, kNegInf, 0};
-    if (with_q && m < n - 1) r.q = row_stats(q_part + (size_t)m * a.chunks, a.chunks, warm, c, lane);
-    r.row = first + m;
-    r.rest = warm && m < n - 1 && (!a.draft || r.q.Z > 0.0);
-    if (lane == 0) {
-      s_choice = r;
-      if (writes) {
-        if (a.choice) a.choice[b] = r;
-        a.n_tokens[b] = m + 1;
+    r.p = row_stats(p_part + (size_t)i * a.chunks, a.chunks, warm, c, lane, s_table);
+    r.q = VfStats{1.0, 0.0, 0};
+    if (stands) {
+      if (with_q) r.q = row_stats(q_part + (size_t)i * a.chunks, a.chunks, warm, c, lane, s_table);
+      stands = real && r.p.Z > 0.0 && r.q.Z > 0.0;
+      if (stands && warm) {
+        const double q = with_q ? probability(lq, r.q, c, s_table) : 1.0;
+        stands = number_of(u) * q < probability(lx, r.p, c, s_table);
+        if (writes && a.logp && lane == 0) a.logp[first + i] = log_probability(lx, r.p, c);   // (of those that stand)
+      } else if (stands) {
+        stands = x == r.p.first;
+        if (writes && a.logp && lane == 0) a.logp[first + i] = 0.0f;
       }
     }
+    if (!stands) {
+      fell = i;
+      break;
+    }
+  }
+  if (lane == 0) {
+    r.row = fell;
+    s_choice[wave] = r;
   }
   __syncthreads();
+  int who = 0;
+#pragma unroll
+  for (int w = 1; w < kVdWaves; ++w)
+    if (s_choice[w].row < s_choice[who].row) who = w;
+  r = s_choice[who];
+  const int m = r.row;   // drafts that stand
+  r.row += first;
+  r.rest = warm && m < n - 1 && r.q.Z > 0.0;
   if (writes) {
-    for (int i = tid; i < n; i += kVfThreads) {
+    if (tid == 0) {
+      a.choice[b] = r;
+      a.n_tokens[b] = m + 1;
+    }
+    for (int i = tid; i < n; i += kVdThreads) {
       if (i < m) a.tokens[first + i] = a.ids[first + i + 1];
       else if (i > m) {
         a.tokens[first + i] = -1;
@@ -473,95 +763,102 @@ k_vd_decide(const VfArgs a) {
       }
     }
   }
-  const VfChoice r = s_choice;
-  if (!r.rest || !a.draft || !(r.p.Z > 0.0)) return;
-  const VfWeights<F32> weights(a.logits + (size_t)r.row * a.stride, r.p, a.draft + (size_t)r.row * a.draft_stride, r.q, c, -1);
-  for (int ch = blockIdx.x * kVfWaves + wave; ch < a.chunks; ch += gridDim.x * kVfWaves) {
-    const double s = weights.sum_of_chunk(a.V, ch, lane, s_table);
-    if (lane == 0) a.rest[(size_t)b * a.chunks + ch] = s;
+  if (!a.draft) {
+    draw_next<F32>(a, b, r, warm, c, s_table, &s_draw);
+  } else if (a.together && r.rest && r.p.Z > 0.0) {
+    const VfWeights<F32> weights(a.logits + (size_t)r.row * a.stride, r.p, a.draft + (size_t)r.row * a.draft_stride, r.q, c, -1);
+    const int pieces = a.chunks * kVdPieces;
+    rest_sums(weights, a.V, blockIdx.x * kVdWaves + wave, pieces, gridDim.x * kVdWaves, a.rest + (size_t)b * pieces, s_table, lane);
   }
 }
 
-// The token after the drafts that stand: a wave a request.
+// The same sums apart, where there are many requests: those that a draft fell of,
+// in equal shares whatever their number.
 template <bool F32>
-__global__ void __launch_bounds__(kVfSteps)
-k_vd_draw(const VfArgs a) {
+__global__ void __launch_bounds__(kVfThreads)
+k_vd_rest(const VfArgs a) {
   __shared__ double s_table[kVfSteps];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const auto has_rest = [&](int b) {
+    const VfChoice& r = a.choice[b];
+    return r.row >= 0 && r.rest && r.p.Z > 0.0;
+  };
   fill_table(s_table);
   __syncthreads();
-  if (threadIdx.x >= kWave) return;
-  const int b = blockIdx.x, lane = threadIdx.x;
+  // (every wave by itself: a lane counts neighbouring requests)
+  const int per = (a.B + kWave - 1) / kWave, b0 = min(lane * per, a.B), b1 = min(b0 + per, a.B);
+  int mine = 0;
+  for (int b = b0; b < b1; ++b) mine += has_rest(b);
+  int incl = mine;
+#pragma unroll
+  for (int x = 1; x < kWave; x <<= 1) {
+    const int y = __shfl_up(incl, x);
+    if (lane >= x) incl += y;
+  }
+  const int requests = __builtin_amdgcn_readlane(incl, kWave - 1), pieces = a.chunks * kVdPieces;
+  const long long units = (long long)requests * pieces;
+  const long long u_begin = units * blockIdx.x / gridDim.x, u_end = units * (blockIdx.x + 1) / gridDim.x;
+  for (long long u = u_begin; u < u_end;) {
+    const int k = (int)(u / pieces);            // the k-th of them
+    const int L = __ffsll((unsigned long long)__ballot(incl > k)) - 1;
+    int b = L * per, left = k - __builtin_amdgcn_readlane(incl - mine, L);
+    while (!has_rest(b) || left-- > 0) ++b;
+    const long long upto = min(u_end, (long long)(k + 1) * pieces);
+    const VfChoice r = a.choice[b];
+    double c = 0.0;
+    scale_for(a, b, &c);
+    const VfWeights<F32> weights(a.logits + (size_t)r.row * a.stride, r.p, a.draft + (size_t)r.row * a.draft_stride, r.q, c, -1);
+    const int from = (int)(u - (long long)k * pieces), to = (int)(upto - (long long)k * pieces);
+    rest_sums(weights, a.V, from + wave, to, kVfWaves, a.rest + (size_t)b * pieces, s_table, lane);
+    u = upto;
+  }
+}
+
+// The draw apart, where there are a drafter's logits: a workgroup a request.
+template <bool F32>
+__global__ void __launch_bounds__(kVfThreads)
+k_vd_draw(const VfArgs a) {
+  __shared__ double s_table[kVfSteps];
+  __shared__ VfDrawScratch<kVfWaves> s_draw;
+  const int b = blockIdx.x;
   const VfChoice r = a.choice[b];
-  if (r.row < 0) return;
   double c = 0.0;
   const bool warm = scale_for(a, b, &c);
-  const char* row = a.logits + (size_t)r.row * a.stride;
-  const VfPart* part = a.part + (size_t)r.row * a.chunks;
-  int y = -1;
-  if (!(r.p.Z > 0.0)) {
-    // no token can be
-  } else if (!warm) {
-    y = r.p.first;
-  } else {
-    const double u = number_of(a.u_draw[b]);
-    if (r.rest && a.draft) {
-      const VfWeights<F32> w(row, r.p, a.draft + (size_t)r.row * a.draft_stride, r.q, c, -1);
-      const double* rest = a.rest + (size_t)b * a.chunks;
-      y = draw_token(w, a.V, a.chunks, s_table, u, lane, [&](int ch) { return rest[ch]; });
-    } else if (r.rest) {
-      // all but the draft: its chunk's sum without it
-      const int x = a.ids[r.row + 1];
-      const VfWeights<F32> w(row, r.p, nullptr, r.q, c, x >= 0 && x < a.V ? x : -1);
-      const int its = w.without >= 0 ? x / kVfChunk : -1;
-      const double other = its >= 0 ? w.sum_of_chunk(a.V, its, lane, s_table) : 0.0;
-      y = draw_token(w, a.V, a.chunks, s_table, u, lane,
-                     [&](int ch) { return ch == its ? other : part_weight(part[ch], r.p.M, c); });
-    }
-    if (y < 0) {
-      const VfWeights<F32> w(row, r.p, nullptr, r.q, c, -1);
-      y = draw_token(w, a.V, a.chunks, s_table, u, lane, [&](int ch) { return part_weight(part[ch], r.p.M, c); });
-    }
-  }
-  if (lane == 0) {
-    a.tokens[r.row] = y;
-    if (a.logp) a.logp[r.row] = warm && y >= 0 ? log_probability<F32>(row, y, r.p, c) : 0.0f;
-  }
+  fill_table(s_table);
+  if (r.row < 0) return;
+  __syncthreads();
+  draw_next<F32>(a, b, r, warm, c, s_table, &s_draw);
 }
 
 // ---------------------------------------------------------------------------
-// a tree: a draw at every node, a wave each; then the walk, a workgroup a request
+// a tree: a draw at every node, a workgroup each; then the walk, a workgroup a
+// request
 // ---------------------------------------------------------------------------
 template <bool F32>
 __global__ void __launch_bounds__(kVfThreads)
 k_vt_draw(const VfArgs a) {
   __shared__ double s_table[kVfSteps];
-  const int b = blockIdx.y, lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  int first;
-  const int n = packed_rows(a.cu_q, b, a.T, a.max_q, &first);
-  if ((int)blockIdx.x * kVfWaves >= n) return;
+  __shared__ VfDrawScratch<kVfWaves> s_draw;
+  const int b = blockIdx.y, i = blockIdx.x, tid = threadIdx.x, lane = tid % kWave;
+  const VfRequest rq = request_of(a, b);
+  const int n = rq.n, first = rq.first;
+  if (i >= n) return;
   fill_table(s_table);
   __syncthreads();
-  const int i = blockIdx.x * kVfWaves + wave;
-  if (i >= n) return;
-  double c = 0.0;
-  const bool warm = scale_for(a, b, &c);
   const int r = first + i;
-  const char* row = a.logits + (size_t)r * a.stride;
   const VfPart* part = a.part + (size_t)r * a.chunks;
-  const VfStats sp = row_stats(part, a.chunks, warm, c, lane);
-  int y = -1;
-  float lp = 0.0f;
-  if (sp.Z > 0.0 && warm) {
-    const VfWeights<F32> w(row, sp, nullptr, sp, c, -1);
-    y = draw_token(w, a.V, a.chunks, s_table, number_of(a.u[r]), lane,
-                   [&](int ch) { return part_weight(part[ch], sp.M, c); });
-    if (y >= 0) lp = log_probability<F32>(row, y, sp, c);
+  const VfStats sp = row_stats(part, a.chunks, rq.warm, rq.c, lane, s_table);
+  VfDrawn y{-1, 0.0f};
+  if (sp.Z > 0.0 && rq.warm) {
+    const VfWeights<F32> w(a.logits + (size_t)r * a.stride, sp, nullptr, sp, rq.c, -1);
+    y = draw_token(w, a.V, a.chunks, kVfChunk, s_table, number_of(a.u[r]), &s_draw,
+                   [&](int ch) { return part_weight(part[ch], sp.M, rq.c, s_table); });
   } else if (sp.Z > 0.0) {
-    y = sp.first;
+    y.token = sp.first;
   }
-  if (lane == 0) {
-    a.drawn[r] = y;
-    a.drawn_lp[r] = lp;
+  if (tid == 0) {
+    a.drawn[r] = y.token;
+    a.drawn_lp[r] = rq.warm && y.token >= 0 ? log_probability(y.x, sp, rq.c) : 0.0f;
   }
 }
 
@@ -575,29 +872,29 @@ k_vt_walk(const VfArgs a) {
     if (tid == 0) a.n_tokens[b] = 0;
     return;
   }
-  for (int i = tid; i < n; i += kVfThreads) {
-    s_y[i] = a.drawn[first + i];
-    s_child[i] = INT32_MAX;
+  for (int k = tid; k < n; k += kVfThreads) {
+    s_y[k] = a.drawn[first + k];
+    s_child[k] = INT32_MAX;
   }
   __syncthreads();
-  for (int i = tid; i < n; i += kVfThreads) {
-    const int p = a.parents[first + i];
-    if (p >= 0 && p < i && s_y[p] >= 0 && a.ids[first + i] == s_y[p]) atomicMin(&s_child[p], i);   // the lowest, in any order
+  for (int k = tid; k < n; k += kVfThreads) {
+    const int p = a.parents[first + k];
+    if (p >= 0 && p < k && s_y[p] >= 0 && a.ids[first + k] == s_y[p]) atomicMin(&s_child[p], k);   // the lowest, in any order
   }
   __syncthreads();
   if (tid == 0) {
     int len = 0;
-    for (int i = 0; i < n; i = s_child[i]) s_path[len++] = i;   // children come after their parents
+    for (int k = 0; k < n; k = s_child[k]) s_path[len++] = k;   // children come after their parents
     s_len = len;
     a.n_tokens[b] = len;
   }
   __syncthreads();
   const int len = s_len;
-  for (int i = tid; i < n; i += kVfThreads) {
-    const int node = i < len ? s_path[i] : -1;
-    a.path[first + i] = node;
-    a.tokens[first + i] = node >= 0 ? s_y[node] : -1;
-    if (a.logp) a.logp[first + i] = node >= 0 ? a.drawn_lp[first + node] : 0.0f;
+  for (int k = tid; k < n; k += kVfThreads) {
+    const int node = k < len ? s_path[k] : -1;
+    a.path[first + k] = node;
+    a.tokens[first + k] = node >= 0 ? s_y[node] : -1;
+    if (a.logp) a.logp[first + k] = node >= 0 ? a.drawn_lp[first + node] : 0.0f;
   }
 }
 
@@ -609,7 +906,10 @@ struct VfPlan {
   size_t at_rest, at_choice, at_drawn, at_lp, bytes;
 };
 
-static bool vf_sizes_ok(int T, int B, int V) { return V >= 1 && V <= (1 << 30) && B <= 65535; }
+static bool vf_sizes_ok(int T, int B, int V) {
+  if (V < 1 || V > (1 << 30) || B > 65535) return false;
+  return 2.0 * T * ((V + kVfChunk - 1) / kVfChunk) < 2.0e9;   // chunks are counted in 32 bits
+}
 
 static VfPlan vf_plan(int T, int B, int V, bool tree, bool marginals) {
   VfPlan p{};
@@ -625,23 +925,29 @@ static VfPlan vf_plan(int T, int B, int V, bool tree, bool marginals) {
     p.at_lp = take((size_t)T * 4);
   } else {
     p.at_choice = take((size_t)B * sizeof(VfChoice));
-    if (marginals) p.at_rest = take((size_t)B * p.chunks * sizeof(double));
+    if (marginals) p.at_rest = take((size_t)B * p.chunks * kVdPieces * sizeof(double));
   }
   p.bytes = at;
   return p;
 }
 
-// Workgroups a row: eight a CU in all, no more than a wave a chunk.
-static int vf_parts(long long rows, int chunks) {
-  const long long want = (256 * 8 + rows - 1) / (rows < 1 ? 1 : rows), most = (chunks + kVfWaves - 1) / kVfWaves;
-  return (int)(want < 1 ? 1 : want < most ? want : most);
-}
+// Workgroups of the pass that the chip holds at a time.
+constexpr int kVfFill = 256 * 4, kVtFill = 256 * 2;
+// Chunks a wave from which the table pays (100 rows of 126464, 1.5 a wave: 21.8 us
+// without and 20.9 with; 400 rows 43 and 33, 800 rows 75 and 52).
+constexpr int kVtChunks = 1;
+// Requests up to which the decision forms the sums of max(p - q, 0): a workgroup a
+// CU in all, and a request that needs none leaves its CUs idle (8 drafts of
+// 126464: 16 requests 35.4 us together and 39.8 apart, 32 47.4 and 49.2; six, 64
+// 64.1 and 62.5; four, 96 72.9 and 61.6).
+constexpr int kVdTogether = 32, kVdFill = 256, kVdRestFill = 256 * 4;
 
 static fdllm_status vf_check(const void* logits, int64_t stride, fdllm_dtype dtype, int T, int V, const int32_t* cu_q, int B,
                              int max_q, const int32_t* n_tokens) {
   if (T < 0 || B < 0 || max_q < 0) return FDLLM_ERR_INVALID_ARG;
   if (dtype != FDLLM_BF16 && dtype != FDLLM_F32) return FDLLM_ERR_UNSUPPORTED_DTYPE;
   if (!vf_sizes_ok(T, B, V) || max_q > FDLLM_MAX_TREE) return FDLLM_ERR_SIZE;
+  if (2.0 * B * (max_q < T ? max_q : T) * ((V + kVfChunk - 1) / kVfChunk) >= 2.0e9) return FDLLM_ERR_SIZE;
   if (stride < V) return FDLLM_ERR_INVALID_ARG;
   if ((double)stride * T > 1.0e18) return FDLLM_ERR_SIZE;   // offsets fit 64 bits
   if (B > 0 && (!cu_q || !n_tokens)) return FDLLM_ERR_INVALID_ARG;
@@ -651,28 +957,38 @@ static fdllm_status vf_check(const void* logits, int64_t stride, fdllm_dtype dty
 }
 
 template <bool F32>
-static void vf_sums(const VfArgs& a, int sides, hipStream_t st) {
+static void vf_sums(const VfArgs& a, hipStream_t st) {
   if (a.T == 0 || a.max_q == 0) return;
-  const int rows = a.max_q < a.T ? a.max_q : a.T;   // of a request
-  hipLaunchKernelGGL((k_vf_sums<F32>), dim3((unsigned)vf_parts((long long)a.T * sides, a.chunks), (unsigned)(rows * sides), (unsigned)a.B),
-                     dim3(kVfThreads), 0, st, a, sides);
+  const long long chunks = (long long)a.T * (a.draft ? 2 : 1) * a.chunks;
+  if constexpr (!F32) {
+    if (chunks >= (long long)kVtFill * (kVtThreads / kWave) * kVtChunks) {
+      hipLaunchKernelGGL((k_vf_sums<false, true>), dim3(kVtFill), dim3(kVtThreads), 0, st, a);
+      return;
+    }
+  }
+  const long long most = (chunks + kVfWaves - 1) / kVfWaves;
+  hipLaunchKernelGGL((k_vf_sums<F32, false>), dim3((unsigned)(most < kVfFill ? most : kVfFill)), dim3(kVfThreads), 0, st, a);
 }
 
 template <bool F32>
 static hipError_t vd_launch(const VfArgs& a, hipStream_t st) {
-  vf_sums<F32>(a, a.draft ? 2 : 1, st);
-  const int parts = a.draft ? vf_parts(a.B, a.chunks) : 1;
-  hipLaunchKernelGGL((k_vd_decide<F32>), dim3((unsigned)parts, (unsigned)a.B), dim3(kVfThreads), 0, st, a);
-  hipLaunchKernelGGL((k_vd_draw<F32>), dim3((unsigned)a.B), dim3(kVfSteps), 0, st, a);
+  vf_sums<F32>(a, st);
+  // with a drafter's logits workgroups for all CUs, a wave a piece at most
+  const int most = (a.chunks * kVdPieces + kVdWaves - 1) / kVdWaves, fill = kVdFill / a.B;
+  VfArgs d = a;
+  d.together = a.draft && a.B <= kVdTogether;
+  const int parts = !d.together ? 1 : fill < most ? fill : most;
+  hipLaunchKernelGGL((k_vd_decide<F32>), dim3((unsigned)parts, (unsigned)a.B), dim3(kVdThreads), 0, st, d);
+  if (a.draft && !d.together) hipLaunchKernelGGL((k_vd_rest<F32>), dim3(kVdRestFill), dim3(kVfThreads), 0, st, a);
+  if (a.draft) hipLaunchKernelGGL((k_vd_draw<F32>), dim3((unsigned)a.B), dim3(kVfThreads), 0, st, a);
   return hipGetLastError();
 }
 
 template <bool F32>
 static hipError_t vt_launch(const VfArgs& a, hipStream_t st) {
-  vf_sums<F32>(a, 1, st);
+  vf_sums<F32>(a, st);
   const int rows = a.max_q < a.T ? a.max_q : a.T;
-  if (rows > 0)
-    hipLaunchKernelGGL((k_vt_draw<F32>), dim3((unsigned)((rows + kVfWaves - 1) / kVfWaves), (unsigned)a.B), dim3(kVfThreads), 0, st, a);
+  if (rows > 0) hipLaunchKernelGGL((k_vt_draw<F32>), dim3((unsigned)rows, (unsigned)a.B), dim3(kVfThreads), 0, st, a);
   hipLaunchKernelGGL(k_vt_walk, dim3((unsigned)a.B), dim3(kVfThreads), 0, st, a);
   return hipGetLastError();
 }

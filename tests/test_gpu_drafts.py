@@ -459,6 +459,48 @@ def test_verify_tree_walks_to_the_end(gpu):
         assert got[2][0] == 1 and got[1][0] == -1 and got[3][0] == 0
 
 
+def _mixed_rows(T, V, seed, dtype=torch.bfloat16):
+    """Rows of many kinds: far from 0, zeros, nothing near 0, -inf in between and at the end."""
+    x = _logits(T, V, seed, torch.float32)
+    x[1::8] += 200.0
+    x[2::8] *= 30.0
+    x[3::8, ::7] = 0.0
+    x[4::8] *= 1e-6
+    x[5::8, V // 2:] = -float("inf")
+    x[6::8, 1000:] = -float("inf")
+    return x.to(dtype)
+
+
+def test_many_rows_of_bfloat16(gpu):
+    # rows enough for the terms to be looked up in a table; temperatures that allow it and not
+    V, n, B = 126464, 10, 9
+    T, cu, parents = n * B, _cu([n] * B), np.tile(_tree(n, 5), B)
+    x = _mixed_rows(T, V, 3)
+    temperature = [1.0, 0.2, 0.19, 0.0, 3.0, 1e-3, 1.0, 1.0, 50.0]
+    likely = x.float().topk(2, dim=1).indices.numpy()
+    ids = np.zeros(T, dtype=np.int64)
+    for b in range(B):
+        for i in range(1, n):
+            ids[cu[b] + i] = likely[cu[b] + parents[cu[b] + i], i % 2]
+    u, logits = _numbers(T, 8), _strided(x, 1)
+    _check_tree(cu, logits, ids, parents, temperature, u, _verify_tree(gpu, cu, n, logits, ids, parents, temperature, u)[:4])
+
+
+def test_many_requests_with_a_drafter(gpu):
+    # requests and rows enough for every variant: the table, the sums of p - q apart
+    V, counts = 126464, [2 + b % 3 for b in range(44)]
+    T = sum(counts)
+    x = _mixed_rows(T, V, 4)
+    g = torch.Generator().manual_seed(6)
+    d = (x.float() + 0.5 * torch.randn((T, V), generator=g)).to(torch.bfloat16)
+    ids = np.concatenate([[0], d.float().topk(2, dim=1).indices[:, 1].numpy()[:-1]])
+    temperature = [(1.0, 0.0, 0.5, 2.0, 0.1)[b % 5] for b in range(44)]
+    u, u_draw = _numbers(T, 1), _numbers(44, 2)
+    logits, draft = x.to(DEV), _strided(d, 3)
+    got = _verify_draft(gpu, counts, V, logits, draft, ids, temperature, u, u_draw)
+    _check_draft(counts, logits, draft, ids, temperature, u, u_draw, got[:3])
+
+
 def test_equal_logits_take_the_lowest(gpu):
     V = 5000
     x = torch.zeros((2, V), dtype=torch.bfloat16, device=DEV)
