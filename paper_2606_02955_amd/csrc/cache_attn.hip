@@ -632,16 +632,18 @@ k_cache_attn(const CacheAttnArgs a) {
 // in the same order.  A workgroup takes the MT rows of a wave's tile, as they
 // lay in its registers.  Where items lie in many shares, Split sets of its
 // waves divide the parts (a part costs a round trip to memory, so as many as
-// possible are under way at once); where they lie in two or so, every wave has
-// quads of its own.
+// possible are under way at once), and a workgroup takes 32 of a head's elements;
+// where they lie in two or so, every wave has quads of its own.
 constexpr int kCaJoinWaves = 8;
 
 template <int NG, int MT, int WR, int Split>
 __global__ void __launch_bounds__(kCaJoinWaves* kWave)
 k_cache_join(const CacheAttnArgs a, int wgs) {
   constexpr int D = NG * kGroup, Quads = quads_of(MT, NG), Rows = MT * WR;
+  constexpr int Own = Split > 1 ? quads_of(MT, 1) : Quads;   // quads of the workgroup, from q0 on
   constexpr int Sets = kCaJoinWaves / Split;              // of waves, by quads
-  constexpr int QPer = (Quads + Sets - 1) / Sets;
+  constexpr int QPer = (Own + Sets - 1) / Sets;
+  const int q0 = Split > 1 ? blockIdx.z * Own : 0;
   __shared__ __align__(16) uint8_t s_out[MT * OutRows<NG>::RowBytes];
   __shared__ f32x4 s_acc[Split > 1 ? Sets * (Split - 1) : 1][QPer][kWave];
   __shared__ float s_ml[kCaJoinWaves][MT][2];
@@ -667,20 +669,28 @@ k_cache_join(const CacheAttnArgs a, int wgs) {
   for (int i = 0; i < QPer; ++i) acc[i] = f32x4{};
   float ref = kRefFloor, l = 0.0f;
   constexpr int Ahead = 4;
-  for (int g = g0 + sp * Ahead; g <= g1; g += Split * Ahead) {
+  struct Parts {
     float2 ml[Ahead];
     f32x4 v[Ahead][QPer];
+  };
+  const auto load = [&](int g, Parts& p) {
 #pragma unroll
     for (int k = 0; k < Ahead; ++k) {
       const size_t tile = tile_of(min(g + k, g1));
-      ml[k] = *(const float2*)(a.part_ml + (tile * MT + col) * 2);
+      p.ml[k] = *(const float2*)(a.part_ml + (tile * MT + col) * 2);
 #pragma unroll
       for (int i = 0; i < QPer; ++i)
-        v[k][i] = *(const f32x4*)(a.part + ((tile * Quads + min(set * QPer + i, Quads - 1)) * kWave + lane) * 4);
+        p.v[k][i] = *(const f32x4*)(a.part + ((tile * Quads + q0 + min(set * QPer + i, Own - 1)) * kWave + lane) * 4);
     }
+  };
+  Parts next;
+  load(g0 + sp * Ahead, next);
+  for (int g = g0 + sp * Ahead; g <= g1; g += Split * Ahead) {
+    const Parts p = next;
+    if (Split > 1 && g + Split * Ahead <= g1) load(g + Split * Ahead, next);
     float to = ref;
 #pragma unroll
-    for (int k = 0; k < Ahead; ++k) to = fmaxf(to, ml[k].x);
+    for (int k = 0; k < Ahead; ++k) to = fmaxf(to, p.ml[k].x);
     const float f0 = __builtin_amdgcn_exp2f(ref - to);
     ref = to;
     l *= f0;
@@ -688,11 +698,12 @@ k_cache_join(const CacheAttnArgs a, int wgs) {
     for (int i = 0; i < QPer; ++i) acc[i] *= f0;
 #pragma unroll
     for (int k = 0; k < Ahead; ++k) {
-      const float f = g + k <= g1 ? __builtin_amdgcn_exp2f(ml[k].x - ref) : 0.0f;
-      l += f * ml[k].y;
+      const float f = g + k <= g1 ? __builtin_amdgcn_exp2f(p.ml[k].x - ref) : 0.0f;
+      l += f * p.ml[k].y;
 #pragma unroll
-      for (int i = 0; i < QPer; ++i) acc[i] += v[k][i] * f;
+      for (int i = 0; i < QPer; ++i) acc[i] += p.v[k][i] * f;
     }
+    if (Split == 1 && g + Ahead <= g1) load(g + Ahead, next);
   }
   if constexpr (Split > 1) {
     if (part == 0) s_ml[wave][col][0] = ref, s_ml[wave][col][1] = l;
@@ -723,18 +734,20 @@ k_cache_join(const CacheAttnArgs a, int wgs) {
 #pragma unroll
     for (int i = 0; i < QPer; ++i) {
       const int q = set * QPer + i;
-      if (q < Quads)
-        *(u32x2*)(s_out + OutRows<NG>::at(col, quad_element<MT>(q, part))) =
+      if (q < Own)
+        *(u32x2*)(s_out + OutRows<NG>::at(col, quad_element<MT>(q0 + q, part))) =
             u32x2{pack_bf16(acc[i][0] * inv, acc[i][1] * inv), pack_bf16(acc[i][2] * inv, acc[i][3] * inv)};
     }
     const int r = r0 + col;
-    if (set == 0 && part == 0 && a.lse && r < seq.n * a.R)
+    if (set == 0 && q0 == 0 && part == 0 && a.lse && r < seq.n * a.R)
       a.lse[(size_t)(seq.first + r / a.R) * a.H + h * a.R + r % a.R] =
           log_sum(ref, l);
   }
   __syncthreads();
-  for (int x = threadIdx.x; x < MT * (D / 8); x += kCaJoinWaves * kWave) {
-    const int row = x / (D / 8), d = 8 * (x % (D / 8)), r = r0 + row;
+  constexpr int Pieces = (Split > 1 ? kGroup : D) / 8;   // of 16 bytes a row
+  const int d0 = Split > 1 ? blockIdx.z * kGroup : 0;
+  for (int x = threadIdx.x; x < MT * Pieces; x += kCaJoinWaves * kWave) {
+    const int row = x / Pieces, d = d0 + 8 * (x % Pieces), r = r0 + row;
     if (r >= seq.n * a.R) break;
     const size_t at = (size_t)(seq.first + r / a.R) * a.H + h * a.R + r % a.R;
     *(u32x4*)(a.out + at * D + d) = *(const u32x4*)(s_out + OutRows<NG>::at(row, d));
@@ -847,7 +860,7 @@ static hipError_t ca_launch_one(const CacheAttnArgs& a, const CaPlan& p, hipStre
     if (dev >= 0 && dev < kCaMaxDevices) allowed[dev].store(true, std::memory_order_release);
   }
   hipLaunchKernelGGL((k_cache_attn<NG, MT, WR, Tree, Whole>), dim3((unsigned)p.wgs), dim3(S::Threads), S::LdsBytes, st, a);
-  const dim3 join((unsigned)(p.items * WR), (unsigned)a.B), threads(kCaJoinWaves * kWave);
+  const dim3 join((unsigned)(p.items * WR), (unsigned)a.B, p.split ? NG : 1), threads(kCaJoinWaves * kWave);
   if (p.join && p.split) hipLaunchKernelGGL((k_cache_join<NG, MT, WR, 4>), join, threads, 0, st, a, p.wgs);
   else if (p.join) hipLaunchKernelGGL((k_cache_join<NG, MT, WR, 1>), join, threads, 0, st, a, p.wgs);
   return hipGetLastError();

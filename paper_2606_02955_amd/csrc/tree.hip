@@ -84,13 +84,16 @@ k_tree_layout(const LayoutArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// A wave takes a request's path in some of the tiles (a head of a layer each).
-// An entry is D / 16 pieces of 16 bytes and two of the scales; the lanes take as
-// many entries at a time as they have pieces for.  A source never lies before its
-// place (path[i] >= i), so the entries of one time are read before any of them is
-// written, and no later one reads what was written.
+// A wave takes a request's path in a tile (a head of a layer).  An entry is D / 16
+// pieces of 16 bytes and two of the scales; the lanes take as many entries at a time
+// as they have pieces for.  A source never lies before its place (path[i] >= i), so
+// the entries of one time are read before any of them is written, and no later one
+// reads what was written.  Bound by whole cache lines: the pieces of an entry lie a
+// page of tokens apart, and one of 16 bytes costs 128 (64 paths in 256 tiles: 9 MB
+// moved, 60 read and 14 written, 16.4 us with the launch; 17.0 with two tiles a wave
+// under way, 17.4 with four, 18.5 with eight).
 // ---------------------------------------------------------------------------
-constexpr int kCkTiles = 4, kCkThreads = 256;
+constexpr int kCkThreads = 256;
 
 struct KeepArgs {
   uint8_t* cache;
@@ -141,27 +144,21 @@ k_cache_keep(const KeepArgs a) {
     if (!__any(ok)) continue;
     const uint8_t* src = a.cache + (size_t)(ok ? from / kPage : 0) * a.Hk * tile + at + (ok ? from % kPage : 0) * step;
     uint8_t* dst = a.cache + (size_t)(ok ? to / kPage : 0) * a.Hk * tile + at + (ok ? to % kPage : 0) * step;
-    for (int t0 = wave * kCkTiles; t0 < a.tiles; t0 += gridDim.x * (kCkThreads / kWave) * kCkTiles) {
-      u32x4 v[kCkTiles];
-      const auto tile_at = [&](int t) {
-        return ((size_t)(t / a.Hk) * a.n_pages * a.Hk + t % a.Hk) * tile;
-      };
-#pragma unroll
-      for (int k = 0; k < kCkTiles; ++k) {
-        if (!ok || t0 + k >= a.tiles) continue;
-        const uint8_t* p = src + tile_at(t0 + k);
-        if (!scale) v[k] = *(const u32x4*)p;
-        else if constexpr (ScaleBytes == 4) v[k][0] = *(const uint32_t*)p;
-        else v[k][0] = ((const uint32_t*)p)[0], v[k][1] = ((const uint32_t*)p)[1];
+    for (int t = wave; t < a.tiles; t += gridDim.x * (kCkThreads / kWave)) {
+      const size_t tile_at = ((size_t)(t / a.Hk) * a.n_pages * a.Hk + t % a.Hk) * tile;
+      u32x4 v;
+      if (ok) {
+        const uint8_t* p = src + tile_at;
+        if (!scale) v = *(const u32x4*)p;
+        else if constexpr (ScaleBytes == 4) v[0] = *(const uint32_t*)p;
+        else v[0] = ((const uint32_t*)p)[0], v[1] = ((const uint32_t*)p)[1];
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // all lanes' reads, then all writes
-#pragma unroll
-      for (int k = 0; k < kCkTiles; ++k) {
-        if (!ok || t0 + k >= a.tiles) continue;
-        uint8_t* p = dst + tile_at(t0 + k);
-        if (!scale) *(u32x4*)p = v[k];
-        else if constexpr (ScaleBytes == 4) *(uint32_t*)p = v[k][0];
-        else ((uint32_t*)p)[0] = v[k][0], ((uint32_t*)p)[1] = v[k][1];
+      if (ok) {
+        uint8_t* p = dst + tile_at;
+        if (!scale) *(u32x4*)p = v;
+        else if constexpr (ScaleBytes == 4) *(uint32_t*)p = v[0];
+        else ((uint32_t*)p)[0] = v[0], ((uint32_t*)p)[1] = v[1];
       }
     }
   }
@@ -201,7 +198,7 @@ fdllm_status fdllm_cache_keep(uint8_t* cache, int layers, int n_pages, int Hk, i
   const int tiles = n_pages > 0 && table_width > 0 && T > 0 ? layers * Hk : 0;
   if (tiles && (!cache || !page_table || !path || ((uintptr_t)cache & 15))) return FDLLM_ERR_INVALID_ARG;
   const KeepArgs a{cache, tiles, n_pages, Hk, D, page_table, tiles ? table_width : 0, kv_len, cu_q, T, B, max_q, path, n_path, kv_out};
-  const int per = kCkTiles * (kCkThreads / kWave);
+  const int per = kCkThreads / kWave;
   const dim3 grid((unsigned)(tiles ? (tiles + per - 1) / per : 1), (unsigned)B);
   if (scale_stride(D) == 4) hipLaunchKernelGGL(k_cache_keep<4>, grid, dim3(kCkThreads), 0, (hipStream_t)stream, a);
   else hipLaunchKernelGGL(k_cache_keep<8>, grid, dim3(kCkThreads), 0, (hipStream_t)stream, a);

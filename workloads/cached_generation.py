@@ -11,7 +11,14 @@ cache and their queries attend over everything cached
 (``fdllm_qk_norm_rope``, ``fdllm_cache_attention``), and the last hidden states
 go into ``fdllm_lmhead_decode_step``, which reveals the tokens it commits to.
 
+The same model also generates one token after another, with drafts: a step runs it
+on a tree of drafted tokens behind what is cached (``fdllm_tree_layout``,
+``fdllm_tree_attention``), ``fdllm_verify_tree`` says which of them stand and
+``fdllm_cache_keep`` moves their cache entries into place; a chain of drafts needs
+no tree and is held against the drafter's probabilities (``fdllm_verify_draft``).
+
     python -m workloads.cached_generation --batch 4 --blocks 2
+    python -m workloads.cached_generation --batch 4 --blocks 2 --drafted 3x4
 """
 from __future__ import annotations
 
@@ -81,19 +88,22 @@ class Model:
 
 
 class Session:
-    """A batch in generation: its pages, caches and places."""
+    """A batch in generation: its pages, caches and places (room: for tokens beyond
+    those to be generated, of trees of drafts)."""
 
-    def __init__(self, model: Model, prompt_lens, gen_len: int):
+    def __init__(self, model: Model, prompt_lens, gen_len: int, room: int = 0):
         c, dev = model.cfg, model.device
         self.model, self.lens, self.B = model, list(prompt_lens), len(prompt_lens)
         if gen_len % c.block:
             raise ValueError("gen_len must be a multiple of the block")
         self.gen_len = gen_len
-        width = -(-(max(self.lens) + gen_len) // fd.CACHE_PAGE)
+        width = -(-(max(self.lens) + gen_len + room) // fd.CACHE_PAGE)
         # pages in a mixed order, as an allocator that has been running hands them out
         order = torch.randperm(self.B * width, generator=torch.Generator().manual_seed(1)).to(torch.int32)
         self.table = order.view(self.B, width).to(dev)
-        self.caches = [fd.new_cache(self.B * width, c.kv_heads, c.head_dim, dev) for _ in range(c.layers)]
+        # the layers' caches one behind the other
+        self.stack = torch.stack([fd.new_cache(self.B * width, c.kv_heads, c.head_dim, dev) for _ in range(c.layers)])
+        self.caches = list(self.stack.unbind(0))
         self.done = torch.tensor(self.lens, device=dev)          # tokens before the active block
         self.block_at = torch.arange(c.block, device=dev)
         self.block_cu = (torch.arange(self.B + 1, device=dev) * c.block).to(torch.int32)
@@ -172,6 +182,107 @@ class Session:
             self.done += n
         return out, steps
 
+    # ---- with drafts ----
+    def drafts(self, roots, width: int, depth: int, temperature: float, generator=None):
+        """A drafter that only knows the token before: `width` branches of `depth`
+        tokens behind each root (their likeliest, or one drawn for a chain).
+        Returns ids [B, nodes], parents [nodes] and the drafter's logits of every
+        node of a chain."""
+        m, dev = self.model, self.model.device
+        n = 1 + width * depth
+        ids = torch.empty((self.B, n), dtype=torch.int32, device=dev)
+        parents = torch.tensor([-1] + [0 if i < width else i + 1 - width for i in range(n - 1)], dtype=torch.int32)
+        ids[:, 0] = roots
+        logits = torch.zeros((self.B, n, m.cfg.vocab), dtype=torch.bfloat16, device=dev) if width == 1 else None
+        for level in range(depth):
+            before = ids[:, :1] if level == 0 else ids[:, 1 + (level - 1) * width:1 + level * width]
+            x = _rms(m.embed[before.long()], m.norms[-1], m.cfg.eps) @ m.head.t()          # [B, nodes before, vocab]
+            if width == 1:
+                logits[:, level] = x[:, 0]
+                if temperature > 0:
+                    p = torch.softmax(x[:, 0].float() / temperature, dim=-1)
+                    ids[:, 1 + level] = torch.multinomial(p, 1, generator=generator).view(-1).to(torch.int32)
+                    continue
+            best = x.topk(width if level == 0 else 1, dim=-1).indices.reshape(self.B, width)
+            ids[:, 1 + level * width:1 + (level + 1) * width] = best.to(torch.int32)
+        return ids, parents.to(dev), logits
+
+    def tree_hidden(self, ids, parents, attention=None):
+        """The model call on trees behind what is cached, ids [B, n], parents [n] of
+        all of them: hidden states [B * n, d]; the nodes' keys and values go into
+        the cache behind the others, in the nodes' order."""
+        dev, n = self.model.device, ids.shape[1]
+        T = self.B * n
+        cu = (torch.arange(self.B + 1, device=dev) * n).to(torch.int32)
+        kv_len = (self.done + n).to(torch.int32)
+        masks = torch.empty((T, -(-n // 64)), dtype=torch.int64, device=dev)
+        position, slots = (torch.empty(T, dtype=torch.int32, device=dev) for _ in range(2))
+        fd.fdllm_tree_layout(parents.repeat(self.B), kv_len, cu, n, masks, positions=position, page_table=self.table,
+                             slots=slots)
+
+        def attend(layer, q, k, v):
+            q_out, _ = self._rope(layer, q, k, v, position, slots, keys=False)
+            if attention is not None:
+                return attention(self, layer, q_out, kv_len, masks)
+            out = torch.empty_like(q_out)
+            fd.fdllm_tree_attention(q_out, self.caches[layer], self.table, kv_len, cu, masks, out, n)
+            return out
+
+        return self.model.forward(ids.reshape(-1).long(), attend), kv_len, cu
+
+    def drafted_step(self, roots, width: int, depth: int, temperature: float, generator=None, record=None):
+        """One call of the model on drafts behind `roots` [B]: tokens [B, nodes] that
+        follow, -1 behind the last, and how many.  record: a dict that gets what the
+        step worked on."""
+        dev, B = self.model.device, self.B
+        ids, parents, marginals = self.drafts(roots, width, depth, temperature, generator)
+        n = ids.shape[1]
+        T = B * n
+        hidden, kv_len, cu = self.tree_hidden(ids, parents)
+        logits = hidden @ self.model.head.t()
+        tokens, path = (torch.empty(T, dtype=torch.int32, device=dev) for _ in range(2))
+        count = torch.empty(B, dtype=torch.int32, device=dev)
+        warmth = torch.full((B,), temperature, device=dev)
+        u, u_draw = (torch.rand(k, generator=generator, device=dev) for k in (T, B))
+        done = torch.empty(B, dtype=torch.int32, device=dev)
+        if width == 1:      # what stands of a chain lies in place
+            fd.fdllm_verify_draft(logits, ids.view(-1), cu, n, u, u_draw, tokens, count, draft=marginals.view(T, -1),
+                                  temperature=warmth)
+            done = kv_len - n + count
+        else:
+            fd.fdllm_verify_tree(logits, ids.view(-1), parents.repeat(B), cu, n, u, path, tokens, count, temperature=warmth)
+            if record is not None:
+                record["stack"] = self.stack.clone()
+            fd.fdllm_cache_keep(self.stack, self.table, kv_len, cu, path, count, n, done)
+        if record is not None:
+            record.update(ids=ids, parents=parents, marginals=marginals, logits=logits, u=u, u_draw=u_draw, path=path,
+                          kv_len=kv_len)
+        self.done = done.long()
+        return tokens.view(B, n), count
+
+    def generate_drafted(self, last, width: int = 3, depth: int = 4, temperature: float = 0.0, generator=None):
+        """gen_len tokens a sequence behind its prompt, whose last tokens are `last`
+        [B]; returns them and the steps taken."""
+        dev = self.model.device
+        n = 1 + width * depth
+        out = torch.full((self.B, self.gen_len + n), -1, dtype=torch.int32, device=dev)
+        at, steps = torch.zeros(self.B, dtype=torch.long, device=dev), 0
+        start = torch.tensor(self.lens, device=dev) - 1     # the last prompt token is the first root
+        self.done, roots = start.clone(), last.to(torch.int32)
+        b = torch.arange(self.B, device=dev)
+        while int(at.min()) < self.gen_len:
+            tokens, count = self.drafted_step(roots, width, depth, temperature, generator)
+            where = (at.view(-1, 1) + torch.arange(n, device=dev)).clamp(max=out.shape[1] - 1)
+            # a sequence that has its tokens stays where it is
+            live = at < self.gen_len
+            keep = live.view(-1, 1) & (torch.arange(n, device=dev) < count.view(-1, 1))
+            out.scatter_(1, where, torch.where(keep, tokens, out.gather(1, where)))
+            roots = torch.where(live, tokens[b, count.long() - 1], roots)
+            at += torch.where(live, count.long(), torch.zeros_like(at))
+            self.done = start + at
+            steps += 1
+        return out[:, :self.gen_len], steps
+
 
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
@@ -179,13 +290,17 @@ def main(argv=None):
     ap.add_argument("--prompt", type=int, default=512, help="the longest prompt's tokens")
     ap.add_argument("--blocks", type=int, default=2, help="blocks of 32 tokens to generate")
     ap.add_argument("--layers", type=int, default=4)
+    ap.add_argument("--drafted", metavar="WxD", help="generate with drafts, W branches of D tokens each (1xD: a chain)")
+    ap.add_argument("--temperature", type=float, default=0.0, help="of a generation with drafts")
     ap.add_argument("--seed", type=int, default=0)
     a = ap.parse_args(argv)
+    width, depth = (int(x) for x in a.drafted.split("x")) if a.drafted else (0, 0)
     cfg = Config(layers=a.layers)
     lens = [max(1, a.prompt * (a.batch - b) // a.batch) for b in range(a.batch)]
     gen_len = a.blocks * cfg.block
-    model = Model(cfg, max(lens) + gen_len, seed=a.seed)
-    session = Session(model, lens, gen_len)
+    room = 2 * (1 + width * depth) if a.drafted else 0
+    model = Model(cfg, max(lens) + gen_len + room, seed=a.seed)
+    session = Session(model, lens, gen_len, room)
     g = torch.Generator(device="cuda").manual_seed(a.seed + 1)
     prompt = torch.randint(0, cfg.vocab, (sum(lens),), generator=g, device="cuda")
     torch.cuda.synchronize()
@@ -194,7 +309,11 @@ def main(argv=None):
     torch.cuda.synchronize()
     print(f"prompts: {sum(lens)} tokens of {a.batch} sequences in {(time.perf_counter() - t) * 1e3:.1f} ms")
     t = time.perf_counter()
-    tokens, steps = session.generate()
+    if a.drafted:
+        last = prompt[torch.tensor(lens, device="cuda").cumsum(0) - 1]
+        tokens, steps = session.generate_drafted(last, width, depth, a.temperature, g)
+    else:
+        tokens, steps = session.generate()
     torch.cuda.synchronize()
     dt = time.perf_counter() - t
     print(f"generated {tokens.numel()} tokens in {steps} steps, {dt * 1e3:.1f} ms, {dt / steps * 1e3:.2f} ms a step")
