@@ -784,11 +784,11 @@ static bool ca_sizes_ok(int B, int H, int Hk, int D, int max_q, int table_w, int
   return units < 2.0e9;
 }
 
-static CaPlan ca_plan(int B, int H, int Hk, int D, int max_q, int table_w) {
+static CaPlan ca_plan(int B, int H, int Hk, int D, int max_q, int table_w, int most_wr = 4) {
   CaPlan p{};
   const long long rows = (long long)max_q * (H / Hk);
   p.mt = rows <= 16 ? 16 : 32;
-  p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+  p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : most_wr;
   const int per = p.mt * p.wr;
   const long long groups = (rows + per - 1) / per;
   p.items = (int)(groups * Hk);
@@ -821,6 +821,10 @@ static CaPlan ca_plan(int B, int H, int Hk, int D, int max_q, int table_w) {
 // and 39.3.  128: 4000 29.2 and 25.2, 6000 33.0 and 32.5.  256: 1000 24.8 and 12.9, 8000
 // 54.6 and 46.1.  512, twice what the chip holds: 500 27.5 and 20.2, 2000 40.3 and 32.9,
 // 3000 47.0 and 42.4.  768: 200 20.6 and 24.8.)
+// Divided items of heads of 64 have 64 rows rather than 128, two sets of waves (16
+// heads over 2, us with 128 rows and with 64: 2 x 26 nodes over 99000 to 131000 keys
+// 50.8 and 49.2, 2 x 16 over 8000 18.7 and 15.8, 64 x 32 over 8000 96.9 and 92.9; heads
+// of 96 and 128 lose by it, 64 blocks 261 and 302).
 static CaPlan ca_tree_plan(int B, int H, int Hk, int D, int max_q, int table_w, int* whole) {
   const long long rows = (long long)max_q * (H / Hk);
   const int mt = rows <= 16 ? 16 : 32;
@@ -828,7 +832,10 @@ static CaPlan ca_tree_plan(int B, int H, int Hk, int D, int max_q, int table_w, 
   const int held = D == 64 ? 512 : 256;   // by LDS: two workgroups a CU, or one
   *whole = 0;
   const long long most = all <= held ? 32 + (all < 256 ? all : 256) / 2 : all <= 2 * held ? 64 : 0;
-  if (table_w > most) return ca_plan(B, H, Hk, D, max_q, table_w);
+  if (table_w > most) {
+    const CaPlan wide = ca_plan(B, H, Hk, D, max_q, table_w), narrow = ca_plan(B, H, Hk, D, max_q, table_w, D == 64 ? 2 : 4);
+    return narrow.bytes <= wide.bytes ? narrow : wide;   // (the workspace is asked for by the wide plan)
+  }
   CaPlan p{};
   p.mt = mt, p.wr = 1;
   p.items = *whole = (int)items;
