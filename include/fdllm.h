@@ -640,9 +640,8 @@ fdllm_status fdllm_tree_attention(const void* q, int64_t q_stride, int T, const 
  *   weight 0.  Numbers are floats in [0, 1): negative ones and NaN with a sign
  *   count as 0, others outside as 1 - 2^-24.  Probabilities, sums and comparisons
  *   are formed in 64 bits (a relative error below 1e-12), so that the token is the
- *   definition's unless u lies that near a border; equal float logits have borders
- *   exactly where the definition has them.
- * Results are packed as the rows are: of a request's rows the first n_tokens get
+ *   definition's unless u lies that near a border.
+ * Results (not in the place of an input) are packed as the rows are: of a request's rows the first n_tokens get
  *   the tokens that follow (the drafted ones that stand, then the one drawn), the
  *   others -1.  logp [T] float (may be NULL): the logarithms of their
  *   probabilities p, 0 for the others.  Rows of no request are not written;
@@ -702,7 +701,7 @@ fdllm_status fdllm_verify_tree(const void* logits, int64_t logits_stride, fdllm_
  *   An entry path[i] that is not at least i and below n moves nothing, neither
  *   does one whose page, or its place's, the table does not have; a request with
  *   n_path outside [0, n] is left as it is;
- *   kv_out [B] int32 (out, may be NULL; not kv_len itself): the new length, kv_len - n +
+ *   kv_out [B] int32 (out, may be NULL; not kv_len or n_path itself): the new length, kv_len - n +
  *   n_path (kv_len for a request that is left as it is).
  * Requests must not share pages that they write.  Sizes (FDLLM_ERR_SIZE beyond):
  * layers * Hk below 2^24, B at most 65535, max_q at most FDLLM_MAX_TREE; D a multiple of

@@ -194,7 +194,7 @@ fdllm_status fdllm_cache_keep(uint8_t* cache, int layers, int n_pages, int Hk, i
   if (fdllm_cache_tile_bytes(D, &tile) != FDLLM_OK) return FDLLM_ERR_SIZE;
   if ((long long)layers * Hk >= (1 << 24) || B > 65535 || max_q > FDLLM_MAX_TREE || n_pages > INT32_MAX / kPage) return FDLLM_ERR_SIZE;
   if (B == 0) return FDLLM_OK;
-  if (!kv_len || !cu_q || !n_path || kv_out == kv_len) return FDLLM_ERR_INVALID_ARG;
+  if (!kv_len || !cu_q || !n_path || kv_out == kv_len || (kv_out && kv_out == n_path)) return FDLLM_ERR_INVALID_ARG;
   const int tiles = n_pages > 0 && table_width > 0 && T > 0 ? layers * Hk : 0;
   if (tiles && (!cache || !page_table || !path || ((uintptr_t)cache & 15))) return FDLLM_ERR_INVALID_ARG;
   const KeepArgs a{cache, tiles, n_pages, Hk, D, page_table, tiles ? table_width : 0, kv_len, cu_q, T, B, max_q, path, n_path, kv_out};

@@ -51,7 +51,7 @@ struct VfArgs {
   int32_t* n_tokens;
   float* logp;               // may be null
   struct VfPart* part;       // [sides][T][chunks]
-  double* rest;              // [B][chunks]: sums of max(p - q, 0)
+  double* rest;              // [B][pieces]: sums of max(p - q, 0)
   struct VfChoice* choice;   // [B]
   bool together;             // the decision forms rest as well
   int32_t* drawn;            // [T]: a tree's tokens
@@ -343,11 +343,16 @@ k_vf_sums(const VfArgs a) {
           }
         }
       }
-      float m = kNegInf;
+      float m = kNegInf, some = -kNegInf;   // the least of the vectors' maxima tells whether one is empty
+      float most[Row::Vecs];
 #pragma unroll
-      for (int j = 0; j < Row::Vecs; ++j)
+      for (int j = 0; j < Row::Vecs; ++j) {
+        most[j] = x.at(j, 0);
 #pragma unroll
-        for (int e = 0; e < Row::Per; ++e) m = fmaxf(m, x.at(j, e));
+        for (int e = 1; e < Row::Per; ++e) most[j] = fmaxf(most[j], x.at(j, e));
+        m = fmaxf(m, most[j]);
+        some = fminf(some, most[j]);
+      }
       m = wave_max(m);
       double s = 0.0;
       int at = 0;
@@ -362,13 +367,21 @@ k_vf_sums(const VfArgs a) {
       } else if (m > kNegInf) {
         const double M = m;
         double s1 = 0.0;
-#pragma unroll
-        for (int j = 0; j < Row::Vecs; ++j)
+        const auto add = [&](int j) {
 #pragma unroll
           for (int e = 0; e < Row::Per; e += 2) {
             s += exp2_steps(fmax((double)x.at(j, e) - M, lowest), rq.c, s_table);
             s1 += exp2_steps(fmax((double)x.at(j, e + 1) - M, lowest), rq.c, s_table);
           }
+        };
+        if (!__any(some == kNegInf)) {
+#pragma unroll
+          for (int j = 0; j < Row::Vecs; ++j) add(j);
+        } else {   // a filter has left few tokens: vectors without any are passed over
+#pragma unroll
+          for (int j = 0; j < Row::Vecs; ++j)
+            if (__any(most[j] > kNegInf)) add(j);
+        }
         s = wave_sum_f64(s + s1);
       }
       if (lane == 0) a.part[place] = VfPart{s, m, at};
@@ -749,7 +762,7 @@ k_vd_decide(const VfArgs a) {
   r = s_choice[who];
   const int m = r.row;   // drafts that stand
   r.row += first;
-  r.rest = warm && m < n - 1 && r.q.Z > 0.0;
+  r.rest = warm && m < n - 1 && r.q.Z > 0.0 && r.p.Z > 0.0;
   if (writes) {
     if (tid == 0) {
       a.choice[b] = r;
@@ -765,7 +778,7 @@ k_vd_decide(const VfArgs a) {
   }
   if (!a.draft) {
     draw_next<F32>(a, b, r, warm, c, s_table, &s_draw);
-  } else if (a.together && r.rest && r.p.Z > 0.0) {
+  } else if (a.together && r.rest) {
     const VfWeights<F32> weights(a.logits + (size_t)r.row * a.stride, r.p, a.draft + (size_t)r.row * a.draft_stride, r.q, c, -1);
     const int pieces = a.chunks * kVdPieces;
     rest_sums(weights, a.V, blockIdx.x * kVdWaves + wave, pieces, gridDim.x * kVdWaves, a.rest + (size_t)b * pieces, s_table, lane);
@@ -781,7 +794,7 @@ k_vd_rest(const VfArgs a) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const auto has_rest = [&](int b) {
     const VfChoice& r = a.choice[b];
-    return r.row >= 0 && r.rest && r.p.Z > 0.0;
+    return r.row >= 0 && r.rest;
   };
   fill_table(s_table);
   __syncthreads();
@@ -802,7 +815,7 @@ k_vd_rest(const VfArgs a) {
     const int k = (int)(u / pieces);            // the k-th of them
     const int L = __ffsll((unsigned long long)__ballot(incl > k)) - 1;
     int b = L * per, left = k - __builtin_amdgcn_readlane(incl - mine, L);
-    while (!has_rest(b) || left-- > 0) ++b;
+    while (b < a.B - 1 && (!has_rest(b) || left-- > 0)) ++b;
     const long long upto = min(u_end, (long long)(k + 1) * pieces);
     const VfChoice r = a.choice[b];
     double c = 0.0;
@@ -1022,7 +1035,7 @@ fdllm_status fdllm_verify_draft(const void* logits, int64_t logits_stride, const
   if (ok == FDLLM_OK && draft_logits) ok = vf_check(draft_logits, draft_stride, dtype, T, V, cu_q, B, max_q, n_tokens);
   if (ok != FDLLM_OK) return ok;
   if (B == 0) return FDLLM_OK;
-  if (T > 0 && (!ids || !u || !u_draw || !tokens)) return FDLLM_ERR_INVALID_ARG;
+  if (T > 0 && (!ids || !u || !u_draw || !tokens || tokens == ids)) return FDLLM_ERR_INVALID_ARG;
   const VfPlan p = vf_plan(T, B, V, false, draft_logits != nullptr);
   if ((uintptr_t)workspace & 15) return FDLLM_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < p.bytes) return FDLLM_ERR_WORKSPACE;
@@ -1047,7 +1060,9 @@ fdllm_status fdllm_verify_tree(const void* logits, int64_t logits_stride, fdllm_
   const fdllm_status ok = vf_check(logits, logits_stride, dtype, T, V, cu_q, B, max_q, n_tokens);
   if (ok != FDLLM_OK) return ok;
   if (B == 0) return FDLLM_OK;
-  if (T > 0 && (!ids || !parents || !u || !path || !tokens)) return FDLLM_ERR_INVALID_ARG;
+  if (T > 0 && (!ids || !parents || !u || !path || !tokens || tokens == ids || tokens == parents || path == ids || path == parents ||
+                path == tokens))
+    return FDLLM_ERR_INVALID_ARG;
   const VfPlan p = vf_plan(T, B, V, true, false);
   if ((uintptr_t)workspace & 15) return FDLLM_ERR_INVALID_ARG;
   if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return FDLLM_ERR_WORKSPACE;

@@ -13,6 +13,7 @@ HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))
 P = ctypes.c_void_p(0x1000)      # never dereferenced: checks fail first
 ODD = ctypes.c_void_p(0x1004)
 ODD1 = ctypes.c_void_p(0x1001)
+Q, R = ctypes.c_void_p(0x2000), ctypes.c_void_p(0x3000)
 
 
 @pytest.fixture(scope="module")
@@ -61,21 +62,21 @@ def _attention(lib, **kw):
     (dict(width=1 << 26), fd.ERR_SIZE), (dict(q=None), fd.ERR_INVALID_ARG), (dict(cu=None), fd.ERR_INVALID_ARG),
     (dict(kv=None), fd.ERR_INVALID_ARG), (dict(cache=None), fd.ERR_INVALID_ARG), (dict(table=None), fd.ERR_INVALID_ARG),
     (dict(out=None), fd.ERR_INVALID_ARG), (dict(q=ODD), fd.ERR_INVALID_ARG), (dict(qs=252), fd.ERR_INVALID_ARG),
-    (dict(qs=260), fd.ERR_INVALID_ARG), (dict(ws=None), fd.ERR_WORKSPACE), (dict(bytes=1), fd.ERR_WORKSPACE),
+    (dict(qs=260), fd.ERR_INVALID_ARG), (dict(ws=None, width=200), fd.ERR_WORKSPACE), (dict(bytes=1, width=200), fd.ERR_WORKSPACE),
     (dict(T=0), fd.OK), (dict(B=0), fd.OK), (dict(max_q=0), fd.OK)])
 def test_attention_refuses(lib, kw, status):
     assert _attention(lib, **kw) == status
 
 
 def _draft(lib, **kw):
-    a = dict(logits=P, stride=100, draft=P, dstride=100, dt=0, T=6, V=100, ids=P, cu=P, B=2, max_q=4, temp=P, u=P, ud=P, tokens=P,
+    a = dict(logits=P, stride=100, draft=P, dstride=100, dt=0, T=6, V=100, ids=P, cu=P, B=2, max_q=4, temp=P, u=P, ud=P, tokens=Q,
              n=P, logp=P, ws=P, bytes=1 << 40)
     a.update(kw)
     return lib.fdllm_verify_draft(*a.values(), None)
 
 
 def _tree(lib, **kw):
-    a = dict(logits=P, stride=100, dt=0, T=6, V=100, ids=P, parents=P, cu=P, B=2, max_q=4, temp=P, u=P, path=P, tokens=P, n=P,
+    a = dict(logits=P, stride=100, dt=0, T=6, V=100, ids=P, parents=P, cu=P, B=2, max_q=4, temp=P, u=P, path=R, tokens=Q, n=P,
              logp=P, ws=P, bytes=1 << 40)
     a.update(kw)
     return lib.fdllm_verify_tree(*a.values(), None)
@@ -89,7 +90,7 @@ def _tree(lib, **kw):
     (dict(stride=99), fd.ERR_INVALID_ARG), (dict(stride=1 << 60), fd.ERR_SIZE), (dict(cu=None), fd.ERR_INVALID_ARG),
     (dict(n=None), fd.ERR_INVALID_ARG), (dict(logits=None), fd.ERR_INVALID_ARG), (dict(logits=ODD1), fd.ERR_INVALID_ARG),
     (dict(logits=ctypes.c_void_p(0x1002), dt=1), fd.ERR_INVALID_ARG), (dict(ids=None), fd.ERR_INVALID_ARG),
-    (dict(u=None), fd.ERR_INVALID_ARG), (dict(tokens=None), fd.ERR_INVALID_ARG), (dict(ws=ODD), fd.ERR_INVALID_ARG),
+    (dict(u=None), fd.ERR_INVALID_ARG), (dict(tokens=P), fd.ERR_INVALID_ARG), (dict(tokens=None), fd.ERR_INVALID_ARG), (dict(ws=ODD), fd.ERR_INVALID_ARG),
     (dict(ws=None), fd.ERR_WORKSPACE), (dict(bytes=95), fd.ERR_WORKSPACE), (dict(B=0), fd.OK)])
 def test_verify_refuses(lib, call, kw, status):
     assert call(lib, **kw) == status
@@ -98,7 +99,8 @@ def test_verify_refuses(lib, call, kw, status):
 @pytest.mark.parametrize("call,kw,status", [
     (_draft, dict(dstride=99), fd.ERR_INVALID_ARG), (_draft, dict(draft=ODD1), fd.ERR_INVALID_ARG),
     (_draft, dict(ud=None), fd.ERR_INVALID_ARG), (_tree, dict(parents=None), fd.ERR_INVALID_ARG),
-    (_tree, dict(path=None), fd.ERR_INVALID_ARG)])
+    (_tree, dict(path=None), fd.ERR_INVALID_ARG), (_tree, dict(path=P), fd.ERR_INVALID_ARG),
+    (_tree, dict(path=Q), fd.ERR_INVALID_ARG)])
 def test_verify_refuses_more(lib, call, kw, status):
     assert call(lib, **kw) == status
 
@@ -131,7 +133,7 @@ def _keep(lib, **kw):
     (dict(pages=1 << 26), fd.ERR_SIZE), (dict(kv=None), fd.ERR_INVALID_ARG), (dict(cu=None), fd.ERR_INVALID_ARG),
     (dict(n=None), fd.ERR_INVALID_ARG), (dict(path=None), fd.ERR_INVALID_ARG), (dict(cache=None), fd.ERR_INVALID_ARG),
     (dict(cache=ODD), fd.ERR_INVALID_ARG), (dict(table=None), fd.ERR_INVALID_ARG), (dict(out=P), fd.ERR_INVALID_ARG),
-    (dict(B=0), fd.OK)])
+    (dict(n=R, out=R), fd.ERR_INVALID_ARG), (dict(B=0), fd.OK)])
 def test_keep_refuses(lib, kw, status):
     assert _keep(lib, **kw) == status
 
