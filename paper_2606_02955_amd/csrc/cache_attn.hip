@@ -683,11 +683,15 @@ k_cache_join(const CacheAttnArgs a, int wgs) {
         p.v[k][i] = *(const f32x4*)(a.part + ((tile * Quads + q0 + min(set * QPer + i, Own - 1)) * kWave + lane) * 4);
     }
   };
-  Parts next;
-  load(g0 + sp * Ahead, next);
+  Parts p, next;   // in many shares the next ones are under way
+  if constexpr (Split > 1) load(g0 + sp * Ahead, next);
   for (int g = g0 + sp * Ahead; g <= g1; g += Split * Ahead) {
-    const Parts p = next;
-    if (Split > 1 && g + Split * Ahead <= g1) load(g + Split * Ahead, next);
+    if constexpr (Split > 1) {
+      p = next;
+      if (g + Split * Ahead <= g1) load(g + Split * Ahead, next);
+    } else {
+      load(g, p);
+    }
     float to = ref;
 #pragma unroll
     for (int k = 0; k < Ahead; ++k) to = fmaxf(to, p.ml[k].x);
@@ -703,7 +707,6 @@ k_cache_join(const CacheAttnArgs a, int wgs) {
 #pragma unroll
       for (int i = 0; i < QPer; ++i) acc[i] += p.v[k][i] * f;
     }
-    if (Split == 1 && g + Ahead <= g1) load(g + Ahead, next);
   }
   if constexpr (Split > 1) {
     if (part == 0) s_ml[wave][col][0] = ref, s_ml[wave][col][1] = l;
