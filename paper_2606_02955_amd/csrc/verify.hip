@@ -26,8 +26,23 @@
 
 namespace fdllm {
 
-typedef u32x4 u32x4_a2 __attribute__((aligned(2)));   // rows may begin at any element
-typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
+// Rows may begin at any element: 16 bytes of one promise no more alignment than
+// that.  (A type passed as a template's argument would lose its alignment.)
+template <bool F32>
+struct VfVec;
+template <>
+struct VfVec<false> {
+  typedef u32x4 type __attribute__((aligned(2)));
+};
+template <>
+struct VfVec<true> {
+  typedef u32x4 type __attribute__((aligned(4)));
+};
+static_assert(alignof(VfVec<false>::type) == 2 && alignof(VfVec<true>::type) == 4, "alignment of a row");
+template <bool F32>
+__device__ __forceinline__ u32x4 load_16(const char* p) {
+  return *(const typename VfVec<F32>::type*)p;
+}
 
 constexpr int kVfThreads = 256, kVfWaves = kVfThreads / kWave;
 constexpr int kVtThreads = 512;               // of the pass with a table
@@ -114,9 +129,11 @@ __device__ __forceinline__ double weight_of(float x, float M, double c, double l
   return d > lowest ? exp2_steps(d, c, table) : 0.0;
 }
 
-// The request's temperature: c in steps; false for 0.
-__device__ __forceinline__ bool scale_for(const VfArgs& a, int b, double* c) {
-  uint32_t bits = a.temperature ? __float_as_uint(a.temperature[b]) : __float_as_uint(1.0f);
+// A request's temperature: c in steps; false for 0.
+__device__ __forceinline__ uint32_t temperature_of(const VfArgs& a, int b) {
+  return a.temperature ? __float_as_uint(a.temperature[b]) : __float_as_uint(1.0f);
+}
+__device__ __forceinline__ bool scale_for(uint32_t bits, double* c) {
   if (bits == 0 || bits > 0x7f800000u) return false;           // 0, negative, NaN
   bits = min(bits, 0x7f7fffffu);
   *c = 1.44269504088896340736 * kVfSteps / (double)__uint_as_float(bits);
@@ -151,6 +168,42 @@ __device__ __forceinline__ u16x2 places_of(uint32_t word) {
   return w * (unsigned short)2 + ((w >> 15) - (unsigned short)kVtLow);
 }
 
+template <bool F32>
+__device__ __forceinline__ float logit_at(const char* row, int v) {
+  if constexpr (F32) return *(const float*)(row + (size_t)v * 4);
+  else return __uint_as_float((uint32_t)*(const uint16_t*)(row + (size_t)v * 2) << 16);
+}
+
+// 16 bytes of a row from element i on, past whose end nothing can be (-inf): the
+// last 16 that the row has, shifted, so that all lanes load at once.
+template <bool F32>
+__device__ __forceinline__ u32x4 load_end(const char* row, int V, int i) {
+  constexpr int Bits = F32 ? 32 : 16, Per = 128 / Bits;
+  constexpr unsigned long long none = F32 ? 0xff800000ff800000ull : 0xff80ff80ff80ff80ull;
+  unsigned long long lo = none, hi = none;
+  if (V >= Per) {
+    const int from = min(i, V - Per);
+    const u32x4 v = load_16<F32>(row + (size_t)from * (Bits / 8));
+    lo = v[0] | (unsigned long long)v[1] << 32;
+    hi = v[2] | (unsigned long long)v[3] << 32;
+    const int past = min(i - from, Per) * Bits;   // bits to be dropped
+    if (past >= 64) {
+      lo = past == 128 ? none : past == 64 ? hi : hi >> (past - 64) | none << (128 - past);
+      hi = none;
+    } else if (past > 0) {
+      lo = lo >> past | hi << (64 - past);
+      hi = hi >> past | none << (64 - past);
+    }
+  } else {
+#pragma unroll 1
+    for (int e = V - 1; e >= i; --e) {
+      hi = hi << Bits | lo >> (64 - Bits);
+      lo = lo << Bits | __float_as_uint(logit_at<F32>(row, e)) >> (32 - Bits);
+    }
+  }
+  return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
 // ---------------------------------------------------------------------------
 // a lane's logits of a chunk: vectors of 16 bytes, a wave's side by side
 // ---------------------------------------------------------------------------
@@ -165,41 +218,26 @@ struct VfRow {
     else return __uint_as_float(e % 2 ? v[j][e / 2] & 0xffff0000u : v[j][e / 2] << 16);
   }
   __device__ __forceinline__ void load(const char* row, int V, int chunk, int lane) {
-    typedef typename std::conditional<F32, u32x4_a4, u32x4_a2>::type Vec;
     if ((chunk + 1) * kVfChunk <= V) {
       const char* p = row + (size_t)chunk * kVfChunk * Bytes;
 #pragma unroll
-      for (int j = 0; j < Vecs; ++j) v[j] = __builtin_nontemporal_load((const Vec*)(p + (uint32_t)(j * kWave + lane) * 16u));
+      for (int j = 0; j < Vecs; ++j) v[j] = __builtin_nontemporal_load((const typename VfVec<F32>::type*)(p + (uint32_t)(j * kWave + lane) * 16u));
       return;
     }
 #pragma unroll
-    for (int j = 0; j < Vecs; ++j) {   // the row's last: past its end nothing can be
-      const int i = index(chunk, j, lane);
-      if (i + Per <= V) {
-        v[j] = *(const Vec*)(row + (size_t)i * Bytes);
+    for (int j = 0; j < Vecs; ++j) {   // the row's last chunk
+      const int first = index(chunk, j, 0);
+      if (first + kWave * Per <= V) {
+        v[j] = load_16<F32>(row + ((size_t)first + lane * Per) * Bytes);
+      } else if (first < V) {
+        v[j] = load_end<F32>(row, V, first + lane * Per);
       } else {
         const uint32_t none = F32 ? 0xff800000u : 0xff80ff80u;
         v[j] = u32x4{none, none, none, none};
-#pragma unroll
-        for (int e = 0; e < Per; ++e) {
-          if (i + e >= V) continue;
-          if constexpr (F32) {
-            v[j][e] = *(const uint32_t*)(row + (size_t)(i + e) * 4);
-          } else {
-            const uint32_t h = *(const uint16_t*)(row + (size_t)(i + e) * 2);
-            v[j][e / 2] = e % 2 ? (v[j][e / 2] & 0xffffu) | h << 16 : (v[j][e / 2] & 0xffff0000u) | h;
-          }
-        }
       }
     }
   }
 };
-
-template <bool F32>
-__device__ __forceinline__ float logit_at(const char* row, int v) {
-  if constexpr (F32) return *(const float*)(row + (size_t)v * 4);
-  else return __uint_as_float((uint32_t)*(const uint16_t*)(row + (size_t)v * 2) << 16);
-}
 
 // ---------------------------------------------------------------------------
 // the pass over all rows.  The units of work are chunks: of a request those of
@@ -212,14 +250,22 @@ struct VfRequest {
   bool warm;
   double c;
 };
-__device__ __forceinline__ VfRequest request_of(const VfArgs& a, int b) {
+struct VfLoaded {   // what has to be loaded for it (first, so that other things are done meanwhile)
+  int32_t cu[2];
+  uint32_t temperature;
+};
+__device__ __forceinline__ VfLoaded load_request(const VfArgs& a, int b) {
+  return VfLoaded{{a.cu_q[b], a.cu_q[b + 1]}, temperature_of(a, b)};
+}
+__device__ __forceinline__ VfRequest request_of(const VfArgs& a, const VfLoaded& l) {
   VfRequest r;
-  r.n = packed_rows(a.cu_q, b, a.T, a.max_q, &r.first);
+  r.n = packed_rows(l.cu, 0, a.T, a.max_q, &r.first);
   r.c = 0.0;
-  r.warm = scale_for(a, b, &r.c);
+  r.warm = scale_for(l.temperature, &r.c);
   r.rows = r.n + (a.draft && r.warm ? max(r.n - 1, 0) : 0);   // (the drafter's last row is not read)
   return r;
 }
+__device__ __forceinline__ VfRequest request_of(const VfArgs& a, int b) { return request_of(a, load_request(a, b)); }
 
 // Lookup: terms of bfloat16 logits out of a table.
 template <bool F32, bool Lookup>
@@ -237,8 +283,10 @@ k_vf_sums(const VfArgs a) {
   const bool apart = a.B <= kWave;
   const int who = apart ? lane : tid, per = apart ? 1 : (a.B + Threads - 1) / Threads;
   const int b0 = min(who * per, a.B), b1 = min(b0 + per, a.B);
-  int mine = 0;
-  for (int i = b0; i < b1; ++i) mine += request_of(a, i).rows * a.chunks;
+  const VfLoaded loaded = load_request(a, min(b0, a.B - 1));
+  fill_table(s_table);
+  int mine = b0 < b1 ? request_of(a, loaded).rows * a.chunks : 0;
+  for (int i = b0 + 1; i < b1; ++i) mine += request_of(a, i).rows * a.chunks;
   int incl = mine;
 #pragma unroll
   for (int x = 1; x < kWave; x <<= 1) {
@@ -246,7 +294,6 @@ k_vf_sums(const VfArgs a) {
     if (lane >= x) incl += y;
   }
   int units = __builtin_amdgcn_readlane(incl, kWave - 1);
-  fill_table(s_table);
   if (lane == kWave - 1) s_sum[wave] = incl;
   __syncthreads();
   if (!apart) {
@@ -442,18 +489,14 @@ struct VfEight {
   __device__ __forceinline__ void load(const char* row, int V, int at) {
     if (at + kVfEight <= V) {
       if constexpr (F32) {
-        v[0] = *(const u32x4_a4*)(row + (size_t)at * 4);
-        v[1] = *(const u32x4_a4*)(row + (size_t)at * 4 + 16);
+        v[0] = load_16<true>(row + (size_t)at * 4);
+        v[1] = load_16<true>(row + (size_t)at * 4 + 16);
       } else {
-        v[0] = *(const u32x4_a2*)(row + (size_t)at * 2);
+        v[0] = load_16<false>(row + (size_t)at * 2);
       }
     } else {
-#pragma unroll
-      for (int e = 0; e < kVfEight; ++e) {
-        const uint32_t x = __float_as_uint(at + e < V ? logit_at<F32>(row, at + e) : kNegInf);
-        if constexpr (F32) v[e / 4][e % 4] = x;
-        else v[0][e / 2] = e % 2 ? v[0][e / 2] | x : x >> 16;
-      }
+      v[0] = load_end<F32>(row, V, at);
+      if constexpr (F32) v[1] = load_end<F32>(row, V, at + 4);
     }
   }
 };
@@ -702,7 +745,9 @@ k_vd_decide(const VfArgs a) {
   const int b = blockIdx.y;
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const bool writes = blockIdx.x == 0;
-  const VfRequest rq = request_of(a, b);
+  const VfLoaded loaded = load_request(a, b);
+  fill_table(s_table);
+  const VfRequest rq = request_of(a, loaded);
   const int first = rq.first, n = rq.n;
   if (n == 0) {
     if (writes && tid == 0) {
@@ -711,7 +756,6 @@ k_vd_decide(const VfArgs a) {
     }
     return;
   }
-  fill_table(s_table);
   __syncthreads();
   const bool warm = rq.warm, with_q = warm && a.draft;
   const double c = rq.c;
@@ -781,7 +825,7 @@ k_vd_decide(const VfArgs a) {
   } else if (a.together && r.rest) {
     const VfWeights<F32> weights(a.logits + (size_t)r.row * a.stride, r.p, a.draft + (size_t)r.row * a.draft_stride, r.q, c, -1);
     const int pieces = a.chunks * kVdPieces;
-    rest_sums(weights, a.V, blockIdx.x * kVdWaves + wave, pieces, gridDim.x * kVdWaves, a.rest + (size_t)b * pieces, s_table, lane);
+    rest_sums(weights, a.V, blockIdx.x + wave * gridDim.x, pieces, gridDim.x * kVdWaves, a.rest + (size_t)b * pieces, s_table, lane);
   }
 }
 
@@ -819,7 +863,7 @@ k_vd_rest(const VfArgs a) {
     const long long upto = min(u_end, (long long)(k + 1) * pieces);
     const VfChoice r = a.choice[b];
     double c = 0.0;
-    scale_for(a, b, &c);
+    scale_for(temperature_of(a, b), &c);
     const VfWeights<F32> weights(a.logits + (size_t)r.row * a.stride, r.p, a.draft + (size_t)r.row * a.draft_stride, r.q, c, -1);
     const int from = (int)(u - (long long)k * pieces), to = (int)(upto - (long long)k * pieces);
     rest_sums(weights, a.V, from + wave, to, kVfWaves, a.rest + (size_t)b * pieces, s_table, lane);
@@ -835,10 +879,11 @@ k_vd_draw(const VfArgs a) {
   __shared__ VfDrawScratch<kVfWaves> s_draw;
   const int b = blockIdx.x;
   const VfChoice r = a.choice[b];
-  double c = 0.0;
-  const bool warm = scale_for(a, b, &c);
+  const uint32_t temperature = temperature_of(a, b);
   fill_table(s_table);
   if (r.row < 0) return;
+  double c = 0.0;
+  const bool warm = scale_for(temperature, &c);
   __syncthreads();
   draw_next<F32>(a, b, r, warm, c, s_table, &s_draw);
 }
@@ -853,12 +898,12 @@ k_vt_draw(const VfArgs a) {
   __shared__ double s_table[kVfSteps];
   __shared__ VfDrawScratch<kVfWaves> s_draw;
   const int b = blockIdx.y, i = blockIdx.x, tid = threadIdx.x, lane = tid % kWave;
-  const VfRequest rq = request_of(a, b);
-  const int n = rq.n, first = rq.first;
-  if (i >= n) return;
+  const VfLoaded loaded = load_request(a, b);
   fill_table(s_table);
+  const VfRequest rq = request_of(a, loaded);
+  if (i >= rq.n) return;
   __syncthreads();
-  const int r = first + i;
+  const int r = rq.first + i;
   const VfPart* part = a.part + (size_t)r * a.chunks;
   const VfStats sp = row_stats(part, a.chunks, rq.warm, rq.c, lane, s_table);
   VfDrawn y{-1, 0.0f};
@@ -986,8 +1031,9 @@ static void vf_sums(const VfArgs& a, hipStream_t st) {
 template <bool F32>
 static hipError_t vd_launch(const VfArgs& a, hipStream_t st) {
   vf_sums<F32>(a, st);
-  // with a drafter's logits workgroups for all CUs, a wave a piece at most
-  const int most = (a.chunks * kVdPieces + kVdWaves - 1) / kVdWaves, fill = kVdFill / a.B;
+  // with a drafter's logits workgroups for all CUs, of four waves with a piece at least (16 of one
+  // CU: a chain of nine rows of 126464 19.7 us for 18.5)
+  const int most = (a.chunks * kVdPieces + 3) / 4, fill = kVdFill / a.B;
   VfArgs d = a;
   d.together = a.draft && a.B <= kVdTogether;
   const int parts = !d.together ? 1 : fill < most ? fill : most;
