@@ -7,6 +7,8 @@
 
 #include <stdint.h>
 
+#include <initializer_list>
+
 #ifndef FDLLM_HD
 #ifdef __HIPCC__
 #define FDLLM_HD __host__ __device__
@@ -23,6 +25,19 @@ inline FDLLM_HD int packed_rows(const int32_t* cu, int b, int T, int most, int* 
   const int s = cu[b], e = cu[b + 1];
   *first = s;
   return (s >= 0 && s <= e && e <= T && e - s <= most) ? e - s : 0;
+}
+
+// Whether no result of a call lies at an input's address, or another result's
+// (null: not there).
+inline bool apart(std::initializer_list<const void*> results, std::initializer_list<const void*> inputs) {
+  for (const void* const* r = results.begin(); r != results.end(); ++r) {
+    if (!*r) continue;
+    for (const void* i : inputs)
+      if (*r == i) return false;
+    for (const void* const* o = results.begin(); o != r; ++o)
+      if (*r == *o) return false;
+  }
+  return true;
 }
 
 constexpr int kPaRows = 128;   // rows of a row tile: query tokens times the heads of a key head

@@ -1081,10 +1081,12 @@ fdllm_status fdllm_verify_draft(const void* logits, int64_t logits_stride, const
   if (ok == FDLLM_OK && draft_logits) ok = vf_check(draft_logits, draft_stride, dtype, T, V, cu_q, B, max_q, n_tokens);
   if (ok != FDLLM_OK) return ok;
   if (B == 0) return FDLLM_OK;
-  if (T > 0 && (!ids || !u || !u_draw || !tokens || tokens == ids)) return FDLLM_ERR_INVALID_ARG;
+  if (T > 0 && (!ids || !u || !u_draw || !tokens)) return FDLLM_ERR_INVALID_ARG;
   const VfPlan p = vf_plan(T, B, V, false, draft_logits != nullptr);
   if ((uintptr_t)workspace & 15) return FDLLM_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < p.bytes) return FDLLM_ERR_WORKSPACE;
+  if (T > 0 && !apart({tokens, n_tokens, logp}, {logits, draft_logits, ids, cu_q, temperature, u, u_draw, workspace}))
+    return FDLLM_ERR_INVALID_ARG;
   char* ws = (char*)workspace;
   const int es = dtype == FDLLM_F32 ? 4 : 2;
   VfArgs a{};
@@ -1106,12 +1108,12 @@ fdllm_status fdllm_verify_tree(const void* logits, int64_t logits_stride, fdllm_
   const fdllm_status ok = vf_check(logits, logits_stride, dtype, T, V, cu_q, B, max_q, n_tokens);
   if (ok != FDLLM_OK) return ok;
   if (B == 0) return FDLLM_OK;
-  if (T > 0 && (!ids || !parents || !u || !path || !tokens || tokens == ids || tokens == parents || path == ids || path == parents ||
-                path == tokens))
-    return FDLLM_ERR_INVALID_ARG;
+  if (T > 0 && (!ids || !parents || !u || !path || !tokens)) return FDLLM_ERR_INVALID_ARG;
   const VfPlan p = vf_plan(T, B, V, true, false);
   if ((uintptr_t)workspace & 15) return FDLLM_ERR_INVALID_ARG;
   if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return FDLLM_ERR_WORKSPACE;
+  if (T > 0 && !apart({path, tokens, n_tokens, logp}, {logits, ids, parents, cu_q, temperature, u, workspace}))
+    return FDLLM_ERR_INVALID_ARG;
   char* ws = (char*)workspace;
   const int es = dtype == FDLLM_F32 ? 4 : 2;
   VfArgs a{};

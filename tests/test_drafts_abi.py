@@ -105,6 +105,20 @@ def test_verify_refuses_more(lib, call, kw, status):
     assert call(lib, **kw) == status
 
 
+S = ctypes.c_void_p(0x4000)
+
+
+@pytest.mark.parametrize("call,kw", [
+    (_draft, dict(n=P)), (_draft, dict(n=Q)), (_draft, dict(n=R, logp=P)), (_draft, dict(n=R, logp=R)),
+    (_draft, dict(n=R, logp=S, ud=S)), (_draft, dict(n=R, logp=S, temp=S)), (_draft, dict(n=R, logp=S, ws=S)),
+    (_draft, dict(n=R, logp=None, cu=Q)), (_tree, dict(n=P)), (_tree, dict(n=R)), (_tree, dict(n=S, logp=P)),
+    (_tree, dict(n=S, logp=None, cu=R)), (_tree, dict(n=S, logp=None, ws=Q)),
+    (_layout, dict(masks=P)), (_layout, dict(masks=Q, pos=P)), (_layout, dict(masks=Q, pos=R, slots=P)),
+    (_layout, dict(masks=Q, pos=R, slots=R)), (_layout, dict(masks=Q, pos=None, slots=S, table=S))])
+def test_results_in_the_place_of_inputs_are_refused(lib, call, kw):
+    assert call(lib, **kw) == fd.ERR_INVALID_ARG
+
+
 def test_verify_workspace_sizes(lib):
     for args in ((0, 0, 1), (7, 2, 126464), (1, 1, 1)):
         one = fd.fdllm_verify_draft_workspace_size(*args, False)
@@ -133,7 +147,8 @@ def _keep(lib, **kw):
     (dict(pages=1 << 26), fd.ERR_SIZE), (dict(kv=None), fd.ERR_INVALID_ARG), (dict(cu=None), fd.ERR_INVALID_ARG),
     (dict(n=None), fd.ERR_INVALID_ARG), (dict(path=None), fd.ERR_INVALID_ARG), (dict(cache=None), fd.ERR_INVALID_ARG),
     (dict(cache=ODD), fd.ERR_INVALID_ARG), (dict(table=None), fd.ERR_INVALID_ARG), (dict(out=P), fd.ERR_INVALID_ARG),
-    (dict(n=R, out=R), fd.ERR_INVALID_ARG), (dict(B=0), fd.OK)])
+    (dict(n=R, out=R), fd.ERR_INVALID_ARG), (dict(cu=R, out=R), fd.ERR_INVALID_ARG),
+    (dict(path=R, out=R), fd.ERR_INVALID_ARG), (dict(table=R, out=R), fd.ERR_INVALID_ARG), (dict(B=0), fd.OK)])
 def test_keep_refuses(lib, kw, status):
     assert _keep(lib, **kw) == status
 
