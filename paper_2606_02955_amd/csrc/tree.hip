@@ -36,7 +36,7 @@ __device__ __forceinline__ int slot_of(const int32_t* table, int table_w, int b,
 // A workgroup a request, a thread a node.  A node's set of ancestors doubles its
 // reach each round: with A_k(i) the first 2^k of the chain i, parent(i), ... and
 // j_k(i) the node behind them, A_k+1(i) = A_k(i) or A_k(j_k(i)), so a chain of n
-// takes log2 n rounds.  Latency-bound.
+// takes log2 n rounds.  Latency-bound: 26 nodes 2.8 us, 64 trees of 100 to 250 5.4.
 __global__ void __launch_bounds__(FDLLM_MAX_TREE)
 k_tree_layout(const LayoutArgs a) {
   __shared__ unsigned long long s_set[kTlWords][FDLLM_MAX_TREE];

@@ -148,7 +148,7 @@ __device__ __forceinline__ double number_of(float u) {
 // ---------------------------------------------------------------------------
 // Bfloat16 logits are few: between 2^-18 and 64 there are 6144, both signs taken
 // together.  Where a workgroup has many of one temperature it looks 2^(x c) up
-// (four instructions a logit for sixteen), without a reference: for 64 c <= 480 all
+// (7 vector instructions a logit for 23, all counted), without a reference: for 64 c <= 480 all
 // terms and sums are numbers of 64 bits.  Entries lie by the bits of a logit with its
 // sign moved to the end, so that two are told from one word at a time.
 // ---------------------------------------------------------------------------
@@ -243,7 +243,12 @@ struct VfRow {
 // the pass over all rows.  The units of work are chunks: of a request those of
 // its rows, then those of its drafter's.  Every workgroup takes an equal share,
 // whatever the requests' lengths, its waves one chunk after another in turn, the
-// next one's loads under way.
+// next one's loads under way.  Bound by HBM where chunks are many: 48 chains of 3 to
+// 17 rows with their drafter's, 231 MB of bfloat16, 38 us, 6.0 TB/s (95 -> 69 us for
+// the call by the table of terms and nontemporal loads, 5 of it the latter); 16 float
+// trees of 11 to 61 rows of 50021, filtered, 23.5 us, 4.9 TB/s, with 3.4 chunks a wave;
+// by starting and the loads' latency where few: 26 rows of 126464 6.5 us.  (A second
+// chunk under way, workgroups of 1024, three a CU: no gain, or spills.)
 // ---------------------------------------------------------------------------
 struct VfRequest {
   int first, n, rows;   // rows: of both sides
@@ -649,7 +654,8 @@ __device__ VfDrawn draw_token(const VfWeights<F32>& weights, int V, int pieces, 
 // and the draw.  Every workgroup of a request decides by itself, a wave a draft;
 // the first writes it down.  (One launch, the last workgroup of a request to be
 // done drawing, took longer than two: to tell it that the others' sums are written
-// is to write an XCD's cache back, 48 chains 66 -> 114 to 165 us.)
+// is to write an XCD's cache back, 48 chains 66 -> 114 to 165 us.)  Chains of loads
+// that wait for one another: one chain of five rows of 126464 5.0 us, 48 7.3.
 // ---------------------------------------------------------------------------
 constexpr int kVdThreads = 1024, kVdWaves = kVdThreads / kWave;
 constexpr int kVdPiece = kWave * kVfEight, kVdPieces = kVfChunk / kVdPiece;   // pieces of a chunk
@@ -830,7 +836,8 @@ k_vd_decide(const VfArgs a) {
 }
 
 // The same sums apart, where there are many requests: those that a draft fell of,
-// in equal shares whatever their number.
+// in equal shares whatever their number.  48 chains 9.5 us, half of it the terms in
+// 64 bits; the rows come out of the caches.
 template <bool F32>
 __global__ void __launch_bounds__(kVfThreads)
 k_vd_rest(const VfArgs a) {
@@ -871,7 +878,9 @@ k_vd_rest(const VfArgs a) {
   }
 }
 
-// The draw apart, where there are a drafter's logits: a workgroup a request.
+// The draw apart, where there are a drafter's logits: a workgroup a request, three
+// trips to memory (4.6 us for one, 6.0 for 48; the sums loaded beside the choice 0.5
+// less, not kept).
 template <bool F32>
 __global__ void __launch_bounds__(kVfThreads)
 k_vd_draw(const VfArgs a) {
@@ -889,8 +898,9 @@ k_vd_draw(const VfArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// a tree: a draw at every node, a workgroup each; then the walk, a workgroup a
-// request
+// a tree: a draw at every node, a workgroup each (26 nodes 5.0 us, 16 trees of 11
+// to 61 6.0: counts, sums, a chunk, one after another); then the walk, a workgroup
+// a request (2.0)
 // ---------------------------------------------------------------------------
 template <bool F32>
 __global__ void __launch_bounds__(kVfThreads)
