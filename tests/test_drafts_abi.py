@@ -153,6 +153,14 @@ def test_keep_refuses(lib, kw, status):
     assert _keep(lib, **kw) == status
 
 
+@pytest.mark.parametrize("drafted", ["3", "0x4", "3x0", "x", "3x4x5", "-1x2", "32x32"])
+def test_command_refuses(drafted, capsys):
+    from workloads import cached_generation
+    with pytest.raises(SystemExit):
+        cached_generation.main([f"--drafted={drafted}"])
+    assert "WxD" in capsys.readouterr().err
+
+
 # ---- tensors ----
 def _i(*shape):
     return torch.zeros(shape, dtype=torch.int32)

@@ -294,7 +294,11 @@ def main(argv=None):
     ap.add_argument("--temperature", type=float, default=0.0, help="of a generation with drafts")
     ap.add_argument("--seed", type=int, default=0)
     a = ap.parse_args(argv)
-    width, depth = (int(x) for x in a.drafted.split("x")) if a.drafted else (0, 0)
+    width, depth = 0, 0
+    if a.drafted:
+        width, _, depth = (int(x) if x.isdigit() else 0 for x in a.drafted.partition("x"))
+        if not (width and depth and 1 + width * depth <= fd.MAX_TREE):
+            ap.error(f"--drafted {a.drafted}: WxD, with 1 + W * D at most {fd.MAX_TREE}")
     cfg = Config(layers=a.layers)
     lens = [max(1, a.prompt * (a.batch - b) // a.batch) for b in range(a.batch)]
     gen_len = a.blocks * cfg.block
