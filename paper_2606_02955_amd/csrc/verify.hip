@@ -1001,9 +1001,11 @@ static VfPlan vf_plan(int T, int B, int V, bool tree, bool marginals) {
 
 // Workgroups of the pass that the chip holds at a time.
 constexpr int kVfFill = 256 * 4, kVtFill = 256 * 2;
-// Chunks a wave from which the table pays (100 rows of 126464, 1.5 a wave: 21.8 us
-// without and 20.9 with; 400 rows 43 and 33, 800 rows 75 and 52).
-constexpr int kVtChunks = 1;
+// Chunks two waves have from which the table pays (without it and with; 1.1 a wave:
+// 15 chains of 10 rows of 32000 25.2 and 27.4 us, 60 trees of 5 19.6 and 22.3; 1.5, 5
+// trees of 20 rows of 126464: 21.1 and 21.4; 1.8, 24 chains of 10 rows of 32000: 30.8
+// and 29.3; 2.3, 10 of 8 rows of 126464: 32.5 and 30.3; 800 rows of them 75 and 52).
+constexpr int kVtChunks = 3;
 // Requests up to which the decision forms the sums of max(p - q, 0): a workgroup a
 // CU in all, and a request that needs none leaves its CUs idle (8 drafts of
 // 126464: 16 requests 35.4 us together and 39.8 apart, 32 47.4 and 49.2; six, 64
@@ -1029,7 +1031,7 @@ static void vf_sums(const VfArgs& a, hipStream_t st) {
   if (a.T == 0 || a.max_q == 0) return;
   const long long chunks = (long long)a.T * (a.draft ? 2 : 1) * a.chunks;
   if constexpr (!F32) {
-    if (chunks >= (long long)kVtFill * (kVtThreads / kWave) * kVtChunks) {
+    if (2 * chunks >= (long long)kVtFill * (kVtThreads / kWave) * kVtChunks) {
       hipLaunchKernelGGL((k_vf_sums<false, true>), dim3(kVtFill), dim3(kVtThreads), 0, st, a);
       return;
     }

@@ -477,12 +477,13 @@ def _mixed_rows(T, V, seed, dtype=torch.bfloat16):
     return x.to(dtype)
 
 
-def test_many_rows_of_bfloat16(gpu):
-    # rows enough for the terms to be looked up in a table; temperatures that allow it and not
-    V, n, B = 126464, 10, 9
+@pytest.mark.parametrize("B", [9, 11])
+def test_many_rows_of_bfloat16(gpu, B):
+    # rows almost enough, and enough, for the terms to be looked up in a table; temperatures that allow it and not
+    V, n = 126464, 10
     T, cu, parents = n * B, _cu([n] * B), np.tile(_tree(n, 5), B)
     x = _mixed_rows(T, V, 3)
-    temperature = [1.0, 0.2, 0.19, 0.0, 3.0, 1e-3, 1.0, 1.0, 50.0]
+    temperature = [1.0, 0.2, 0.19, 0.0, 3.0, 1e-3, 1.0, 1.0, 50.0, 0.7, 1.0][:B]
     likely = x.float().topk(2, dim=1).indices.numpy()
     ids = np.zeros(T, dtype=np.int64)
     for b in range(B):
