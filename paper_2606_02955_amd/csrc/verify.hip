@@ -478,8 +478,11 @@ __device__ __forceinline__ double probability(float x, const VfStats& r, double 
   const double d = (double)x - (double)r.M;
   return d * c > kVfCut ? exp2_steps(d, c, table) / r.Z : 0.0;
 }
+__device__ __forceinline__ double exponent(float x, const VfStats& r, double c) {
+  return ((double)x - (double)r.M) * c * (0.69314718055994530942 / kVfSteps);
+}
 __device__ __forceinline__ float log_probability(float x, const VfStats& r, double c) {
-  return (float)(((double)x - (double)r.M) * c * (0.69314718055994530942 / kVfSteps) - log(r.Z));
+  return (float)(exponent(x, r, c) - log(r.Z));
 }
 
 // Eight logits from an element on, a thread's of a piece that is looked at again.
@@ -562,22 +565,32 @@ struct VfDrawScratch {
   VfDrawn drawn;
 };
 
-// The token drawn with number u, by a workgroup; all threads get it.  A row is
-// `pieces` pieces of `each` tokens (at most eight a thread), sum_of(piece) the sum
-// of one's weights, the same for every lane that asks.
-constexpr int kVfOwn = 4;   // sums that a lane keeps
+// A row in pieces, sum_of(piece) the sum of one's weights, the same for every lane
+// that asks.  A lane has neighbouring pieces, of which it keeps the first few sums.
+constexpr int kVfOwn = 4;
+struct VfOwn {
+  double sum[kVfOwn];
+};
+template <typename F>
+__device__ __forceinline__ VfOwn own_sums(int pieces, F&& sum_of) {
+  const int lane = threadIdx.x % kWave, per = (pieces + kWave - 1) / kWave, c0 = lane * per, c1 = min(c0 + per, pieces);
+  VfOwn own;
+#pragma unroll
+  for (int i = 0; i < kVfOwn; ++i) own.sum[i] = c0 + i < c1 ? sum_of(c0 + i) : 0.0;
+  return own;
+}
+
+// The token drawn with number u, by a workgroup; all threads get it.  A piece is
+// `each` tokens, at most eight a thread.
 template <bool F32, int Waves, typename F>
 __device__ VfDrawn draw_token(const VfWeights<F32>& weights, int V, int pieces, int each, const double* table, double u,
-                              VfDrawScratch<Waves>* s, F&& sum_of) {
+                              VfDrawScratch<Waves>* s, const VfOwn& own, F&& sum_of) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   // the piece, by every wave for itself: a lane adds up neighbouring pieces
   const int per = (pieces + kWave - 1) / kWave, c0 = min(lane * per, pieces), c1 = min(c0 + per, pieces);
-  double mine = 0.0, own[kVfOwn];
+  double mine = 0.0;
 #pragma unroll
-  for (int i = 0; i < kVfOwn; ++i) {
-    own[i] = c0 + i < c1 ? sum_of(c0 + i) : 0.0;
-    mine += own[i];
-  }
+  for (int i = 0; i < kVfOwn; ++i) mine += own.sum[i];
   for (int k = c0 + kVfOwn; k < c1; ++k) mine += sum_of(k);
   const double incl = wave_scan_f64(mine, lane);
   const double total = readlane_f64(incl, kWave - 1);
@@ -597,7 +610,7 @@ __device__ VfDrawn draw_token(const VfWeights<F32>& weights, int V, int pieces, 
     found = before + w > target;
   };
 #pragma unroll
-  for (int i = 0; i < kVfOwn; ++i) look(L * per + i, readlane_f64(own[i], L));
+  for (int i = 0; i < kVfOwn; ++i) look(L * per + i, readlane_f64(own.sum[i], L));
   for (int k = L * per + kVfOwn; k < min((L + 1) * per, pieces) && !found; ++k) look(k, sum_of(k));
   piece = __builtin_amdgcn_readfirstlane(piece);
   if (piece < 0 || piece >= pieces) return VfDrawn{-1, 0.0f};
@@ -684,10 +697,10 @@ __device__ __forceinline__ void rest_sums(const VfWeights<F32>& weights, int V, 
   }
 }
 
-// The token after the drafts that stand, by a workgroup.
+// The token after the drafts that stand, by a workgroup.  of_rest: own sums of max(p - q, 0).
 template <bool F32, int Waves>
-__device__ void draw_next(const VfArgs& a, int b, const VfChoice& r, bool warm, double c, const double* table,
-                          VfDrawScratch<Waves>* scratch) {
+__device__ void draw_next(const VfArgs& a, int b, const VfChoice& r, bool warm, double c, float u_draw, const VfOwn& of_rest,
+                          const double* table, VfDrawScratch<Waves>* scratch) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const char* row = a.logits + (size_t)r.row * a.stride;
   const VfPart* part = a.part + (size_t)r.row * a.chunks;
@@ -697,12 +710,12 @@ __device__ void draw_next(const VfArgs& a, int b, const VfChoice& r, bool warm, 
   } else if (!warm) {
     y.token = r.p.first;
   } else {
-    const double u = number_of(a.u_draw[b]);
+    const double u = number_of(u_draw);
     if (r.rest && a.draft) {
       const VfWeights<F32> w(row, r.p, a.draft + (size_t)r.row * a.draft_stride, r.q, c, -1);
       const int pieces = a.chunks * kVdPieces;
       const double* rest = a.rest + (size_t)b * pieces;
-      y = draw_token(w, a.V, pieces, kVdPiece, table, u, scratch, [&](int k) { return rest[k]; });
+      y = draw_token(w, a.V, pieces, kVdPiece, table, u, scratch, of_rest, [&](int k) { return rest[k]; });
     } else if (r.rest) {
       // all but the draft: its chunk's sum without it
       const int x = a.ids[r.row + 1];
@@ -726,14 +739,14 @@ __device__ void draw_next(const VfArgs& a, int b, const VfChoice& r, bool warm, 
         for (int k = 0; k < Waves; ++k) other += scratch->total[k];
         __syncthreads();
       }
-      y = draw_token(w, a.V, a.chunks, kVfChunk, table, u, scratch,
-                     [&](int ch) { return ch == its ? other : part_weight(part[ch], r.p.M, c, table); });
+      const auto sum_of = [&](int ch) { return ch == its ? other : part_weight(part[ch], r.p.M, c, table); };
+      y = draw_token(w, a.V, a.chunks, kVfChunk, table, u, scratch, own_sums(a.chunks, sum_of), sum_of);
     }
     if (y.token < 0) {
       const VfWeights<F32> w(row, r.p, nullptr, r.q, c, -1);
       __syncthreads();
-      y = draw_token(w, a.V, a.chunks, kVfChunk, table, u, scratch,
-                     [&](int ch) { return part_weight(part[ch], r.p.M, c, table); });
+      const auto sum_of = [&](int ch) { return part_weight(part[ch], r.p.M, c, table); };
+      y = draw_token(w, a.V, a.chunks, kVfChunk, table, u, scratch, own_sums(a.chunks, sum_of), sum_of);
     }
   }
   if (tid == 0) {
@@ -748,6 +761,7 @@ k_vd_decide(const VfArgs a) {
   __shared__ double s_table[kVfSteps];
   __shared__ VfChoice s_choice[kVdWaves];
   __shared__ VfDrawScratch<kVdWaves> s_draw;
+  __shared__ double s_exponent[FDLLM_MAX_TREE], s_sum[FDLLM_MAX_TREE];   // of the drafts: their logarithms are taken together
   const int b = blockIdx.y;
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const bool writes = blockIdx.x == 0;
@@ -789,10 +803,9 @@ k_vd_decide(const VfArgs a) {
       if (stands && warm) {
         const double q = with_q ? probability(lq, r.q, c, s_table) : 1.0;
         stands = number_of(u) * q < probability(lx, r.p, c, s_table);
-        if (writes && a.logp && lane == 0) a.logp[first + i] = log_probability(lx, r.p, c);   // (of those that stand)
+        if (lane == 0) s_exponent[i] = exponent(lx, r.p, c), s_sum[i] = r.p.Z;
       } else if (stands) {
         stands = x == r.p.first;
-        if (writes && a.logp && lane == 0) a.logp[first + i] = 0.0f;
       }
     }
     if (!stands) {
@@ -819,15 +832,13 @@ k_vd_decide(const VfArgs a) {
       a.n_tokens[b] = m + 1;
     }
     for (int i = tid; i < n; i += kVdThreads) {
-      if (i < m) a.tokens[first + i] = a.ids[first + i + 1];
-      else if (i > m) {
-        a.tokens[first + i] = -1;
-        if (a.logp) a.logp[first + i] = 0.0f;
-      }
+      if (i == m) continue;   // (the token drawn)
+      a.tokens[first + i] = i < m ? a.ids[first + i + 1] : -1;
+      if (a.logp) a.logp[first + i] = i < m && warm ? (float)(s_exponent[i] - log(s_sum[i])) : 0.0f;
     }
   }
   if (!a.draft) {
-    draw_next<F32>(a, b, r, warm, c, s_table, &s_draw);
+    draw_next<F32>(a, b, r, warm, c, a.u_draw[b], VfOwn{}, s_table, &s_draw);
   } else if (a.together && r.rest) {
     const VfWeights<F32> weights(a.logits + (size_t)r.row * a.stride, r.p, a.draft + (size_t)r.row * a.draft_stride, r.q, c, -1);
     const int pieces = a.chunks * kVdPieces;
@@ -879,8 +890,8 @@ k_vd_rest(const VfArgs a) {
 }
 
 // The draw apart, where there are a drafter's logits: a workgroup a request, three
-// trips to memory (4.6 us for one, 6.0 for 48; the sums loaded beside the choice 0.5
-// less, not kept).
+// trips to memory (4.6 us for one, 6 for 48; the call of 48 63.6 -> 62.4 us by loading
+// the sums beside the choice).
 template <bool F32>
 __global__ void __launch_bounds__(kVfThreads)
 k_vd_draw(const VfArgs a) {
@@ -889,12 +900,16 @@ k_vd_draw(const VfArgs a) {
   const int b = blockIdx.x;
   const VfChoice r = a.choice[b];
   const uint32_t temperature = temperature_of(a, b);
+  // (loaded beside the choice, which says whether they are wanted; the sums are loaded in any case)
+  const float u_draw = a.T > 0 ? a.u_draw[b] : 0.0f;
+  const double* rest = a.rest + (size_t)b * a.chunks * kVdPieces;
+  const VfOwn own = own_sums(a.chunks * kVdPieces, [&](int k) { return rest[k]; });
   fill_table(s_table);
   if (r.row < 0) return;
   double c = 0.0;
   const bool warm = scale_for(temperature, &c);
   __syncthreads();
-  draw_next<F32>(a, b, r, warm, c, s_table, &s_draw);
+  draw_next<F32>(a, b, r, warm, c, u_draw, own, s_table, &s_draw);
 }
 
 // ---------------------------------------------------------------------------
@@ -919,8 +934,8 @@ k_vt_draw(const VfArgs a) {
   VfDrawn y{-1, 0.0f};
   if (sp.Z > 0.0 && rq.warm) {
     const VfWeights<F32> w(a.logits + (size_t)r * a.stride, sp, nullptr, sp, rq.c, -1);
-    y = draw_token(w, a.V, a.chunks, kVfChunk, s_table, number_of(a.u[r]), &s_draw,
-                   [&](int ch) { return part_weight(part[ch], sp.M, rq.c, s_table); });
+    const auto sum_of = [&](int ch) { return part_weight(part[ch], sp.M, rq.c, s_table); };
+    y = draw_token(w, a.V, a.chunks, kVfChunk, s_table, number_of(a.u[r]), &s_draw, own_sums(a.chunks, sum_of), sum_of);
   } else if (sp.Z > 0.0) {
     y.token = sp.first;
   }
