@@ -244,7 +244,7 @@ struct VfRow {
 // its rows, then those of its drafter's.  Every workgroup takes an equal share,
 // whatever the requests' lengths, its waves one chunk after another in turn, the
 // next one's loads under way.  Bound by HBM where chunks are many: 48 chains of 3 to
-// 17 rows with their drafter's, 231 MB of bfloat16, 38 us, 6.0 TB/s (95 -> 69 us for
+// 17 rows with their drafter's, 231 MB of bfloat16, 37.4 us at best, 6.2 TB/s (95 -> 69 us for
 // the call by the table of terms and nontemporal loads, 5 of it the latter); 16 float
 // trees of 11 to 61 rows of 50021, filtered, 23.5 us, 4.9 TB/s, with 3.4 chunks a wave;
 // by starting and the loads' latency where few: 26 rows of 126464 6.5 us.  (A second
@@ -668,7 +668,7 @@ __device__ VfDrawn draw_token(const VfWeights<F32>& weights, int V, int pieces, 
 // the first writes it down.  (One launch, the last workgroup of a request to be
 // done drawing, took longer than two: to tell it that the others' sums are written
 // is to write an XCD's cache back, 48 chains 66 -> 114 to 165 us.)  Chains of loads
-// that wait for one another: one chain of five rows of 126464 5.0 us, 48 7.3.
+// that wait for one another: one chain of five rows of 126464 4.5 us, 48 6.8.
 // ---------------------------------------------------------------------------
 constexpr int kVdThreads = 1024, kVdWaves = kVdThreads / kWave;
 constexpr int kVdPiece = kWave * kVfEight, kVdPieces = kVfChunk / kVdPiece;   // pieces of a chunk
@@ -847,7 +847,7 @@ k_vd_decide(const VfArgs a) {
 }
 
 // The same sums apart, where there are many requests: those that a draft fell of,
-// in equal shares whatever their number.  48 chains 9.5 us, half of it the terms in
+// in equal shares whatever their number.  48 chains 9.6 us, half of it the terms in
 // 64 bits; the rows come out of the caches.
 template <bool F32>
 __global__ void __launch_bounds__(kVfThreads)
@@ -890,7 +890,7 @@ k_vd_rest(const VfArgs a) {
 }
 
 // The draw apart, where there are a drafter's logits: a workgroup a request, three
-// trips to memory (4.6 us for one, 6 for 48; the call of 48 63.6 -> 62.4 us by loading
+// trips to memory (4.6 us for one, 5.5 for 48; the call of 48 63.6 -> 62.4 us by loading
 // the sums beside the choice).
 template <bool F32>
 __global__ void __launch_bounds__(kVfThreads)
