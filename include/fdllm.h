@@ -666,7 +666,8 @@ fdllm_status fdllm_tree_attention(const void* q, int64_t q_stride, int T, const 
  * With temperature 0 a draft stands when it is the highest logit's, and the
  * token drawn is that: neither the drafter's logits nor the numbers are looked
  * at.  A draft whose row of draft_logits cannot have any token falls, and the
- * token is drawn from p; so it is where p - q is positive nowhere.
+ * token is drawn from p; so it is where p - q is positive nowhere (by more than
+ * 2^-39 of p: less cannot be told from equal).
  *   workspace: fdllm_verify_draft_workspace_size() bytes, 16-byte aligned,
  *   scratch between calls.
  */

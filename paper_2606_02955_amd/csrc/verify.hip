@@ -510,7 +510,11 @@ struct VfEight {
 };
 
 // The weights that a token is drawn from: 2^((x - M) c) of a row, without the
-// token `without`, or, where there is a row q, max(p - q, 0).
+// token `without`, or, where there is a row q, max(p - q, 0).  Of that p and q are
+// each off by 1.2e-12 of themselves at most (three terms meet in them) and their
+// products are rounded: where they are equal the difference is what that leaves, of
+// either sign.  So p is taken less by kVfEqual of itself, and equal ones have none.
+constexpr double kVfEqual = 0x1p-39;   // 1.8e-12
 template <bool F32>
 struct VfWeights {
   const char* p;
@@ -520,7 +524,7 @@ struct VfWeights {
   int without;
 
   __device__ VfWeights(const char* p_, const VfStats& sp_, const char* q_, const VfStats& sq_, double c_, int without_)
-      : p(p_), q(q_), sp(sp_), sq(sq_), c(c_), ip(q_ ? 1.0 / sp_.Z : 1.0), iq(q_ ? 1.0 / sq_.Z : 0.0), lowest(kVfCut / c_),
+      : p(p_), q(q_), sp(sp_), sq(sq_), c(c_), ip(q_ ? (1.0 - kVfEqual) / sp_.Z : 1.0), iq(q_ ? 1.0 / sq_.Z : 0.0), lowest(kVfCut / c_),
         without(without_) {}
 
   __device__ __forceinline__ void load(int V, int at, VfEight<F32>& x, VfEight<F32>& y) const {
