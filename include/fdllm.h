@@ -615,7 +615,9 @@ fdllm_status fdllm_tree_layout(const int32_t* parents, int T, const int32_t* cu_
  * Attention of trees over the cache: fdllm_cache_attention with another mask.
  * Every node sees the first kv_len - n keys, and of its request's nodes those
  * whose bits its row of masks has (any bits will do, not only ancestors'; bits
- * from n on are not looked at).  A node that sees nothing gets out = 0 and lse =
+ * from n on are not looked at).  The nodes are the last n of kv_len tokens (negative
+ * counts as 0) also where the table ends before them: what it has no page for, the
+ * context's or a node's, is unseen.  A node that sees nothing gets out = 0 and lse =
  * -inf.  masks [T, mask_words] uint64, mask_words at least ceil(max_q / 64); the other
  * arguments, the values and the limits are those of fdllm_cache_attention, the
  * workspace too (fdllm_cache_attention_workspace_size).
