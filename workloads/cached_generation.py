@@ -183,6 +183,14 @@ class Session:
         return out, steps
 
     # ---- with drafts ----
+    def _need_room(self, tokens: int, positions: int):
+        """Refuses sequences of more tokens than they have pages for, or at positions
+        beyond the model's: their keys would be nowhere and their results anything."""
+        pages, last = self.table.shape[1] * fd.CACHE_PAGE, len(self.model.cos_sin)
+        if tokens > pages or positions > last:
+            raise ValueError(f"no room for the drafts: {tokens} tokens and {positions} positions are needed, a sequence's "
+                             f"pages hold {pages} (Session's room) and the model has {last}")
+
     def drafts(self, roots, width: int, depth: int, temperature: float, generator=None):
         """A drafter that only knows the token before: `width` branches of `depth`
         tokens behind each root (their likeliest, or one drawn for a chain).
@@ -212,6 +220,11 @@ class Session:
         all of them: hidden states [B * n, d]; the nodes' keys and values go into
         the cache behind the others, in the nodes' order."""
         dev, n = self.model.device, ids.shape[1]
+        level = []      # of each node
+        for i, p in enumerate(parents.tolist()):
+            level.append(level[p] + 1 if 0 <= p < i else 0)
+        done = int(self.done.max())
+        self._need_room(done + n, done + max(level) + 1)
         T = self.B * n
         cu = (torch.arange(self.B + 1, device=dev) * n).to(torch.int32)
         kv_len = (self.done + n).to(torch.int32)
@@ -262,9 +275,13 @@ class Session:
 
     def generate_drafted(self, last, width: int = 3, depth: int = 4, temperature: float = 0.0, generator=None):
         """gen_len tokens a sequence behind its prompt, whose last tokens are `last`
-        [B]; returns them and the steps taken."""
+        [B]; returns them and the steps taken.  Sequences need pages for a step's nodes
+        behind their last token but one, and where there are several, of which one that has
+        its tokens goes on beside the others, behind depth + 1 more."""
         dev = self.model.device
         n = 1 + width * depth
+        most = max(self.lens) + self.gen_len - 2 + (depth + 1 if self.B > 1 else 0)    # cached before a step
+        self._need_room(most + n, most + depth + 1)
         out = torch.full((self.B, self.gen_len + n), -1, dtype=torch.int32, device=dev)
         at, steps = torch.zeros(self.B, dtype=torch.long, device=dev), 0
         start = torch.tensor(self.lens, device=dev) - 1     # the last prompt token is the first root
