@@ -102,7 +102,7 @@ class Session:
         order = torch.randperm(self.B * width, generator=torch.Generator().manual_seed(1)).to(torch.int32)
         self.table = order.view(self.B, width).to(dev)
         # the layers' caches one behind the other
-        self.stack = torch.stack([fd.new_cache(self.B * width, c.kv_heads, c.head_dim, dev) for _ in range(c.layers)])
+        self.stack = fd.new_cache(c.layers * self.B * width, c.kv_heads, c.head_dim, dev).unflatten(0, (c.layers, -1))
         self.caches = list(self.stack.unbind(0))
         self.done = torch.tensor(self.lens, device=dev)          # tokens before the active block
         self.block_at = torch.arange(c.block, device=dev)
