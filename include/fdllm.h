@@ -587,6 +587,9 @@ fdllm_status fdllm_prompt_attention(const void* q, int64_t q_stride, const void*
  *   the cache with the n nodes, which are its last, in the nodes' order.  A
  *   request whose counts are out of order, or that has more than max_q rows, is
  *   one without rows.
+ * Results.  They share no memory with an input, the workspace or another result
+ *   (FDLLM_ERR_INVALID_ARG), but that out of fdllm_tree_attention may be its q where
+ *   that is contiguous.
  * Trees.  parents [T] int32: the node of the same request that a node follows,
  *   an earlier one; anything else stands for none (-1: it follows the context).
  */
@@ -603,8 +606,7 @@ fdllm_status fdllm_prompt_attention(const void* q, int64_t q_stride, const void*
  *   node's ancestors: the row of cos_sin for it;
  *   page_table [B, table_width], slots [T] int32 (out; both may be NULL): the
  *   cache slot of a node, -1 where the table has no page for it (or a negative one).
- * Results are not in the place of an input (FDLLM_ERR_INVALID_ARG), and rows of no
- * request are not written.  Sizes (FDLLM_ERR_SIZE beyond): max_q at most
+ * Rows of no request are not written.  Sizes (FDLLM_ERR_SIZE beyond): max_q at most
  * FDLLM_MAX_TREE, B 65535, mask_words 2^16.
  */
 fdllm_status fdllm_tree_layout(const int32_t* parents, int T, const int32_t* cu_q, int B, int max_q,
@@ -644,8 +646,7 @@ fdllm_status fdllm_tree_attention(const void* q, int64_t q_stride, int T, const 
  *   count as 0, others outside as 1 - 2^-24.  Probabilities, sums and comparisons
  *   are formed in 64 bits (a relative error below 1e-12), so that the token is the
  *   definition's unless u lies that near a border.
- * Results (not in the place of an input: FDLLM_ERR_INVALID_ARG) are packed as the
- *   rows are: of a request's rows the first n_tokens get the tokens that follow
+ * Results are packed as the rows are: of a request's rows the first n_tokens get the tokens that follow
  *   (the drafted ones that stand, then the one drawn), the others -1.  logp [T] float (may be NULL): the logarithms of their
  *   probabilities p, 0 for the others.  Rows of no request are not written;
  *   n_tokens of a request without rows is 0.  A row that cannot have any token
@@ -705,9 +706,10 @@ fdllm_status fdllm_verify_tree(const void* logits, int64_t logits_stride, fdllm_
  *   An entry path[i] that is not at least i and below n moves nothing, neither
  *   does one whose page, or its place's, the table does not have; a request with
  *   n_path outside [0, n] is left as it is;
- *   kv_out [B] int32 (out, may be NULL; not in the place of an input): the new
+ *   kv_out [B] int32 (out, may be NULL): the new
  *   length, kv_len - n + n_path (kv_len for a request that is left as it is).
- * Requests must not share pages that they write.  Sizes (FDLLM_ERR_SIZE beyond):
+ * Requests must not share pages that they write, and the cache holds none of the
+ * other arguments (FDLLM_ERR_INVALID_ARG).  Sizes (FDLLM_ERR_SIZE beyond):
  * layers * Hk below 2^24, B at most 65535, max_q at most FDLLM_MAX_TREE; D a multiple of
  * 32, 32 to 256.
  */

@@ -1,10 +1,12 @@
 // attn_work.h -- which rows a packed sequence has, and where the row tiles of
 // prompts whose keys are divided have their scratch: plain functions of the
-// cumulated counts, evaluated on the device (the host does not know them).
+// cumulated counts, evaluated on the device (the host does not know them); and
+// whether a call's results lie apart from its inputs, evaluated on the host.
 // Internal to libfdllm.so; compiled for the host as well, to be tested there.
 #ifndef FDLLM_ATTN_WORK_H
 #define FDLLM_ATTN_WORK_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #include <initializer_list>
@@ -27,15 +29,36 @@ inline FDLLM_HD int packed_rows(const int32_t* cu, int b, int T, int most, int* 
   return (s >= 0 && s <= e && e <= T && e - s <= most) ? e - s : 0;
 }
 
-// Whether no result of a call lies at an input's address, or another result's
-// (null: not there).
-inline bool apart(std::initializer_list<const void*> results, std::initializer_list<const void*> inputs) {
-  for (const void* const* r = results.begin(); r != results.end(); ++r) {
-    if (!*r) continue;
-    for (const void* i : inputs)
-      if (*r == i) return false;
-    for (const void* const* o = results.begin(); o != r; ++o)
-      if (*r == *o) return false;
+// Memory of an argument: `rows` pieces of `bytes`, `stride` bytes from one to the
+// next (null: not there).
+struct Span {
+  uintptr_t p;
+  size_t bytes, stride;
+  long long rows;
+  Span(const void* at, size_t n) : p((uintptr_t)at), bytes(n), stride(n), rows(1) {}
+  Span(const void* at, size_t n, size_t step, long long count) : p((uintptr_t)at), bytes(n), stride(step), rows(count) {}
+};
+
+// Whether a result, of one piece, shares a byte with it: the first piece that ends
+// behind the result's begin is there, and begins before the result's end.
+inline bool meets(const Span& result, const Span& s) {
+  if (!result.p || !s.p || !result.bytes || !s.bytes || s.rows < 1) return false;
+  const uintptr_t begin = result.p, end = result.p + result.bytes;
+  uintptr_t at = s.p;
+  if (begin >= at + s.bytes && s.rows > 1 && s.stride > 0) {
+    const size_t k = (begin - at - s.bytes) / s.stride + 1;
+    at += s.stride * (k < (size_t)s.rows ? k : (size_t)s.rows - 1);
+  }
+  return begin < at + s.bytes && at < end;
+}
+
+// Whether no result of a call shares memory with an input, or another result.
+inline bool apart(std::initializer_list<Span> results, std::initializer_list<Span> inputs) {
+  for (const Span* r = results.begin(); r != results.end(); ++r) {
+    for (const Span& i : inputs)
+      if (meets(*r, i)) return false;
+    for (const Span* o = results.begin(); o != r; ++o)
+      if (meets(*r, *o)) return false;
   }
   return true;
 }

@@ -920,6 +920,19 @@ static fdllm_status ca_call(CacheAttnArgs a, int D, float scale, void* workspace
                         : ca_plan(a.B, a.H, a.Hk, D, a.max_q, a.table_w);
   if (!ca_join_ok(p)) return FDLLM_ERR_SIZE;
   if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return FDLLM_ERR_WORKSPACE;
+  if constexpr (Tree) {
+    // (out may be q itself: a workgroup has read an item's rows of q before it writes them,
+    // and of an item that several have, it writes the join's scratch)
+    const size_t row = (size_t)a.H * D * 2, counts = (size_t)a.B * 4;
+    const bool itself = a.out == a.q && (a.T == 1 || (size_t)a.q_stride * 2 == row);
+    size_t tile = 0;
+    fdllm_cache_tile_bytes(D, &tile);
+    if (!apart({{a.out, a.T * row}, {a.lse, (size_t)a.T * a.H * 4}},
+               {{itself ? nullptr : a.q, row, (size_t)a.q_stride * 2, a.T}, {a.cache, (size_t)a.n_pages * a.Hk * tile},
+                {a.table, counts * a.table_w}, {a.kv_len, counts}, {a.cu_q, counts + 4}, {a.masks, (size_t)a.T * 8 * a.mask_w},
+                {workspace, p.bytes}}))
+      return FDLLM_ERR_INVALID_ARG;
+  }
   char* ws = (char*)workspace;
   a.R = a.H / a.Hk;
   a.c = scale * kLog2e;

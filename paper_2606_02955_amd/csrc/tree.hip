@@ -179,7 +179,10 @@ fdllm_status fdllm_tree_layout(const int32_t* parents, int T, const int32_t* cu_
   if (T == 0 || B == 0 || max_q == 0) return FDLLM_OK;
   if (!parents || !cu_q || !kv_len || !masks || (slots && table_width > 0 && !page_table)) return FDLLM_ERR_INVALID_ARG;
   if ((uintptr_t)masks & 7) return FDLLM_ERR_INVALID_ARG;
-  if (!apart({masks, positions, slots}, {parents, cu_q, kv_len, page_table})) return FDLLM_ERR_INVALID_ARG;
+  const size_t rows = (size_t)T * 4, counts = (size_t)B * 4;
+  if (!apart({{masks, 2 * rows * mask_words}, {positions, rows}, {slots, rows}},
+             {{parents, rows}, {cu_q, counts + 4}, {kv_len, counts}, {page_table, counts * table_width}}))
+    return FDLLM_ERR_INVALID_ARG;
   const LayoutArgs a{parents, T, cu_q, B, max_q, kv_len, page_table, table_width, (unsigned long long*)masks, mask_words,
                      positions, slots};
   const unsigned threads = (unsigned)((max_q + kWave - 1) / kWave * kWave);
@@ -195,7 +198,11 @@ fdllm_status fdllm_cache_keep(uint8_t* cache, int layers, int n_pages, int Hk, i
   if (fdllm_cache_tile_bytes(D, &tile) != FDLLM_OK) return FDLLM_ERR_SIZE;
   if ((long long)layers * Hk >= (1 << 24) || B > 65535 || max_q > FDLLM_MAX_TREE || n_pages > INT32_MAX / kPage) return FDLLM_ERR_SIZE;
   if (B == 0) return FDLLM_OK;
-  if (!kv_len || !cu_q || !n_path || !apart({kv_out}, {kv_len, cu_q, n_path, page_table, path})) return FDLLM_ERR_INVALID_ARG;
+  const size_t counts = (size_t)B * 4;
+  if (!kv_len || !cu_q || !n_path ||
+      !apart({{kv_out, counts}, {cache, (size_t)layers * n_pages * Hk * tile}},
+             {{kv_len, counts}, {cu_q, counts + 4}, {n_path, counts}, {page_table, counts * table_width}, {path, (size_t)T * 4}}))
+    return FDLLM_ERR_INVALID_ARG;
   const int tiles = n_pages > 0 && table_width > 0 && T > 0 ? layers * Hk : 0;
   if (tiles && (!cache || !page_table || !path || ((uintptr_t)cache & 15))) return FDLLM_ERR_INVALID_ARG;
   const KeepArgs a{cache, tiles, n_pages, Hk, D, page_table, tiles ? table_width : 0, kv_len, cu_q, T, B, max_q, path, n_path, kv_out};

@@ -1116,10 +1116,12 @@ fdllm_status fdllm_verify_draft(const void* logits, int64_t logits_stride, const
   const VfPlan p = vf_plan(T, B, V, false, draft_logits != nullptr);
   if ((uintptr_t)workspace & 15) return FDLLM_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < p.bytes) return FDLLM_ERR_WORKSPACE;
-  if (T > 0 && !apart({tokens, n_tokens, logp}, {logits, draft_logits, ids, cu_q, temperature, u, u_draw, workspace}))
+  const size_t es = dtype == FDLLM_F32 ? 4 : 2, rows = (size_t)T * 4, counts = (size_t)B * 4;
+  if (!apart({{tokens, rows}, {n_tokens, counts}, {logp, rows}},
+             {{logits, V * es, logits_stride * es, T}, {draft_logits, V * es, draft_stride * es, T}, {ids, rows}, {cu_q, counts + 4},
+              {temperature, counts}, {u, rows}, {u_draw, counts}, {workspace, p.bytes}}))
     return FDLLM_ERR_INVALID_ARG;
   char* ws = (char*)workspace;
-  const int es = dtype == FDLLM_F32 ? 4 : 2;
   VfArgs a{};
   a.logits = (const char*)logits, a.stride = logits_stride * es;
   a.draft = (const char*)draft_logits, a.draft_stride = draft_stride * es;
@@ -1143,10 +1145,12 @@ fdllm_status fdllm_verify_tree(const void* logits, int64_t logits_stride, fdllm_
   const VfPlan p = vf_plan(T, B, V, true, false);
   if ((uintptr_t)workspace & 15) return FDLLM_ERR_INVALID_ARG;
   if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return FDLLM_ERR_WORKSPACE;
-  if (T > 0 && !apart({path, tokens, n_tokens, logp}, {logits, ids, parents, cu_q, temperature, u, workspace}))
+  const size_t es = dtype == FDLLM_F32 ? 4 : 2, rows = (size_t)T * 4, counts = (size_t)B * 4;
+  if (!apart({{path, rows}, {tokens, rows}, {n_tokens, counts}, {logp, rows}},
+             {{logits, V * es, logits_stride * es, T}, {ids, rows}, {parents, rows}, {cu_q, counts + 4}, {temperature, counts}, {u, rows},
+              {workspace, p.bytes}}))
     return FDLLM_ERR_INVALID_ARG;
   char* ws = (char*)workspace;
-  const int es = dtype == FDLLM_F32 ? 4 : 2;
   VfArgs a{};
   a.logits = (const char*)logits, a.stride = logits_stride * es;
   a.T = T, a.V = V, a.B = B, a.max_q = max_q, a.chunks = p.chunks;
