@@ -644,11 +644,14 @@ fdllm_status fdllm_tree_attention(const void* q, int64_t q_stride, int T, const 
  *   u (w_0 + w_1 + ...); tokens less likely than 2^-500 of the likeliest may have
  *   weight 0.  Numbers are floats in [0, 1): negative ones and NaN with a sign
  *   count as 0, others outside as 1 - 2^-24.  Probabilities, sums and comparisons
- *   are formed in 64 bits (a relative error below 1e-12), so that the token is the
- *   definition's unless u lies that near a border.
- * Results are packed as the rows are: of a request's rows the first n_tokens get the tokens that follow
- *   (the drafted ones that stand, then the one drawn), the others -1.  logp [T] float (may be NULL): the logarithms of their
- *   probabilities p, 0 for the others.  Rows of no request are not written;
+ *   are formed in 64 bits, p and q each within 1.5e-12 of themselves, so that the
+ *   token is the definition's unless u lies within 2.4e-12 of a border, as a share of
+ *   the whole, or, where it is drawn from max(p - q, 0), within 9e-12 over the sum of
+ *   those; and a draft is judged as defined unless u q is within 3e-12 p of p.
+ * Results are packed as the rows are: of a request's rows the first n_tokens get
+ *   the tokens that follow (the drafted ones that stand, then the one drawn), the
+ *   others -1.  logp [T] float (may be NULL): the logarithms of their probabilities
+ *   p, 0 for the others.  Rows of no request are not written;
  *   n_tokens of a request without rows is 0.  A row that cannot have any token
  *   (all -inf) gets -1 for the token drawn, counted in n_tokens, and logp 0.
  *   Rows in more than one request: each must have the same temperature in all.

@@ -1,12 +1,17 @@
-"""Chains whose drafter has the target's probabilities: where p - q is
-positive nowhere the token comes from p, whatever the roundings of p and q are.
+"""Chains whose drafter has the target's probabilities, or nearly: where p - q is
+positive nowhere the token comes from p, whatever the roundings of p and q are, and
+where it is small the borders are as far off as it is smaller.
 
-Bounds as in test_gpu_drafts.py.
+Bounds as in test_gpu_drafts.py; and for a draw from max(p - q, 0), whose weights sum
+to S: p and q are each off by 1.2e-12 of themselves at most (three terms of 3.9e-13),
+p is taken less by 1.9e-12 of itself, so a sum of differences is off by 4.3e-12, and a
+border, a sum by another one, by twice that over S: less than 9e-12 / S.
 """
 import numpy as np
 import pytest
 import torch
 
+from oracle import drafts as od
 from oracle import drafts as od
 from test_gpu_drafts import DEV, _check_draft, _cu, _logits, _numbers, _verify_draft
 
@@ -56,3 +61,26 @@ def test_rows_of_the_same_probabilities(gpu, dtype, V, B):
     got = _verify_draft(gpu, counts, V, logits, draft, ids, None, u, u_draw)
     assert got[1].tolist() == [1] * B
     _check_draft(counts, logits, draft, ids, None, u, u_draw, got[:3])
+
+
+@pytest.mark.parametrize("apart", [1e-2, 1e-4, 1e-6])
+@pytest.mark.parametrize("B", [8, 40])
+def test_drafters_near_the_target(gpu, B, apart):
+    # the draw is from small differences: tokens in the middle of their share of the numbers
+    V, counts = 1000, [2] * B
+    x = _logits(2 * B, V, 11, torch.float32)
+    g = torch.Generator().manual_seed(12)
+    d = x + apart * torch.randn((2 * B, V), generator=g)
+    ids, u = _falls(counts, V, "below", x), _numbers(2 * B, 5)
+    u_draw, want = np.zeros(B, dtype=np.float32), []
+    for b in range(B):
+        p, q = od.softmax(x[2 * b].double().numpy(), 1.0), od.softmax(d[2 * b].double().numpy(), 1.0)
+        w = np.maximum(p - q, 0.0)
+        c = np.cumsum(w)
+        v = int(np.argsort(w)[-1 - b % 8])
+        u_draw[b] = (c[v] - 0.5 * w[v]) / c[-1]
+        token, near = od.draw(w, u_draw[b])
+        assert token == v and near > 9e-12 / c[-1]
+        want.append(v)
+    got = _verify_draft(gpu, counts, V, x.to(DEV), d.to(DEV), ids, None, u, u_draw)
+    assert got[1].tolist() == [1] * B and got[0].tolist()[::2] == want
