@@ -648,6 +648,8 @@ fdllm_status fdllm_tree_attention(const void* q, int64_t q_stride, int T, const 
  *   token is the definition's unless u lies within 2.4e-12 of a border, as a share of
  *   the whole, or, where it is drawn from max(p - q, 0), within 9e-12 over the sum of
  *   those; and a draft is judged as defined unless u q is within 3e-12 p of p.
+ *   Within that a call of another size may give other bits for the same request:
+ *   many rows are summed in another way than few.
  * Results are packed as the rows are: of a request's rows the first n_tokens get
  *   the tokens that follow (the drafted ones that stand, then the one drawn), the
  *   others -1.  logp [T] float (may be NULL): the logarithms of their probabilities

@@ -98,9 +98,11 @@ struct __align__(16) VfChoice {
 // 2^t, t <= 0, in 64 bits: t in steps of 1/128, a table of 2^(j/128) in LDS and
 // the cubic of the remainder: Taylor's, with as much of the fourth term in the
 // square's as leaves the least error (x^4 - a x^2 is smallest over |x| <= 1/2 for a =
-// (sqrt 2 - 1) / 2), off by 3.9e-13 at most.  2^0 is 1 exactly, so that equal logits
-// have borders where the definition has them.  About 15 instructions and a read of
-// LDS; the library's takes three times as many.
+// (sqrt 2 - 1) / 2), off by 3.9e-13 at most.  2^0 is 1 exactly, so that a row of
+// equal logits has its borders where the definition has them (not where terms are
+// looked up, below: those are of logits less 0, not less the highest, and no whole
+// numbers).  About 15 instructions and a read of LDS; the library's takes three times
+// as many.
 // ---------------------------------------------------------------------------
 constexpr int kVfSteps = 128;
 constexpr double kVfCut = -1000.0 * kVfSteps;     // 2^-1000 and less count as nothing
