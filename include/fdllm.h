@@ -622,7 +622,8 @@ fdllm_status fdllm_tree_layout(const int32_t* parents, int T, const int32_t* cu_
  * context's or a node's, is unseen.  A node that sees nothing gets out = 0 and lse =
  * -inf.  masks [T, mask_words] uint64, mask_words at least ceil(max_q / 64); the other
  * arguments, the values and the limits are those of fdllm_cache_attention, the
- * workspace too (fdllm_cache_attention_workspace_size).
+ * workspace too (fdllm_cache_attention_workspace_size).  How the work is divided goes
+ * by table_width: one that is no more than the longest request needs is the fastest.
  */
 fdllm_status fdllm_tree_attention(const void* q, int64_t q_stride, int T, const int32_t* cu_q, int B, int max_q,
                                   int H, int Hk, int D, const uint8_t* cache, int n_pages,

@@ -839,7 +839,10 @@ static CaPlan ca_plan(int B, int H, int Hk, int D, int max_q, int table_w, int m
 // 15.3, 3000 19.0 and 19.2, 4000 20.5 and 23.3.  64 items: 4000 25.2 and 23.6, 8000 29.6
 // and 39.3.  128: 4000 29.2 and 25.2, 6000 33.0 and 32.5.  256: 1000 24.8 and 12.9, 8000
 // 54.6 and 46.1.  512, twice what the chip holds: 500 27.5 and 20.2, 2000 40.3 and 32.9,
-// 3000 47.0 and 42.4.  768: 200 20.6 and 24.8.)
+// 3000 47.0 and 42.4.  768: 200 20.6 and 24.8.  Heads of 64 and 96 go by these and by
+// how many items the chip holds.)  Keys are counted by the table's width, all that the
+// host knows of a length: 16 nodes over 500 keys take 9.6 us with a table of 9 pages and
+// 13.0 with one of 64 to 2048, divided for lengths that are not there.
 // Divided items of heads of 64 have 64 rows rather than 128, two sets of waves (16
 // heads over 2, us with 128 rows and with 64: 2 x 26 nodes over 99000 to 131000 keys
 // 50.8 and 49.2, 2 x 16 over 8000 18.7 and 15.8, 64 x 32 over 8000 96.9 and 92.9; heads

@@ -246,11 +246,12 @@ struct VfRow {
 // its rows, then those of its drafter's.  Every workgroup takes an equal share,
 // whatever the requests' lengths, its waves one chunk after another in turn, the
 // next one's loads under way.  Bound by HBM where chunks are many: 48 chains of 3 to
-// 17 rows with their drafter's, 231 MB of bfloat16, 37.4 us at best, 6.2 TB/s (95 -> 69 us for
-// the call by the table of terms and nontemporal loads, 5 of it the latter); 16 float
-// trees of 11 to 61 rows of 50021, filtered, 23.5 us, 4.9 TB/s, with 3.4 chunks a wave;
-// by starting and the loads' latency where few: 26 rows of 126464 6.5 us.  (A second
-// chunk under way, workgroups of 1024, three a CU: no gain, or spills.)
+// 17 rows with their drafter's, 231 MB of bfloat16, 43 us in the middle and
+// 37.4 at best, 5.4 and 6.2 TB/s (95 -> 69 us for the call by the table of terms and
+// nontemporal loads, 5 of it the latter); 16 float trees of 11 to 61 rows of 50021,
+// filtered, 23.5 us, 4.9 TB/s, with 3.4 chunks a wave; by starting and the loads' latency
+// where few: 26 rows of 126464 6.5 us.  (A second chunk under way, workgroups of 1024,
+// three a CU: no gain, or spills.)
 // ---------------------------------------------------------------------------
 struct VfRequest {
   int first, n, rows;   // rows: of both sides
@@ -1026,6 +1027,9 @@ constexpr int kVfFill = 256 * 4, kVtFill = 256 * 2;
 // 15 chains of 10 rows of 32000 25.2 and 27.4 us, 60 trees of 5 19.6 and 22.3; 1.5, 5
 // trees of 20 rows of 126464: 21.1 and 21.4; 1.8, 24 chains of 10 rows of 32000: 30.8
 // and 29.3; 2.3, 10 of 8 rows of 126464: 32.5 and 30.3; 800 rows of them 75 and 52).
+// It is a loss where requests of few chunks and other temperatures are many, for each
+// of which it is filled again: calls just below and above the border, trees of two rows
+// of 1000 48.6 and 67.5 us, chains of two 75 and 82, trees of four of 9001 25.7 and 27.5.
 constexpr int kVtChunks = 3;
 // Requests up to which the decision forms the sums of max(p - q, 0): a workgroup a
 // CU in all, and a request that needs none leaves its CUs idle (8 drafts of
