@@ -84,7 +84,8 @@ enum {
 
 typedef int fdllm_status;
 #define FDLLM_OK 0
-#define FDLLM_ERR_INVALID_ARG (-1)       /* null pointer, negative size, bad enum   */
+#define FDLLM_ERR_INVALID_ARG (-1)       /* null pointer, negative size, bad enum,
+                                            a result that overlaps an argument      */
 #define FDLLM_ERR_UNSUPPORTED_DTYPE (-2) /* dtype not FDLLM_BF16 / FDLLM_F32         */
 #define FDLLM_ERR_SIZE (-3)              /* V < 1, or B*L*V beyond 2^62 elements     */
 #define FDLLM_ERR_WORKSPACE (-4)         /* workspace missing or too small           */

@@ -1996,7 +1996,7 @@ extern "C" {
 const char* fdllm_status_string(fdllm_status st) {
   switch (st) {
     case FDLLM_OK: return "ok";
-    case FDLLM_ERR_INVALID_ARG: return "invalid argument (null pointer, negative size or bad enum)";
+    case FDLLM_ERR_INVALID_ARG: return "invalid argument (null pointer, negative size, bad enum, or a result that overlaps an argument)";
     case FDLLM_ERR_UNSUPPORTED_DTYPE: return "unsupported logits dtype";
     case FDLLM_ERR_SIZE: return "unsupported size (V < 1 or too many elements)";
     case FDLLM_ERR_WORKSPACE: return "workspace missing or too small";
